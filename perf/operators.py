@@ -1,0 +1,440 @@
+"""The work that surrounds a byte model's layers, as cases that can be timed and checked.
+
+kind        what it stands for
+embed       tokens to the model's inputs: scaled rows of the embedding table
+embed_grad  the table's gradient, rows summed by token
+conv_grad   the gradient of the causal depthwise convolution (+ Swish) in front of the scan
+clip        the global norm of a model's gradients, and the clipped gradients
+verify      drafted tokens against the target's probabilities from given random numbers, and the
+            token after them; with no draft, the next token
+
+The sizes are those of the MambaByte models (widths 1024, 1792 and 2304, twice that in the layers' channels, 53
+and 48 layers, 256 byte values, 8,192-byte training contexts, drafts of about 16 bytes) and the odd ones that
+texts, drafts and other models bring.
+
+With ``own`` false, ``run`` computes the same in elementary torch operations in 32 bits, rounded once at the end.
+"""
+import math
+
+import torch
+
+own = False
+
+K = 4           # taps of the convolution
+N = 16          # states per channel
+DEV = "cuda:0"
+WIDTHS = (1024, 1792, 2304)
+EPS = 1e-6      # added to the norm where gradients are clipped
+
+
+def listed():
+    return [
+        # the last byte of a batch of 32 prompts
+        dict(name="embed_b32", kind="embed", n=32, vocab=256, dim=1792, dtype="bf16", tokens="int32"),
+        # a training batch of bytes
+        dict(name="embed_b4_L8192", kind="embed", n=32768, vocab=256, dim=1792, dtype="bf16", tokens="uint8"),
+        # its gradient: 256 rows of which the commonest bytes take thousands of tokens each
+        dict(name="embed_grad_b4_L8192", kind="embed_grad", n=32768, vocab=256, dim=1792, dtype="bf16", out="f32",
+             tokens="uint8"),
+        # a subword drafter's table, contexts of 2,048 padded at their ends: most rows take no token at all
+        dict(name="embed_grad_v32000", kind="embed_grad", n=16384, vocab=32000, dim=768, dtype="f32", out="f32",
+             tokens="int64"),
+        # the 972M layer's convolution in a training step
+        dict(name="conv_grad_b4_L8192", kind="conv_grad", batch=4, dim=3584, L=8192, dtype="bf16", state=False),
+        # fine-tuning in fp32 on a continued document of odd length
+        dict(name="conv_grad_f32_b2_L1021", kind="conv_grad", batch=2, dim=1536, L=1021, dtype="f32", state=True),
+        # one fine-tuned layer whose gradients are within the bound: nothing changes
+        dict(name="clip_layer_f32", kind="clip", width=1024, layers=1, dtype="f32", align=64, clipped=False),
+        # the 353M model, matrices in bf16 and the rest in fp32
+        dict(name="clip_353m_bf16", kind="clip", width=1024, layers=53, dtype="bf16", align=64, clipped=True),
+        # the 972M model in fp32, gradients one after the other in one buffer, without gaps
+        dict(name="clip_972m_f32", kind="clip", width=1792, layers=48, dtype="f32", align=1, clipped=True),
+        # the next byte of one prompt: a draw from its distribution
+        dict(name="next_b1", kind="verify", batch=1, n=0, vocab=256, dtype="f32", draft="none", ragged=False),
+        # 16 drafted bytes of 32 prompts, with the drafter's own distributions
+        dict(name="verify_b32_n16", kind="verify", batch=32, n=16, vocab=256, dtype="f32", draft="logits", ragged=False),
+        # subword drafts of up to 4 tokens for 16 prompts
+        dict(name="verify_b16_n4_v32000", kind="verify", batch=16, n=4, vocab=32000, dtype="bf16", draft="logits",
+             ragged=True),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(("embed", "embed_grad", "conv_grad", "clip", "verify"))
+    dtype = "f32" if rng.random() < 0.35 else "bf16"
+    c = dict(kind=kind, dtype=dtype)
+    if kind in ("embed", "embed_grad"):
+        c["vocab"] = 256 if rng.random() < 0.5 else _log(rng, 100, 65536)
+        c["dim"] = rng.choice(WIDTHS) if rng.random() < 0.5 else _log(rng, 64, 2304)
+        c["tokens"] = rng.choice(("uint8", "int32", "int64") if c["vocab"] <= 256 else ("int32", "int64"))
+        c["n"] = min(_log(rng, 1 if kind == "embed" else 64, 131072), 32768 * 2304 // c["dim"])
+        if kind == "embed_grad":
+            c["out"] = rng.choice(("f32", "bf16"))
+        return c
+    if kind == "conv_grad":
+        c["batch"] = rng.choice((1, 1, 2, 3, 4))
+        c["dim"] = 2 * rng.choice(WIDTHS) if rng.random() < 0.5 else _log(rng, 256, 4608)
+        # half of the lengths are whole contexts, half are whatever a document has
+        L = min(_log(rng, 64, 32768), (4 * 3584 * 8192) // (c["batch"] * c["dim"]))
+        c["L"] = max(64, L // 64 * 64) if rng.random() < 0.5 else L
+        c["state"] = rng.random() < 0.4
+        return c
+    if kind == "clip":
+        c["width"] = rng.choice(WIDTHS) if rng.random() < 0.5 else _log(rng, 96, 2304)
+        c["layers"] = max(1, min(_log(rng, 1, 53), 48 * 1792 ** 2 // c["width"] ** 2))
+        c["align"] = rng.choice((1, 64))
+        c["clipped"] = rng.random() < 0.7
+        return c
+    c["vocab"] = 256 if rng.random() < 0.6 else _log(rng, 100, 65536)
+    c["n"] = 0 if rng.random() < 0.25 else rng.randint(1, 40 if c["vocab"] <= 4096 else 8)
+    c["batch"] = _log(rng, 1, 64 if c["vocab"] <= 4096 else 16)
+    c["draft"] = rng.choice(("logits", "tokens")) if c["n"] else "none"
+    c["ragged"] = c["n"] > 0 and rng.random() < 0.5
+    return c
+
+
+# ---- inputs -------------------------------------------------------------------
+
+_DT = {"bf16": torch.bfloat16, "f32": torch.float32, "uint8": torch.uint8, "int32": torch.int32, "int64": torch.int64}
+
+
+class _Draws:
+    """Seeded draws on the GPU, in the order asked for."""
+
+    def __init__(self, seed):
+        self.g = torch.Generator(device=DEV)
+        self.g.manual_seed(seed)
+
+    def normal(self, *shape, dtype=torch.float32, scale=1.0):
+        x = torch.randn(shape, generator=self.g, device=DEV)
+        return (x.mul_(scale) if scale != 1.0 else x).to(dtype)
+
+    def uniform(self, *shape):
+        return torch.rand(shape, generator=self.g, device=DEV)
+
+    def exponential(self, *shape):
+        return torch.empty(shape, device=DEV).exponential_(generator=self.g).clamp_(min=1e-20)
+
+    def text(self, n, vocab):
+        """n tokens as frequent as a text's: about 1/rank, the commonest a tenth to a sixth of all for bytes."""
+        share = 1.0 / (torch.arange(vocab, device=DEV) + 1.5)
+        order = torch.randperm(vocab, generator=self.g, device=DEV)
+        return order[torch.multinomial(share, n, replacement=True, generator=self.g)]
+
+
+def _shapes(width, layers):
+    """A MambaByte model's weights: (rows, columns, whether it is one of the large matrices)."""
+    D, r = 2 * width, max(1, width // 16)
+    layer = [(2 * D, width, True), (D, K, False), (D, 1, False), (r + 2 * N, D, True), (D, r, True), (D, 1, False),
+             (D, N, False), (D, 1, False), (width, D, True), (width, 1, False)]
+    return [(256, width, True)] + layer * layers + [(width, 1, False), (256, width, True)]
+
+
+def _tensors(flat, sizes, align):
+    """Views of one buffer, each at the next multiple of `align` elements."""
+    at, views = 0, []
+    for n in sizes:
+        views.append(flat[at:at + n])
+        at += -(-n // align) * align
+    return views
+
+
+def _clip_state(case, r):
+    # fp32 and bf16 tensors lie in a buffer of their own each, as gradients gathered in buckets do
+    act = _DT[case["dtype"]]
+    shapes = _shapes(case["width"], case["layers"])
+    groups = {}
+    for rows, cols, large in shapes:
+        groups.setdefault(act if large else torch.float32, []).append(rows * cols)
+    align, s = case["align"], dict(case=case, grads=[], out=[], flat=[], flat_out=[])
+    total = 0
+    for dtype, sizes in groups.items():
+        n = sum(-(-k // align) * align for k in sizes)
+        flat = r.normal(n, dtype=dtype, scale=1e-3)
+        s["flat"].append(flat)
+        s["grads"] += _tensors(flat, sizes, align)
+        if case["clipped"]:
+            out = torch.zeros_like(flat)
+            s["flat_out"].append(out)
+            s["out"] += _tensors(out, sizes, align)
+        total += sum(sizes)
+    # the norm is about 1e-3 sqrt(total); training clips at 1, or lets the gradients pass
+    s["max_norm"] = 1e-3 * math.sqrt(total) * (0.25 if case["clipped"] else 4.0)
+    return s
+
+
+def prepare(case, seed):
+    r = _Draws(seed)
+    act, kind = _DT[case["dtype"]], case["kind"]
+    s = dict(case=case)
+    if kind in ("embed", "embed_grad"):
+        n, V, d = case["n"], case["vocab"], case["dim"]
+        tokens = r.text(n, V)
+        if case["tokens"] != "uint8" and n >= 64:
+            tokens[-(n // 32):] = -1                    # the padding at the end of a batch
+        s["tokens"] = tokens.to(_DT[case["tokens"]])
+        s["scale"] = math.sqrt(d)
+        if kind == "embed":
+            s["weight"] = r.normal(V, d, dtype=act, scale=0.02)
+        else:
+            s["dy"] = r.normal(n, d, dtype=act)
+        return s
+    if kind == "conv_grad":
+        b, d, L = case["batch"], case["dim"], case["L"]
+        bound = 1.0 / math.sqrt(K)
+        s.update(x=r.normal(b, d, L, dtype=act), dy=r.normal(b, d, L, dtype=act),
+                 w=(r.uniform(d, K) * 2 - 1) * bound, bias=(r.uniform(d) * 2 - 1) * bound, state=None, dstate_out=None)
+        if case["state"]:
+            s.update(state=r.normal(b, d, K - 1), dstate_out=r.normal(b, d, K - 1))
+        return s
+    if kind == "clip":
+        return _clip_state(case, r)
+    b, n, V = case["batch"], case["n"], case["vocab"]
+    # peaked distributions, and a drafter that is near the target: most drafted tokens pass
+    target = r.normal(b, n + 1, V, scale=2.5)
+    drafter = target[:, :n] + r.normal(b, n, V, scale=0.35)
+    s.update(logits=target.to(act), draft_logits=None, lengths=None, temperature=0.8)
+    drafter = drafter.to(act)
+    if case["draft"] == "logits":
+        s["draft_logits"] = drafter
+        race = drafter.float() / s["temperature"] - r.exponential(b, n, V).log_()     # a sample of the drafter's
+        s["draft"] = race.argmax(-1).to(torch.int32)
+    else:
+        s["draft"] = drafter.float().argmax(-1).to(torch.int32)
+    if n == 0:
+        s["draft"] = torch.zeros(b, 0, dtype=torch.int32, device=DEV)
+    if case["ragged"]:
+        s["lengths"] = torch.randint(0, n + 1, (b,), generator=r.g, device=DEV, dtype=torch.int32)
+    s.update(uniform=r.uniform(b, n), noise=r.exponential(b, V))
+    return s
+
+
+# ---- one pass -------------------------------------------------------------------
+
+def run(s):
+    return (_run_own if own else _run_plain)(s)
+
+
+def _run_own(s):
+    import paper_2401_13660_amd as mb
+    c, kind = s["case"], s["case"]["kind"]
+    if kind == "embed":
+        return mb.embedding_fwd(s["tokens"], s["weight"], scale=s["scale"])
+    if kind == "embed_grad":
+        return mb.embedding_bwd(s["tokens"], s["dy"], c["vocab"], scale=s["scale"], out_dtype=_DT[c["out"]])
+    if kind == "conv_grad":
+        g = mb.conv1d_bwd(s["x"], s["w"], s["dy"], s["bias"], s["state"], s["dstate_out"])
+        return g if c["state"] else {k: g[k] for k in ("dx", "dw", "dbias")}
+    if kind == "clip":
+        norm = mb.clip_grad_norm(s["grads"], s["max_norm"], eps=EPS, out=s["out"] if c["clipped"] else None)
+        return {"norm": norm, "grads": s["flat_out"] if c["clipped"] else s["flat"]}
+    accepted, last_pos, next_token, probs = mb.verify_sample(
+        s["logits"], s["draft"], s["uniform"], s["noise"], s["draft_logits"], lengths=s["lengths"],
+        temperature=s["temperature"], return_probs=True)
+    return {"accepted": accepted, "last_pos": last_pos, "next_token": next_token, "probs": probs}
+
+
+def _run_plain(s):
+    c, kind = s["case"], s["case"]["kind"]
+    if kind == "embed":
+        t = s["tokens"].long()
+        factor = torch.where(t >= 0, s["scale"], 0.0)
+        return (s["weight"].float()[t.clamp(min=0)] * factor[:, None]).to(s["weight"].dtype)
+    if kind == "embed_grad":
+        t = s["tokens"].long()
+        rows = torch.where(t >= 0, t, c["vocab"])           # padding: a row past the table's last
+        grad = torch.zeros(c["vocab"] + 1, c["dim"], device=t.device)
+        grad.index_add_(0, rows, s["dy"].float())
+        return (grad[:c["vocab"]] * s["scale"]).to(_DT[c["out"]])
+    if kind == "conv_grad":
+        return _conv_plain(s)
+    if kind == "clip":
+        grads = s["grads"]
+        norm = torch.stack([g.float().square().sum() for g in grads]).sum().sqrt()
+        factor = (s["max_norm"] / (norm + EPS)).clamp(max=1.0)
+        if not c["clipped"]:
+            list(map(lambda g: g.copy_(g.float() * factor), grads))
+            return {"norm": norm, "grads": s["flat"]}
+        list(map(lambda o, g: o.copy_(g.float() * factor), s["out"], grads))
+        return {"norm": norm, "grads": s["flat_out"]}
+    return _verify_plain(s)
+
+
+def _conv_plain(s):
+    x, w, dy = s["x"].float(), s["w"], s["dy"].float()
+    b, d, L = x.shape
+    before = torch.zeros(b, d, K - 1, device=x.device) if s["state"] is None else s["state"]
+    xin = torch.cat([before, x], 2)
+    pre = s["bias"][:, None] + sum(w[:, i:i + 1] * xin[:, :, i:i + L] for i in range(K))
+    sig = torch.sigmoid(pre)
+    g = dy * (sig * (1 + pre * (1 - sig)))
+    zeros = torch.zeros(b, d, K - 1, device=x.device)
+    gz = torch.cat([zeros, g, zeros], 2)                    # g at K - 1 and on
+    dxin = sum(w[:, i:i + 1] * gz[:, :, K - 1 - i:K - 1 - i + L + K - 1] for i in range(K))
+    if s["dstate_out"] is not None:
+        dxin = torch.cat([dxin[:, :, :L], dxin[:, :, L:] + s["dstate_out"]], 2)
+    out = {"dx": dxin[:, :, K - 1:].to(s["dy"].dtype), "dbias": g.sum((0, 2)),
+           "dw": torch.stack([(g * xin[:, :, i:i + L]).sum((0, 2)) for i in range(K)], 1)}
+    if s["state"] is not None:
+        out["dstate"] = dxin[:, :, :K - 1].contiguous()
+    return out
+
+
+def _softmax_plain(logits, temperature):
+    v = logits.float() * (1.0 / temperature)
+    e = torch.exp(v - v.amax(-1, keepdim=True))
+    return e / e.sum(-1, keepdim=True)
+
+
+def _verify_plain(s):
+    b, n = s["draft"].shape
+    V = s["logits"].shape[2]
+    draft = s["draft"].long()[:, :, None]
+    p = _softmax_plain(s["logits"], s["temperature"])
+    if s["draft_logits"] is not None:
+        q = _softmax_plain(s["draft_logits"], s["temperature"])
+    else:
+        q = (torch.arange(V, device=DEV) == draft).float()
+    length = torch.full((b,), n, device=DEV) if s["lengths"] is None else s["lengths"].long()
+    there = torch.arange(n, device=DEV) < length[:, None]
+    probs = p[:, :n].gather(2, draft)[:, :, 0] * there      # the target's of the drafted tokens
+    passes = (s["uniform"] * q.gather(2, draft)[:, :, 0] < probs) & there
+    accepted = passes.int().cumprod(1).sum(1)
+    at = accepted[:, None, None].expand(b, 1, V)
+    target = p.gather(1, at)[:, 0]
+    if n:
+        drafted = q.gather(1, at.clamp(max=n - 1))[:, 0] * (accepted < length)[:, None]
+        left = (target - drafted).clamp(min=0.0)
+        left = torch.where(left.amax(1, keepdim=True) > 0, left, target)
+    else:
+        left = target
+    next_token = (left / s["noise"]).argmax(1)
+    accepted = accepted.int()
+    return {"accepted": accepted, "last_pos": accepted - 1, "next_token": next_token.int(), "probs": probs}
+
+
+# ---- what a pass cannot do without -------------------------------------------------
+
+def work(case):
+    e = 2 if case["dtype"] == "bf16" else 4
+    kind = case["kind"]
+    if kind in ("embed", "embed_grad"):
+        n, V, d = case["n"], case["vocab"], case["dim"]
+        tokens = n * {"uint8": 1, "int32": 4, "int64": 8}[case["tokens"]]
+        if kind == "embed":
+            return {"bytes": tokens + (min(n, V) + n) * d * e, "flops": n * d}
+        return {"bytes": tokens + n * d * e + V * d * (2 if case["out"] == "bf16" else 4), "flops": n * d + V * d}
+    if kind == "conv_grad":
+        el = case["batch"] * case["dim"] * case["L"]
+        side = 4 * case["batch"] * case["dim"] * (K - 1) * (3 if case["state"] else 0) + 2 * 4 * case["dim"] * (K + 1)
+        # the convolution again, Swish and its slope, then K products each for dx and dw
+        return {"bytes": 3 * el * e + side, "flops": el * (2 * K + 10 + 4 * K + 1)}
+    if kind == "clip":
+        b = n = 0
+        for rows, cols, large in _shapes(case["width"], case["layers"]):
+            n += rows * cols
+            b += rows * cols * (e if large else 4)
+        return {"bytes": b * (2 if case["clipped"] else 1), "flops": n * (3 if case["clipped"] else 2)}
+    b, n, V = case["batch"], case["n"], case["vocab"]
+    rows = b * (n + 1) + (b * n if case["draft"] == "logits" else 0)
+    return {"bytes": rows * V * e + b * V * 4 + b * n * 8 + b * 12, "flops": rows * V * 5 + b * V * 3}
+
+
+# ---- 64 bits ----------------------------------------------------------------------
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    kind = case["kind"]
+    if kind == "embed":
+        table = torch.cat([s["weight"].double() * s["scale"], torch.zeros(1, case["dim"], device=DEV).double()])
+        return table[s["tokens"].long()]                    # -1: the row of zeros at the end
+    if kind == "embed_grad":
+        t = s["tokens"].long()
+        order = torch.argsort(t, stable=True)
+        ends = torch.searchsorted(t[order], torch.arange(-1, case["vocab"], device=DEV), right=True)
+        sums = torch.cat([torch.zeros(1, case["dim"], device=DEV).double(), s["dy"].double()[order].cumsum(0)])[ends]
+        return (sums[1:] - sums[:-1]) * s["scale"]
+    if kind == "conv_grad":
+        return _conv64(s)
+    if kind == "clip":
+        grads = torch.cat([g.double() for g in s["flat"]]) if case["align"] == 1 else None
+        if grads is None:
+            norm = math.sqrt(sum(float(g.double().square().sum()) for g in s["grads"]))
+        else:
+            norm = float(grads.square().sum().sqrt())
+            del grads
+        factor = min(1.0, s["max_norm"] / (norm + EPS))
+        if not case["clipped"]:
+            return {"norm": torch.tensor(norm, dtype=torch.float64), "grads": [f.double() for f in s["flat"]]}
+        out = [torch.zeros_like(f, dtype=torch.float64) for f in s["flat"]]
+        base = {f.untyped_storage().data_ptr(): o for f, o in zip(s["flat"], out)}
+        for g in s["grads"]:
+            at = g.storage_offset()
+            base[g.untyped_storage().data_ptr()][at:at + g.numel()] = g.double() * factor
+        return {"norm": torch.tensor(norm, dtype=torch.float64), "grads": out}
+    return _verify64(s)
+
+
+def _verify64(s):
+    """Sequence by sequence, token by token, on logarithms."""
+    b, n = s["draft"].shape
+    V = s["logits"].shape[2]
+    scale = float(torch.tensor(1.0 / s["temperature"]))     # the factor as 32 bits hold it
+    logp = torch.log_softmax(s["logits"].double() * scale, 2)
+    logq = None if s["draft_logits"] is None else torch.log_softmax(s["draft_logits"].double() * scale, 2)
+    draft, uniform = s["draft"].tolist(), s["uniform"].double().tolist()
+    lengths = [n] * b if s["lengths"] is None else s["lengths"].tolist()
+    accepted, tokens = [], []
+    for i in range(b):
+        c = 0
+        while c < lengths[i]:
+            x = draft[i][c]
+            ratio = logp[i, c, x] if logq is None else logp[i, c, x] - logq[i, c, x]
+            if uniform[i][c] >= math.exp(float(ratio)):
+                break
+            c += 1
+        left = torch.exp(logp[i, c])
+        if c < lengths[i]:
+            if logq is None:
+                left[draft[i][c]] = 0.0
+            elif bool((logp[i, c] > logq[i, c]).any()):
+                left = left - torch.exp(logq[i, c])
+        accepted.append(c)
+        tokens.append(int((s["noise"][i].double() / left.clamp(min=0.0)).argmin()))
+    a = torch.tensor(accepted, dtype=torch.int32, device=DEV)
+    probs = torch.exp(logp[:, :n].gather(2, s["draft"].long()[:, :, None])[:, :, 0])
+    probs[torch.arange(n, device=DEV) >= torch.tensor(lengths, device=DEV)[:, None]] = 0.0
+    return {"accepted": a, "last_pos": a - 1, "next_token": torch.tensor(tokens, dtype=torch.int32, device=DEV),
+            "probs": probs}
+
+
+def _conv64(s):
+    """Position by position of the taps: every input's share of every output that it reaches."""
+    c = s["case"]
+    b, d, L = c["batch"], c["dim"], c["L"]
+    w = s["w"].double()
+    x = torch.zeros(b, d, L + K - 1, dtype=torch.float64, device=DEV)
+    if s["state"] is not None:
+        x[:, :, :K - 1] = s["state"]
+    x[:, :, K - 1:] = s["x"]
+    pre = s["bias"].double()[None, :, None].expand(b, d, L).clone()
+    for i in range(K):
+        pre.addcmul_(x[:, :, i:i + L], w[None, :, i, None])
+    sig = torch.sigmoid(pre)
+    pre = sig.addcmul(pre * sig, 1 - sig)                   # the slope of pre * sigmoid(pre)
+    g = pre.mul_(s["dy"])
+    dx = torch.zeros_like(x)
+    dw = torch.empty(d, K, dtype=torch.float64, device=DEV)
+    for i in range(K):
+        dx[:, :, i:i + L].addcmul_(g, w[None, :, i, None])
+        dw[:, i] = (g * x[:, :, i:i + L]).sum((0, 2))
+    if s["dstate_out"] is not None:
+        dx[:, :, L:] += s["dstate_out"]
+    out = {"dx": dx[:, :, K - 1:].contiguous(), "dw": dw, "dbias": g.sum((0, 2))}
+    if s["state"] is not None:
+        out["dstate"] = dx[:, :, :K - 1].contiguous()
+    return out
