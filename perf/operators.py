@@ -163,7 +163,7 @@ def _clip_state(case, r):
             s["out"] += _tensors(out, sizes, align)
         total += sum(sizes)
     # the norm is about 1e-3 sqrt(total); training clips at 1, or lets the gradients pass
-    s["max_norm"] = 1e-3 * math.sqrt(total) * (0.25 if case["clipped"] else 4.0)
+    s["max_norm"] = 1e-3 * math.sqrt(total) * (0.3 if case["clipped"] else 4.0)
     return s
 
 
@@ -285,8 +285,8 @@ def _conv_plain(s):
 
 
 def _softmax_plain(logits, temperature):
-    v = logits.float() * (1.0 / temperature)
-    e = torch.exp(v - v.amax(-1, keepdim=True))
+    v = logits.float()
+    e = torch.exp((v - v.amax(-1, keepdim=True)) * (1.0 / temperature))
     return e / e.sum(-1, keepdim=True)
 
 
