@@ -50,6 +50,7 @@
 extern "C" {
 #endif
 
+/* Raised when an entry point changes; new ones beside the old leave it. */
 #define MB_ABI_VERSION 6
 
 typedef enum {
@@ -64,7 +65,8 @@ typedef enum {
     MB_ERR_DTYPE = -3,       /* in_dtype or out_dtype is not an mb_dtype */
     MB_ERR_ALIGN = -4,       /* a pointer is not aligned to its element size */
     MB_ERR_UNSUPPORTED = -5, /* dstate not in {1, 2, 4, 8, 16}, a convolution width outside
-                                1 .. 4, or a reserved field is set */
+                                1 .. 4, a reserved field is set, or a number (a temperature,
+                                a bound of the norm) outside its range */
     MB_ERR_HIP = -6,         /* the HIP runtime reported an error when launching */
     MB_ERR_ALIAS = -7        /* an output overlaps an input it may not overlap */
 } mb_status;
@@ -332,6 +334,141 @@ int mb_conv1d_step(int64_t batch, int64_t dim, int32_t width, int32_t in_dtype, 
 int mb_verify_rank(int64_t batch, int64_t ndraft, int64_t vocab, int32_t logit_dtype, int32_t beta,
                    const void *logits, const int32_t *draft, int32_t *ranks, int32_t *accepted,
                    int32_t *last_pos, void *stream);
+
+/* Integer types of the tokens of an embedding. */
+typedef enum {
+    MB_TOKEN_U8 = 0,         /* bytes */
+    MB_TOKEN_I32 = 1,
+    MB_TOKEN_I64 = 2
+} mb_token_type;
+
+/*
+ * The embedding lookup with scaling: the byte model's inputs (256 byte values in
+ * every MambaByte model), or a subword drafter's.
+ *
+ *   out[i][:] = scale * weight[tokens[i]][:]
+ *
+ * A negative token is padding: its row is zeros.  A token >= vocab is a mistake
+ * that the host cannot see: its row is NaN.
+ *
+ *   tokens  token_type (ntokens)      any leading shape, flattened
+ *   weight  weight_dtype (vocab, dim) vocab below 2^31
+ *   out     out_dtype (ntokens, dim)  must not overlap an input
+ * One fp32 product per element, rounded once to out_dtype.
+ */
+int mb_embedding_fwd(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_type, int32_t weight_dtype,
+                     int32_t out_dtype, float scale, const void *tokens, const void *weight, void *out, void *stream);
+
+/*
+ * The gradient of mb_embedding_fwd's table:
+ *
+ *   dweight[v][:] = scale * sum of dy[i][:] over the i with tokens[i] == v
+ *
+ * Rows that no token names are zeros; tokens outside [0, vocab) add nothing.
+ * Sums are fp32 in an order that the tokens alone fix (the same bits on every
+ * call), rounded once to out_dtype.  dweight is overwritten, not accumulated.
+ *
+ *   tokens  token_type (ntokens)       ntokens below 2^31
+ *   dy      dy_dtype (ntokens, dim)
+ *   dweight out_dtype (vocab, dim)     must not overlap an input
+ * The call allocates a stream-ordered workspace (hipMallocAsync), freed on the same stream.
+ */
+int mb_embedding_bwd(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_type, int32_t dy_dtype, int32_t out_dtype,
+                     float scale, const void *tokens, const void *dy, void *dweight, void *stream);
+
+/*
+ * The backward of mb_conv1d_fwd: the gradients of sum(dy * y) + sum(dstate_out *
+ * state_out) with respect to every input of the convolution.
+ *
+ *   desc, x, w, bias, state_in     as for mb_conv1d_fwd
+ *   dy          out-dtype (B, D, L)   gradient with respect to y (desc->out_dtype)
+ *   dstate_out  float (B, D, k-1)     gradient with respect to state_out; NULL means 0
+ *   dx          out-dtype (B, D, L)
+ *   dw          float (D, k)          summed over batch and time; required
+ *   dbias       float (D)             required when bias is given, else ignored
+ *   dstate_in   float (B, D, k-1)     NULL means not written
+ * Outputs are overwritten (not accumulated) and must not overlap any other
+ * argument; with no row or no timestep dw and dbias are zeros.  D, B * D and L
+ * below 2^31.  Arithmetic is fp32; results are deterministic.  The call allocates a
+ * stream-ordered workspace (hipMallocAsync), freed on the same stream.
+ */
+int mb_conv1d_bwd(const mb_conv_desc *desc, const void *x, const float *w, const float *bias, const float *state_in,
+                  const void *dy, const float *dstate_out, void *dx, float *dw, float *dbias, float *dstate_in,
+                  void *stream);
+
+/*
+ * The global norm of a list of tensors (the gradients of a model):
+ *
+ *   norm[0] = sqrt(sum of g^2 over every element of every tensor)
+ *
+ *   count          tensors; an empty one (size 0) may have a NULL address
+ *   grads, sizes, dtypes   HOST arrays (count): device addresses, element counts, mb_dtype.
+ *                  They are read before the call returns.
+ *   norm           float, DEVICE memory, must not overlap a tensor
+ * Squares and sums are fp64, in an order that the list alone fixes; the result is
+ * rounded to fp32.  The call allocates a stream-ordered workspace (hipMallocAsync),
+ * freed on the same stream.
+ */
+int mb_grad_norm(int64_t count, const void *const *grads, const int64_t *sizes, const int32_t *dtypes, float *norm,
+                 void *stream);
+
+/*
+ * mb_grad_norm, then the tensors clipped by it:
+ *
+ *   out = g                            where norm + eps <= max_norm
+ *       = g * (max_norm / (norm + eps))  otherwise
+ *
+ * A NaN norm makes every output NaN; an infinite one makes zeros (NaN where g is infinite).
+ *
+ *   out            HOST array (count) of device addresses of tensors of the same sizes and
+ *                  types; NULL: in place, and nothing is written where nothing is clipped.
+ *                  Written tensors overlap neither each other, norm nor (unless in place) grads.
+ *   max_norm, eps  finite, >= 0 (MB_ERR_UNSUPPORTED otherwise)
+ *   norm           the norm before clipping
+ */
+int mb_clip_grad_norm(int64_t count, const void *const *grads, void *const *out, const int64_t *sizes,
+                      const int32_t *dtypes, float max_norm, float eps, float *norm, void *stream);
+
+/*
+ * Verification of drafted tokens against the target's probabilities, from given
+ * random numbers: the check of mb_verify_rank for sampled instead of greedy
+ * generation, with the token that follows.  With ndraft = 0 it samples one token
+ * per sequence.
+ *
+ *   p_i = softmax(logits[b][i] / temperature), q_i = softmax(draft_logits[b][i] / temperature),
+ *   or, without draft_logits, certainty of the drafted token x_i
+ *
+ *   token i passes      uniform[b][i] * q_i(x_i) < p_i(x_i)
+ *   accepted[b]   = c   the number of leading tokens that pass, of the len = lengths[b] drafted
+ *   next_token[b]       the y with the largest r(y) / noise[b][y], the lowest such y, where
+ *                       r = max(p_c - q_c, 0) for c < len (p_c if that is zero everywhere) and
+ *                       r = p_len for c = len
+ *
+ * With uniform numbers in [0, 1) and exponential noise of mean 1 the tokens are
+ * distributed as samples of the target.  A drafted token outside [0, vocab) does not
+ * pass.  A row of logits that is no distribution (a NaN or +infinity in it, or nothing
+ * above -infinity) passes nothing: in the target's row the next token is -1, in the
+ * drafter's r = p_c.  -infinity masks a token.
+ *
+ *   logits        act (batch, ndraft + 1, vocab)
+ *   draft_logits  act (batch, ndraft, vocab)   NULL: drafts without probabilities
+ *   draft         int32 (batch, ndraft)
+ *   lengths       int32 (batch)                tokens drafted, clamped to [0, ndraft]; NULL means ndraft
+ *   uniform       float (batch, ndraft)
+ *   noise         float (batch, vocab)
+ *   accepted, next_token  int32 (batch)        required
+ *   last_pos      int32 (batch)                accepted - 1, as mb_verify_rank's; NULL means not written
+ *   probs         float (batch, ndraft)        p_i(x_i) for i < len (0 for a token outside [0, vocab) or
+ *                                              a row that is no distribution), 0 for i >= len; NULL means
+ *                                              not written
+ *   temperature   > 0, it and its inverse finite (MB_ERR_UNSUPPORTED otherwise)
+ * Outputs must not overlap each other or the inputs.  vocab >= 1; batch, ndraft and
+ * vocab below 2^31 - 1.  Probabilities are fp32.
+ */
+int mb_verify_sample(int64_t batch, int64_t ndraft, int64_t vocab, int32_t logit_dtype, float temperature,
+                     const void *logits, const void *draft_logits, const int32_t *draft, const int32_t *lengths,
+                     const float *uniform, const float *noise, int32_t *accepted, int32_t *last_pos,
+                     int32_t *next_token, float *probs, void *stream);
 
 /* Static, NUL-terminated description of a status code (never NULL). */
 const char *mb_status_string(int status);

@@ -9,15 +9,23 @@ of the scan, ``conv1d`` and ``conv1d_step``, and the top-beta check that ends a
 speculative verification, ``verify_rank``, are loaded on first use.
 ``selective_scan`` is the scan as a differentiable torch operation (forward with
 checkpoints, backward from them).
+
+Around the layers: ``embedding_fwd`` and its gradient ``embedding_bwd``, the convolution's
+gradient ``conv1d_bwd`` (``embedding`` and ``causal_conv1d`` are the differentiable
+operations), ``grad_norm`` and ``clip_grad_norm`` over all of a model's gradients, and
+``verify_sample``, the check of drafted tokens for sampled generation.
 """
 __all__ = ["scan_fwd", "scan_fwd_noalloc", "scan_step", "scan_bwd", "conv1d", "conv1d_step", "verify_rank", "load_library",
-           "MBScanError", "selective_scan"]
+           "MBScanError", "selective_scan", "embedding_fwd", "embedding_bwd", "embedding", "conv1d_bwd", "causal_conv1d",
+           "grad_norm", "clip_grad_norm", "verify_sample"]
+
+_AUTOGRAD = ("selective_scan", "causal_conv1d", "embedding")
 
 
 def __getattr__(name):
-    if name == "selective_scan":
-        from .autograd import selective_scan
-        return selective_scan
+    if name in _AUTOGRAD:
+        from . import autograd
+        return getattr(autograd, name)
     if name in __all__:
         from . import _binding
         return getattr(_binding, name)

@@ -70,6 +70,19 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.mb_scan_fwd_ckpt.argtypes = [ctypes.POINTER(ScanDesc)] + [_VP] * 13
     lib.mb_verify_rank.restype = ctypes.c_int
     lib.mb_verify_rank.argtypes = [ctypes.c_int64] * 3 + [ctypes.c_int32] * 2 + [_VP] * 6
+    i64, i32, f32 = ctypes.c_int64, ctypes.c_int32, ctypes.c_float
+    lib.mb_embedding_fwd.restype = ctypes.c_int
+    lib.mb_embedding_fwd.argtypes = [i64] * 3 + [i32] * 3 + [f32] + [_VP] * 4
+    lib.mb_embedding_bwd.restype = ctypes.c_int
+    lib.mb_embedding_bwd.argtypes = [i64] * 3 + [i32] * 3 + [f32] + [_VP] * 4
+    lib.mb_conv1d_bwd.restype = ctypes.c_int
+    lib.mb_conv1d_bwd.argtypes = [ctypes.POINTER(ConvDesc)] + [_VP] * 11
+    lib.mb_grad_norm.restype = ctypes.c_int
+    lib.mb_grad_norm.argtypes = [i64] + [_VP] * 5
+    lib.mb_clip_grad_norm.restype = ctypes.c_int
+    lib.mb_clip_grad_norm.argtypes = [i64] + [_VP] * 4 + [f32] * 2 + [_VP] * 2
+    lib.mb_verify_sample.restype = ctypes.c_int
+    lib.mb_verify_sample.argtypes = [i64] * 3 + [i32, f32] + [_VP] * 11
     lib.mb_status_string.restype = ctypes.c_char_p
     lib.mb_status_string.argtypes = [ctypes.c_int]
     lib.mb_abi_version.restype = ctypes.c_int
@@ -487,3 +500,177 @@ def scan_bwd(u, delta, A, B, C, dy, D=None, dt_bias=None, z=None, h0=None, dh_la
                              _ptr(g["dD"]), _ptr(g["ddt_bias"]), _ptr(g["dh0"]), stream)
     _check(st, "mb_scan_bwd")
     return g
+
+
+_TOKEN_TYPES = {torch.uint8: 0, torch.int32: 1, torch.int64: 2}
+
+
+def _tokens(tokens, dev=None):
+    """The tokens' type code; they may have any shape."""
+    if not isinstance(tokens, torch.Tensor) or tokens.dtype not in _TOKEN_TYPES:
+        raise MBScanError("tokens must be a uint8, int32 or int64 tensor")
+    _need(tokens, "tokens", tokens.shape, None, dev)
+    return _TOKEN_TYPES[tokens.dtype]
+
+
+def embedding_fwd(tokens, weight, *, scale=1.0, out_dtype=None, out=None):
+    """scale * weight[tokens]: tokens uint8, int32 or int64 of any shape, weight (vocab, dim) fp32 or bf16.
+    Returns tokens.shape + (dim,) in ``out_dtype`` (weight's by default).  A negative token (padding) gives
+    zeros, a token >= vocab NaN."""
+    lib = load_library()
+    if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
+        raise MBScanError("weight must be a (vocab, dim) tensor")
+    V, d = weight.shape
+    dev = weight.device
+    _need(weight, "weight", (V, d))
+    code = _tokens(tokens, dev)
+    shape = tuple(tokens.shape) + (d,)
+    if out is None:
+        out = torch.empty(shape, dtype=out_dtype or weight.dtype, device=dev)
+    else:
+        _need(out, "out", shape, None, dev)
+    with _on_device(dev):
+        st = lib.mb_embedding_fwd(tokens.numel(), V, d, code, _dt(weight.dtype), _dt(out.dtype), float(scale),
+                                  _ptr(tokens), _ptr(weight), _ptr(out), _stream(dev))
+    _check(st, "mb_embedding_fwd")
+    return out
+
+
+def embedding_bwd(tokens, dy, vocab, *, scale=1.0, out_dtype=torch.float32, out=None):
+    """The gradient of embedding_fwd's table: (vocab, dim) in ``out_dtype``, row v the sum of scale * dy over
+    the tokens equal to v (the same bits on every call).  dy: tokens.shape + (dim,), fp32 or bf16."""
+    lib = load_library()
+    if not isinstance(dy, torch.Tensor) or dy.dim() < 1:
+        raise MBScanError("dy must be a tensor of the tokens' shape and a last dimension dim")
+    dev, d = dy.device, dy.shape[-1]
+    code = _tokens(tokens, dev)
+    _need(dy, "dy", tuple(tokens.shape) + (d,))
+    vocab = int(vocab)
+    if vocab < 0:
+        raise MBScanError("vocab must not be negative")
+    if out is None:
+        out = torch.empty((vocab, d), dtype=out_dtype, device=dev)
+    else:
+        _need(out, "out", (vocab, d), None, dev)
+    with _on_device(dev):
+        st = lib.mb_embedding_bwd(tokens.numel(), vocab, d, code, _dt(dy.dtype), _dt(out.dtype), float(scale),
+                                  _ptr(tokens), _ptr(dy), _ptr(out), _stream(dev))
+    _check(st, "mb_embedding_bwd")
+    return out
+
+
+def conv1d_bwd(x, w, dy, bias=None, state=None, dstate_out=None, *, apply_silu=True):
+    """Gradients of sum(dy * y) + sum(dstate_out * state_out) for the convolution of conv1d.
+
+    x, w, bias, state as for ``conv1d``; dy has y's dtype, shape (batch, dim, L); dstate_out:
+    (batch, dim, k-1) fp32 or None.  Returns a dict: dx (dy's dtype), dw (dim, k), dbias (dim,) or None,
+    and dstate (batch, dim, k-1), fp32 but the first."""
+    lib = load_library()
+    if not isinstance(x, torch.Tensor) or x.dim() != 3:
+        raise MBScanError("x must be a (batch, dim, L) tensor")
+    nb, dim, L = x.shape
+    if not isinstance(w, torch.Tensor) or w.dim() != 2:
+        raise MBScanError("w must be a (dim, k) tensor")
+    K, dev = w.shape[1], x.device
+    H = max(K - 1, 0)
+    for t, name, shape, dt in ((x, "x", (nb, dim, L), None), (w, "w", (dim, K), torch.float32),
+                               (dy, "dy", (nb, dim, L), None)):
+        _need(t, name, shape, dt, dev)
+    for t, name, shape in ((bias, "bias", (dim,)), (state, "state", (nb, dim, H)),
+                           (dstate_out, "dstate_out", (nb, dim, H))):
+        if t is not None:
+            _need(t, name, shape, torch.float32, dev)
+    f32 = dict(dtype=torch.float32, device=dev)
+    g = {"dx": torch.empty((nb, dim, L), dtype=dy.dtype, device=dev), "dw": torch.empty((dim, K), **f32),
+         "dbias": torch.empty(dim, **f32) if bias is not None else None,
+         "dstate": torch.empty((nb, dim, H), **f32)}
+    desc = ConvDesc(nb, dim, L, K, _dt(x.dtype), _dt(dy.dtype), 1 if apply_silu else 0, 0, 0)
+    with _on_device(dev):
+        st = lib.mb_conv1d_bwd(ctypes.byref(desc), _ptr(x), _ptr(w), _ptr(bias), _ptr(state) if H else None, _ptr(dy),
+                               _ptr(dstate_out) if H else None, _ptr(g["dx"]), _ptr(g["dw"]), _ptr(g["dbias"]),
+                               _ptr(g["dstate"]) if H else None, _stream(dev))
+    _check(st, "mb_conv1d_bwd")
+    return g
+
+
+def _grad_list(grads):
+    """The tensors of a list, one GPU's and dense: their device, and host arrays of addresses, sizes and types."""
+    if isinstance(grads, torch.Tensor):
+        grads = [grads]
+    grads = list(grads)
+    if not grads:
+        raise MBScanError("the list of tensors is empty")
+    dev = grads[0].device if isinstance(grads[0], torch.Tensor) else None
+    for i, t in enumerate(grads):
+        if not isinstance(t, torch.Tensor):
+            raise MBScanError(f"tensor {i} must be a torch.Tensor")
+        _need(t, f"tensor {i}", t.shape, None, dev)
+    n = len(grads)
+    return (grads, dev, (_VP * n)(*(t.data_ptr() for t in grads)), (ctypes.c_int64 * n)(*(t.numel() for t in grads)),
+            (ctypes.c_int32 * n)(*(_dt(t.dtype) for t in grads)))
+
+
+def grad_norm(grads):
+    """The 2-norm of all elements of a list of fp32 and bf16 tensors: a 0-dimensional fp32 tensor on their GPU."""
+    lib = load_library()
+    grads, dev, ptrs, sizes, types = _grad_list(grads)
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    with _on_device(dev):
+        st = lib.mb_grad_norm(len(grads), ptrs, sizes, types, _ptr(norm), _stream(dev))
+    _check(st, "mb_grad_norm")
+    return norm
+
+
+def clip_grad_norm(grads, max_norm, *, eps=1e-6, out=None):
+    """Scales a list of fp32 and bf16 tensors by max_norm / (norm + eps) where that is below 1, in place or
+    into ``out`` (tensors of the same shapes and types).  Returns the norm before clipping, a 0-dimensional
+    fp32 tensor on the GPU."""
+    lib = load_library()
+    grads, dev, ptrs, sizes, types = _grad_list(grads)
+    optrs = None
+    if out is not None:
+        out = [out] if isinstance(out, torch.Tensor) else list(out)
+        if len(out) != len(grads):
+            raise MBScanError(f"out has {len(out)} tensors, expected {len(grads)}")
+        for i, (o, t) in enumerate(zip(out, grads)):
+            _need(o, f"out {i}", t.shape, t.dtype, dev)
+        optrs = (_VP * len(out))(*(o.data_ptr() for o in out))
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    with _on_device(dev):
+        st = lib.mb_clip_grad_norm(len(grads), ptrs, optrs, sizes, types, float(max_norm), float(eps), _ptr(norm),
+                                   _stream(dev))
+    _check(st, "mb_clip_grad_norm")
+    return norm
+
+
+def verify_sample(logits, draft, uniform, noise, draft_logits=None, *, lengths=None, temperature=1.0,
+                  return_probs=False):
+    """Drafted tokens against the target's probabilities, from given random numbers.
+
+    logits: (batch, ndraft + 1, vocab) fp32 or bf16, row i scoring drafted token i and the row after the last
+    one the token that follows; draft: int32 (batch, ndraft); uniform: fp32 (batch, ndraft) in [0, 1);
+    noise: fp32 (batch, vocab), exponential of mean 1; draft_logits: (batch, ndraft, vocab) of logits' type, or
+    None for drafts without probabilities; lengths: int32 (batch,), the tokens drafted for each sequence.
+    Returns (accepted, last_pos, next_token), each int32 (batch,), and with ``return_probs`` the target's
+    probabilities of the drafted tokens, fp32 (batch, ndraft).  With ndraft = 0 it samples the next token."""
+    lib = load_library()
+    if not isinstance(logits, torch.Tensor) or logits.dim() != 3 or logits.shape[1] < 1:
+        raise MBScanError("logits must be a (batch, ndraft + 1, vocab) tensor")
+    nb, n, V = logits.shape[0], logits.shape[1] - 1, logits.shape[2]
+    dev = logits.device
+    _need(logits, "logits", (nb, n + 1, V))
+    _need(draft, "draft", (nb, n), torch.int32, dev)
+    _need(uniform, "uniform", (nb, n), torch.float32, dev)
+    _need(noise, "noise", (nb, V), torch.float32, dev)
+    if draft_logits is not None:
+        _need(draft_logits, "draft_logits", (nb, n, V), logits.dtype, dev)
+    if lengths is not None:
+        _need(lengths, "lengths", (nb,), torch.int32, dev)
+    accepted, last_pos, next_token = (torch.empty(nb, dtype=torch.int32, device=dev) for _ in range(3))
+    probs = torch.empty((nb, n), dtype=torch.float32, device=dev) if return_probs else None
+    with _on_device(dev):
+        st = lib.mb_verify_sample(nb, n, V, _dt(logits.dtype), float(temperature), _ptr(logits), _ptr(draft_logits),
+                                  _ptr(draft), _ptr(lengths), _ptr(uniform), _ptr(noise), _ptr(accepted),
+                                  _ptr(last_pos), _ptr(next_token), _ptr(probs), _stream(dev))
+    _check(st, "mb_verify_sample")
+    return (accepted, last_pos, next_token, probs) if return_probs else (accepted, last_pos, next_token)

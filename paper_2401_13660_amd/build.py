@@ -11,12 +11,13 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import tempfile
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libmbscan.so")
-SOURCES = ["mbscan.hip"]
+SOURCES = ["mbscan.hip", "model_ops.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -32,20 +33,31 @@ FLAGS = [
 
 def build(verbose: bool = False) -> str:
     tmp = LIB + ".tmp"
-    cmd = [HIPCC, *FLAGS, "-I", os.path.join(ROOT, "include"), "-I", CSRC,
-           *[os.path.join(CSRC, s) for s in SOURCES], "-o", tmp]
-    if verbose:
-        print(" ".join(cmd))
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        sys.stderr.write(res.stdout + res.stderr)
-        raise RuntimeError("hipcc failed to build libmbscan.so")
+    with tempfile.TemporaryDirectory() as objs:
+        # each source by a compiler of its own, all at once; then one link
+        objects = [os.path.join(objs, os.path.splitext(s)[0] + ".o") for s in SOURCES]
+        compile_flags = [f for f in FLAGS if f != "-shared"]
+        _run([[HIPCC, *compile_flags, "-c", "-I", os.path.join(ROOT, "include"), "-I", CSRC, os.path.join(CSRC, s),
+               "-o", o] for s, o in zip(SOURCES, objects)], "libmbscan.so", verbose)
+        _run([[HIPCC, "--offload-arch=gfx950", "-shared", *objects, "-o", tmp]], "libmbscan.so", verbose)
     os.replace(tmp, LIB)
     build_fastcall(verbose)
     build_issue_rates(verbose)
     build_lds_banks(verbose)
     build_bf16_pack_check(verbose)
     return LIB
+
+
+def _run(cmds, what, verbose):
+    """The commands, side by side; raises if one fails."""
+    if verbose:
+        for cmd in cmds:
+            print(" ".join(cmd))
+    started = [subprocess.Popen(c, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True) for c in cmds]
+    said = [p.communicate()[0] for p in started]
+    if any(p.returncode != 0 for p in started):
+        sys.stderr.write("".join(said))
+        raise RuntimeError(f"hipcc failed to build {what}")
 
 
 def build_fastcall(verbose: bool = False) -> str:

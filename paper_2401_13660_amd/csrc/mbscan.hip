@@ -8,6 +8,7 @@
 
 #include <mutex>
 
+#include "abi_checks.hpp"
 #include "conv1d.hpp"
 #include "fwd_plan.hpp"
 #include "mbscan.h"
@@ -25,37 +26,9 @@ namespace {
 using mbs::ScanParams;
 using mbs::StepParams;
 
-// Every element count the entry points form stays below 2^56, so that byte
-// counts (at most 4 bytes per element, times the position count's factor
-// already inside the count) and the address ranges of the alias checks stay far
-// from overflow.  No device memory comes near it.
-constexpr int64_t kMaxElems = int64_t(1) << 56;
-
-bool valid_dtype(int32_t t) { return t == MB_F32 || t == MB_BF16; }
-size_t dtype_size(int32_t t) { return t == MB_BF16 ? 2 : 4; }
-
-bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-
-// Does [a, a+na) overlap [b, b+nb)?  Null or empty ranges never overlap.
-bool overlaps(const void *a, size_t na, const void *b, size_t nb) {
-    if (!a || !b || na == 0 || nb == 0) return false;
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return x < y + nb && y < x + na;
-}
-
-// a * b without overflow past kMaxElems (both non-negative).
-bool mul_ok(int64_t a, int64_t b, int64_t *out) {
-    if (a != 0 && b > kMaxElems / a) return false;
-    *out = a * b;
-    return true;
-}
+using namespace mbs::abi;
 
 bool supported_dstate(int64_t n) { return n == 1 || n == 2 || n == 4 || n == 8 || n == 16; }
-
-hipError_t launch(const void *fn, dim3 grid, dim3 block, void *params, void *stream) {
-    void *args[] = {params};
-    return hipLaunchKernel(fn, grid, block, args, 0, static_cast<hipStream_t>(stream));
-}
 
 template <int IN, int OUT, int N>
 hipError_t fwd_rowwise(ScanParams &p, void *stream) {
@@ -324,7 +297,7 @@ const char *mb_status_string(int status) {
         case MB_ERR_SHAPE: return "a size is negative or too large";
         case MB_ERR_DTYPE: return "unknown element type";
         case MB_ERR_ALIGN: return "a pointer is not aligned to its element size";
-        case MB_ERR_UNSUPPORTED: return "unsupported dstate or convolution width, or reserved field set";
+        case MB_ERR_UNSUPPORTED: return "unsupported dstate, convolution width or number out of range, or reserved field set";
         case MB_ERR_HIP: return "the HIP runtime failed to launch a kernel";
         case MB_ERR_ALIAS: return "an output overlaps an input";
         default: return "unknown status";

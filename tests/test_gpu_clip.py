@@ -1,0 +1,147 @@
+"""GPU parity of the global norm and the clipping against 64 bits.
+
+Tolerances: squares and sums are fp64 and the norm is rounded once (2^-24, doubled); a clipped fp32 element carries the
+norm's rounding, the sum's with eps, the division's and its own product's (4 times 2^-24, doubled), a bf16 one its own
+rounding (2^-9, doubled)."""
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import announce, has_gpu
+from oracle import model_ops as M
+from test_gpu_embedding import DT, np64, randn, shifted
+
+pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not has_gpu(), reason="needs a GPU")]
+U = 2.0 ** -24
+
+
+def tensors(sizes, types, seed, shift=None):
+    out = []
+    for i, (n, t) in enumerate(zip(sizes, types)):
+        g = randn((n,), seed + i, t)
+        out.append(shifted(g, shift(i)) if shift else g)
+    return out
+
+
+def check(grads, factor, eps=1e-6, in_place=True):
+    """Clips at `factor` times the norm."""
+    import paper_2401_13660_amd as mb
+    before = [g.clone() for g in grads]
+    n64 = M.norm([np64(g) for g in before])
+    max_norm = float(np.float32(factor * n64))
+    ref_norm, ref = M.clip([np64(g) for g in before], max_norm, eps)
+    out = None if in_place else [torch.full_like(g, 7.0) for g in grads]
+    norm = mb.clip_grad_norm(grads, max_norm, eps=eps, out=out)
+    only = mb.grad_norm(before)
+    torch.cuda.synchronize()
+    assert norm.shape == () and norm.dtype == torch.float32
+    for v in (norm, only):
+        assert abs(float(v) - ref_norm) <= 2 * U * ref_norm
+    for g, b, o, r in zip(grads, before, out or grads, ref):
+        if not in_place:
+            assert torch.equal(g, b), "an input changed"
+        if factor > 1.001:
+            assert torch.equal(o, b), "gradients within the bound changed"
+        tol = 8 * U if g.dtype == torch.float32 else 2.0 ** -8
+        assert (np.abs(np64(o) - r) <= tol * np.abs(r)).all()
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("factor", [0.3, 2.0])
+@pytest.mark.parametrize("sizes", [[1], [7, 1, 0, 3], [100000], [5, 4096, 8192, 8193, 123457], [0, 0, 9]])
+def test_lists(sizes, factor, in_place):
+    announce(f"clip_grad_norm {sizes} factor {factor} in place {in_place}")
+    for types in (["f32"] * len(sizes), ["bf16"] * len(sizes), (["f32", "bf16"] * len(sizes))[:len(sizes)]):
+        check(tensors(sizes, types, 20), factor, in_place=in_place)
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+def test_many_small_tensors(in_place):
+    """More tensors than any table of fixed size would hold, of every small size and alignment."""
+    announce("clip_grad_norm of 1,500 tensors")
+    sizes = [(i * 37) % 300 for i in range(1500)]
+    check(tensors(sizes, ["f32", "bf16", "bf16"] * 500, 30, lambda i: i % 9), 0.3, in_place=in_place)
+
+
+@pytest.mark.parametrize("shift", range(8))
+def test_alignment(shift):
+    announce(f"clip_grad_norm at addresses {shift} elements on")
+    check(tensors([70001, 33, 8200], ["bf16", "f32", "bf16"], 40, lambda i: shift), 0.3)
+    g = tensors([70001, 33, 8200], ["bf16", "f32", "bf16"], 40, lambda i: shift)
+    check(g, 0.3, in_place=False)
+
+
+def test_views_of_one_buffer():
+    """Gradients side by side in one buffer: nothing between or beside them changes."""
+    import paper_2401_13660_amd as mb
+    announce("clip_grad_norm of views with gaps")
+    for dtype in ("f32", "bf16"):
+        buf = randn((50000,), 50, dtype)
+        was = buf.clone()
+        cuts = [(1, 2), (3, 20), (21, 4000), (4001, 4001), (4003, 30001), (30001, 49999)]
+        mb.clip_grad_norm([buf[a:b] for a, b in cuts], 1.0)
+        torch.cuda.synchronize()
+        inside = torch.zeros(50000, dtype=torch.bool, device="cuda:0")
+        for a, b in cuts:
+            inside[a:b] = True
+        assert torch.equal(buf[~inside], was[~inside])
+        assert (buf[inside] != was[inside]).float().mean() > 0.99
+
+
+def test_shapes_and_types_of_parameters():
+    """Gradients as a module has them: any shape, one tensor alone, a generator."""
+    import paper_2401_13660_amd as mb
+    announce("clip_grad_norm of a module's gradients")
+    g = [randn((3, 4, 5), 60, "f32"), randn((), 61, "f32"), randn((17, 2), 62, "bf16")]
+    ref = M.norm([np64(t) for t in g])
+    assert abs(float(mb.grad_norm(t for t in g)) - ref) <= 2 * U * ref
+    assert abs(float(mb.grad_norm(g[0])) - M.norm([np64(g[0])])) <= 2 * U * ref
+    out = [torch.empty_like(t) for t in g]
+    mb.clip_grad_norm(tuple(g), 0.1, out=tuple(out))
+    torch.cuda.synchronize()
+    assert [o.shape for o in out] == [t.shape for t in g]
+
+
+def test_extremes():
+    import paper_2401_13660_amd as mb
+    announce("clip_grad_norm: sizes of elements, infinities, NaN, zeros")
+    for v in (1e-30, 1e30, 2.0 ** -140):                     # squares outside fp32's range
+        g = torch.full((1000,), v, device="cuda:0")
+        ref = M.norm([np64(g)])
+        assert abs(float(mb.grad_norm([g])) - ref) <= 2 * U * ref + 2.0 ** -149
+    z = torch.zeros(10, device="cuda:0")
+    assert float(mb.clip_grad_norm([z], 1.0)) == 0 and (z == 0).all()
+    assert float(mb.clip_grad_norm([z], 0.0, eps=0.0)) == 0 and (z == 0).all()
+    g = torch.ones(10, device="cuda:0")
+    mb.clip_grad_norm([g], 0.0)
+    assert (g == 0).all()
+    g = torch.tensor([1.0, float("inf"), -2.0], device="cuda:0")
+    assert float(mb.clip_grad_norm([g], 1.0)) == float("inf")
+    assert g[0] == 0 and torch.isnan(g[1]) and g[2] == 0
+    g, h = torch.tensor([1.0, float("nan")], device="cuda:0"), torch.ones(5, device="cuda:0").bfloat16()
+    assert torch.isnan(mb.clip_grad_norm([g, h], 1.0)) and torch.isnan(g).all() and torch.isnan(h).all()
+
+
+def test_exact_threshold():
+    """norm + eps equal to the bound clips nothing; the same norm on every call."""
+    import paper_2401_13660_amd as mb
+    announce("clip_grad_norm at the bound")
+    g = torch.tensor([3.0, 4.0], device="cuda:0")
+    assert float(mb.clip_grad_norm([g], 5.0, eps=0.0)) == 5.0 and g.tolist() == [3.0, 4.0]
+    big = tensors([300007, 50, 123456], ["f32", "bf16", "bf16"], 70)
+    assert len({float(mb.grad_norm(big)) for _ in range(4)}) == 1
+
+
+def test_refusals():
+    import paper_2401_13660_amd as mb
+    announce("clip_grad_norm: refusals")
+    g, h = torch.ones(4, 6, device="cuda:0"), torch.ones(8, device="cuda:0")
+    for call in (lambda: mb.clip_grad_norm([g, g], 1.0), lambda: mb.clip_grad_norm([h[:5], h[4:]], 1.0),
+                 lambda: mb.clip_grad_norm([g.t()], 1.0), lambda: mb.clip_grad_norm([g.half()], 1.0),
+                 lambda: mb.clip_grad_norm([g], 1.0, out=[h]), lambda: mb.clip_grad_norm([g], 1.0, out=[]),
+                 lambda: mb.clip_grad_norm([g], 1.0, out=[g.bfloat16()]), lambda: mb.clip_grad_norm([h], 1.0, out=[h]),
+                 lambda: mb.clip_grad_norm([g], -1.0), lambda: mb.clip_grad_norm([g], float("nan")),
+                 lambda: mb.clip_grad_norm([g, h.cpu()], 1.0), lambda: mb.grad_norm([None])):
+        with pytest.raises(mb.MBScanError):
+            call()
+    assert (g == 1).all() and (h == 1).all()
