@@ -9,16 +9,24 @@
 //   dw[j]  = sum over batch and t of g[t] ext[t + j],   dbias = sum of g[t]
 //
 // pre is computed again from x: storing it would cost a write and a read of the tensor.
+//
+// A wave takes a stretch of one row and walks it from its end to its start in tiles of 64 spans, one
+// span per lane.  A lane's H inputs before its span and the H values of g after it come from the
+// lanes beside it; the g after a tile's last lane are those of the tile just done (or, at the
+// stretch's end, computed there again), so x and dy are read once and dx is written once.  The next
+// tile's loads are on their way while a tile is computed.
 #pragma once
 
 #include <hip/hip_runtime.h>
 
 #include "device_math.hpp"
+#include "lanes.hpp"
 
 namespace mbs {
 namespace convbwd {
 
 constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
 
 struct Params {
     int64_t batch, dim, seqlen;
@@ -30,9 +38,14 @@ struct Params {
     void *dx;                     // (batch, dim, L) out
     float *dw, *dbias;            // (dim, K), (dim) or null
     float *dstate_in;             // (batch, dim, K-1) or null
-    float *part;                  // (batch, dim, K + 1): each row's share of dw and dbias
+    float *part;                  // (nseg, batch, dim, K + 1): each stretch's share of dw and dbias
+    int64_t nseg;                 // stretches per row
+    int32_t seg_tiles;            // tiles per stretch
     int apply_silu;
 };
+
+// Elements per lane: 16 bytes of the narrower of x and dy.
+template <int IN, int OUT> constexpr int kSpan = IN == 0 && OUT == 0 ? 4 : 8;
 
 // The slope of silu at pre: s (1 + pre (1 - s)).
 __device__ __forceinline__ float silu_slope(float pre) {
@@ -40,61 +53,139 @@ __device__ __forceinline__ float silu_slope(float pre) {
     return s * __builtin_fmaf(pre, 1.0f - s, 1.0f);
 }
 
-// One workgroup per row.
 template <int IN, int OUT, int K>
 __global__ __launch_bounds__(kThreads) void conv1d_bwd(Params p) {
-    constexpr int H = K - 1;
+    constexpr int H = K - 1, HH = H > 0 ? H : 1, S = kSpan<IN, OUT>, T = 64 * S;
     const int64_t L = p.seqlen, rows = p.batch * p.dim;
-    __shared__ float red[kThreads];
-    for (int64_t row = blockIdx.x; row < rows; row += gridDim.x) {
-        const int64_t d = row % p.dim;
-        float w[K];
-        for (int j = 0; j < K; ++j) w[j] = p.w[d * K + j];
-        const float b = p.bias ? p.bias[d] : 0.0f;
-        auto ext = [&](int64_t m) {
-            if (m < H) return p.state_in ? p.state_in[row * H + m] : 0.0f;
-            return Act<IN>::ld(p.x, row * L + m - H);
-        };
-        auto grad = [&](int64_t t) {
-            if (t < 0 || t >= L) return 0.0f;
-            float pre = b;
-            for (int j = 0; j < K; ++j) pre = __builtin_fmaf(w[j], ext(t + j), pre);
-            const float dy = Act<OUT>::ld(p.dy, row * L + t);
-            return p.apply_silu ? dy * silu_slope(pre) : dy;
-        };
-        float acc[K + 1] = {};
-        for (int64_t m = threadIdx.x; m < L + H; m += kThreads) {
-            float dext = m >= L && p.dstate_out ? p.dstate_out[row * H + m - L] : 0.0f;
-            for (int j = 0; j < K; ++j) dext = __builtin_fmaf(w[j], grad(m - j), dext);
-            if (m >= H) st_out<OUT>(p.dx, row * L + m - H, dext);
-            else if (p.dstate_in) p.dstate_in[row * H + m] = dext;
-            const float g = grad(m);
-            if (m < L) {
-                for (int j = 0; j < K; ++j) acc[j] = __builtin_fmaf(g, ext(m + j), acc[j]);
-                acc[K] += g;
+    const int64_t item = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+    if (item >= rows * p.nseg) return;
+    const int lane = threadIdx.x & 63;
+    const int64_t seg = item / rows, row = item - seg * rows, d = row % p.dim, base = row * L;
+    const int first = (int)(seg * p.seg_tiles);
+    const int ntiles = (int)((L + T - 1) / T);
+    const int last = min(first + p.seg_tiles, ntiles) - 1;     // below `first` only for L = 0
+
+    float w[K];
+#pragma unroll
+    for (int j = 0; j < K; ++j) w[j] = p.w[d * K + j];
+    const float bias = p.bias ? p.bias[d] : 0.0f;
+    // the input at time t < 0 of the row's beginning, or of the tile before
+    auto before = [&](int64_t t) -> float {
+        if (t >= 0) return Act<IN>::ld(p.x, base + t);
+        return p.state_in ? p.state_in[row * H + t + H] : 0.0f;
+    };
+
+    // g after the stretch
+    float carry[HH] = {};
+    if (H > 0 && last >= first) {
+        const int64_t t = (int64_t)(last + 1) * T + lane;
+        float g = 0.0f;
+        if (lane < H && t < L) {
+            float pre = bias;
+#pragma unroll
+            for (int j = 0; j < K; ++j) pre = __builtin_fmaf(w[j], before(t - H + j), pre);
+            g = Act<OUT>::ld(p.dy, base + t);
+            if (p.apply_silu) g *= silu_slope(pre);
+        }
+#pragma unroll
+        for (int j = 0; j < H; ++j) carry[j] = lane_value(g, j);
+    }
+
+    Span<IN, S> xs;
+    Span<OUT, S> ys;
+    float halo = 0.0f;                                          // lane j < H: the input H - j before the tile
+    auto load = [&](int tile) {
+        const int64_t t = (int64_t)tile * T + lane * S;
+        if ((int64_t)(tile + 1) * T <= L) {
+            xs.load(p.x, base + t);
+            ys.load(p.dy, base + t);
+        } else {
+            const int n = (int)max((int64_t)0, min(L - t, (int64_t)S));
+            xs.load_first(p.x, base + t, n);
+            ys.load_first(p.dy, base + t, n);
+        }
+        if (H > 0 && lane < H) halo = before((int64_t)tile * T - H + lane);
+    };
+
+    float acc[K + 1] = {};
+    if (last >= first) load(last);
+    for (int tile = last; tile >= first; --tile) {
+        const int64_t t0 = (int64_t)tile * T + lane * S;
+        float xin[H + S], g[S + HH];
+#pragma unroll
+        for (int i = 0; i < S; ++i) xin[H + i] = xs.get(i);
+#pragma unroll
+        for (int i = 0; i < S; ++i) g[i] = ys.get(i);
+#pragma unroll
+        for (int j = 0; j < H; ++j) xin[j] = from_lane_before(xin[S + j], lane_value(halo, j));
+        if (tile > first) load(tile - 1);
+
+        if (p.apply_silu) {
+#pragma unroll
+            for (int i = 0; i < S; ++i) {
+                float pre = bias;
+#pragma unroll
+                for (int j = 0; j < K; ++j) pre = __builtin_fmaf(w[j], xin[i + j], pre);
+                g[i] *= silu_slope(pre);
             }
         }
-        for (int j = 0; j <= K; ++j) {
-            red[threadIdx.x] = acc[j];
-            __syncthreads();
-            for (int n = kThreads / 2; n > 0; n /= 2) {
-                if ((int)threadIdx.x < n) red[threadIdx.x] += red[threadIdx.x + n];
-                __syncthreads();
-            }
-            if (threadIdx.x == 0) p.part[row * (K + 1) + j] = red[0];
-            __syncthreads();
+        const bool whole = (int64_t)(tile + 1) * T <= L;
+        if (!whole) {
+#pragma unroll
+            for (int i = 0; i < S; ++i) g[i] = t0 + i < L ? g[i] : 0.0f;
         }
+#pragma unroll
+        for (int i = 0; i < S; ++i) {
+#pragma unroll
+            for (int j = 0; j < K; ++j) acc[j] = __builtin_fmaf(g[i], xin[i + j], acc[j]);
+            acc[K] += g[i];
+        }
+#pragma unroll
+        for (int j = 0; j < H; ++j) {
+            g[S + j] = from_lane_after(g[j], carry[j]);
+            carry[j] = lane_value(g[j], 0);
+        }
+        float dx[S];
+#pragma unroll
+        for (int i = 0; i < S; ++i) {
+            dx[i] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < K; ++j) dx[i] = __builtin_fmaf(w[j], g[i + H - j], dx[i]);
+        }
+        if (H > 0 && p.dstate_out && (int64_t)(tile + 1) * T > L - H) {
+#pragma unroll
+            for (int i = 0; i < S; ++i)
+                if (t0 + i >= L - H && t0 + i < L) dx[i] += p.dstate_out[row * H + t0 + i + H - L];
+        }
+        if (whole) store_span<OUT, S>(p.dx, base + t0, dx);
+        else store_first<OUT, S>(p.dx, base + t0, dx, (int)max((int64_t)0, min(L - t0, (int64_t)S)));
+    }
+
+    if (H > 0 && first == 0 && p.dstate_in && lane < H) {
+        // dext[m], m < H: carry holds g[0 .. H), zeros past L
+        float v = p.dstate_out && lane >= L ? p.dstate_out[row * H + lane - L] : 0.0f;
+#pragma unroll
+        for (int j = 0; j < H; ++j)
+#pragma unroll
+            for (int m = j; m < H; ++m) v = lane == m ? __builtin_fmaf(w[j], carry[m - j], v) : v;
+        p.dstate_in[row * H + lane] = v;
+    }
+#pragma unroll
+    for (int j = 0; j <= K; ++j) {
+        const float s = wave_sum(acc[j]);
+        if (lane == j) p.part[item * (K + 1) + j] = s;
     }
 }
 
-// dw and dbias from the rows' shares, in the order of the batch.
+// dw and dbias from the stretches' shares, in the order of the stretches and of the batch.
 template <int K>
 __global__ __launch_bounds__(kThreads) void conv1d_bwd_finish(Params p) {
-    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (i >= p.dim * (K + 1)) return;
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x, n = p.dim * (K + 1);
+    if (i >= n) return;
     const int64_t d = i / (K + 1), j = i - d * (K + 1);
     float sum = 0.0f;
-    for (int64_t b = 0; b < p.batch; ++b) sum += p.part[(b * p.dim + d) * (K + 1) + j];
+#pragma unroll 8
+    for (int64_t b = 0; b < p.nseg * p.batch; ++b) sum += p.part[b * n + i];
     if (j < K) p.dw[d * K + j] = sum;
     else if (p.dbias) p.dbias[d] = sum;
 }

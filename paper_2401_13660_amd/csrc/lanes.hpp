@@ -1,0 +1,96 @@
+// lanes.hpp -- spans of consecutive elements per lane, lane shifts and sums over a wave.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "device_math.hpp"
+
+namespace mbs {
+
+// 16-byte and smaller vectors at any element's address: the hardware takes them.
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+
+// S consecutive elements as loaded; nothing is unpacked, so nothing is waited for, until get().
+template <int DT, int S> struct Span;
+template <> struct Span<1, 8> {
+    u32x4 v;
+    __device__ __forceinline__ void load(const void *p, int64_t at) {
+        v = *reinterpret_cast<const u32x4_any *>(static_cast<const uint16_t *>(p) + at);
+    }
+    __device__ __forceinline__ void load_first(const void *p, int64_t at, int n) {   // the rest: zeros
+        const uint16_t *e = static_cast<const uint16_t *>(p) + at;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            v[i] = (2 * i < n ? (uint32_t)e[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)e[2 * i + 1] << 16 : 0u);
+    }
+    __device__ __forceinline__ float get(int i) const { return i & 1 ? bf16_hi(v[i >> 1]) : bf16_lo(v[i >> 1]); }
+};
+template <> struct Span<1, 4> {
+    u32x2 v;
+    __device__ __forceinline__ void load(const void *p, int64_t at) {
+        v = *reinterpret_cast<const u32x2_any *>(static_cast<const uint16_t *>(p) + at);
+    }
+    __device__ __forceinline__ void load_first(const void *p, int64_t at, int n) {
+        const uint16_t *e = static_cast<const uint16_t *>(p) + at;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            v[i] = (2 * i < n ? (uint32_t)e[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)e[2 * i + 1] << 16 : 0u);
+    }
+    __device__ __forceinline__ float get(int i) const { return i & 1 ? bf16_hi(v[i >> 1]) : bf16_lo(v[i >> 1]); }
+};
+template <int S> struct Span<0, S> {
+    f32x4 v[S / 4];
+    __device__ __forceinline__ void load(const void *p, int64_t at) {
+#pragma unroll
+        for (int i = 0; i < S / 4; ++i) v[i] = reinterpret_cast<const f32x4_any *>(static_cast<const float *>(p) + at)[i];
+    }
+    __device__ __forceinline__ void load_first(const void *p, int64_t at, int n) {
+#pragma unroll
+        for (int i = 0; i < S; ++i) v[i / 4][i % 4] = i < n ? static_cast<const float *>(p)[at + i] : 0.0f;
+    }
+    __device__ __forceinline__ float get(int i) const { return v[i / 4][i % 4]; }
+};
+
+template <int DT, int S> __device__ __forceinline__ void store_span(void *p, int64_t at, const float (&v)[S]) {
+    if constexpr (DT == 0) {
+#pragma unroll
+        for (int i = 0; i < S / 4; ++i)
+            reinterpret_cast<f32x4_any *>(static_cast<float *>(p) + at)[i] = f32x4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+    } else if constexpr (S == 8) {
+        u32x4 r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = bf16x2_pack(v[2 * i], v[2 * i + 1]);
+        *reinterpret_cast<u32x4_any *>(static_cast<uint16_t *>(p) + at) = r;
+    } else {
+        u32x2 r;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) r[i] = bf16x2_pack(v[2 * i], v[2 * i + 1]);
+        *reinterpret_cast<u32x2_any *>(static_cast<uint16_t *>(p) + at) = r;
+    }
+}
+template <int DT, int S> __device__ __forceinline__ void store_first(void *p, int64_t at, const float (&v)[S], int n) {
+#pragma unroll
+    for (int i = 0; i < S; ++i)
+        if (i < n) st_out<DT>(p, at + i, v[i]);
+}
+
+// Each lane's neighbour's value; the wave's first (last) lane takes `edge`.
+__device__ __forceinline__ float from_lane_before(float v, float edge) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(edge), __float_as_int(v), 0x138, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float from_lane_after(float v, float edge) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(edge), __float_as_int(v), 0x130, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float lane_value(float v, int lane) {
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+    return v;
+}
+
+}  // namespace mbs

@@ -68,12 +68,22 @@ template <int IN, int OUT, int K> hipError_t conv_bwd_k(mbs::convbwd::Params &p,
     namespace C = mbs::convbwd;
     void *args[] = {&p};
     hipError_t e = hipSuccess;
-    if (p.batch > 0)
-        e = hipLaunchKernel(reinterpret_cast<const void *>(&C::conv1d_bwd<IN, OUT, K>), dim3(blocks_for(p.batch * p.dim)),
-                            dim3(C::kThreads), args, 0, st);
+    const int64_t waves = p.batch * p.dim * p.nseg;
+    if (waves > 0)
+        e = hipLaunchKernel(reinterpret_cast<const void *>(&C::conv1d_bwd<IN, OUT, K>),
+                            dim3((unsigned)((waves + C::kWaves - 1) / C::kWaves)), dim3(C::kThreads), args, 0, st);
     if (e != hipSuccess) return e;
     return hipLaunchKernel(reinterpret_cast<const void *>(&C::conv1d_bwd_finish<K>),
                            dim3((unsigned)((p.dim * (K + 1) + C::kThreads - 1) / C::kThreads)), dim3(C::kThreads), args, 0, st);
+}
+
+// Stretches per row: as many as bring the waves to 16 per SIMD.
+void conv_bwd_segments(mbs::convbwd::Params &p, int span) {
+    const int64_t rows = p.batch * p.dim, tiles = std::max<int64_t>((p.seqlen + 64 * span - 1) / (64 * span), 1);
+    const int64_t want = 4 * 256 * 16;
+    const int64_t n = std::min(tiles, std::max<int64_t>(1, want / std::max<int64_t>(rows, 1)));
+    p.seg_tiles = (int32_t)((tiles + n - 1) / n);
+    p.nseg = (tiles + p.seg_tiles - 1) / p.seg_tiles;
 }
 
 template <int IN, int OUT> hipError_t conv_bwd_dispatch(mbs::convbwd::Params &p, int K, hipStream_t st) {
@@ -227,7 +237,8 @@ int mb_conv1d_bwd(const mb_conv_desc *desc, const void *x, const float *w, const
     p.x = x; p.w = w; p.bias = bias; p.state_in = state_in; p.dy = dy; p.dstate_out = dstate_out;
     p.dx = dx; p.dw = dw; p.dbias = bias ? dbias : nullptr; p.dstate_in = dstate_in;
     p.apply_silu = desc->apply_silu ? 1 : 0;
-    hipError_t e = hipMallocAsync(reinterpret_cast<void **>(&p.part), (size_t)std::max<int64_t>(padded, 1) * 4, st);
+    conv_bwd_segments(p, desc->in_dtype == MB_F32 && desc->out_dtype == MB_F32 ? 4 : 8);
+    hipError_t e = hipMallocAsync(reinterpret_cast<void **>(&p.part), (size_t)std::max<int64_t>(padded * p.nseg, 1) * 4, st);
     if (e != hipSuccess) return MB_ERR_HIP;
     if (desc->in_dtype == MB_F32)
         e = desc->out_dtype == MB_F32 ? conv_bwd_dispatch<0, 0>(p, (int)K, st) : conv_bwd_dispatch<0, 1>(p, (int)K, st);
