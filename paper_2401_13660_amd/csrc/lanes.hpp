@@ -12,12 +12,38 @@ typedef u32x4 u32x4_any __attribute__((aligned(2)));
 typedef u32x2 u32x2_any __attribute__((aligned(2)));
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
 
+// ONCE: what is read or written once and is larger than the caches (their streaming policy).
+template <bool ONCE> __device__ __forceinline__ u32x4 fetch(const u32x4_any *p) {
+    if constexpr (ONCE) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+template <bool ONCE> __device__ __forceinline__ void put(u32x4_any *p, u32x4 r) {
+    if constexpr (ONCE) __builtin_nontemporal_store(r, p);
+    else *p = r;
+}
+template <bool ONCE> __device__ __forceinline__ u32x2 fetch(const u32x2_any *p) {
+    if constexpr (ONCE) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+template <bool ONCE> __device__ __forceinline__ void put(u32x2_any *p, u32x2 r) {
+    if constexpr (ONCE) __builtin_nontemporal_store(r, p);
+    else *p = r;
+}
+template <bool ONCE> __device__ __forceinline__ f32x4 fetch(const f32x4_any *p) {
+    if constexpr (ONCE) return __builtin_nontemporal_load(p);
+    else return *p;
+}
+template <bool ONCE> __device__ __forceinline__ void put(f32x4_any *p, f32x4 r) {
+    if constexpr (ONCE) __builtin_nontemporal_store(r, p);
+    else *p = r;
+}
+
 // S consecutive elements as loaded; nothing is unpacked, so nothing is waited for, until get().
 template <int DT, int S> struct Span;
 template <> struct Span<1, 8> {
     u32x4 v;
-    __device__ __forceinline__ void load(const void *p, int64_t at) {
-        v = *reinterpret_cast<const u32x4_any *>(static_cast<const uint16_t *>(p) + at);
+    template <bool ONCE = false> __device__ __forceinline__ void load(const void *p, int64_t at) {
+        v = fetch<ONCE>(reinterpret_cast<const u32x4_any *>(static_cast<const uint16_t *>(p) + at));
     }
     __device__ __forceinline__ void load_first(const void *p, int64_t at, int n) {   // the rest: zeros
         const uint16_t *e = static_cast<const uint16_t *>(p) + at;
@@ -29,8 +55,8 @@ template <> struct Span<1, 8> {
 };
 template <> struct Span<1, 4> {
     u32x2 v;
-    __device__ __forceinline__ void load(const void *p, int64_t at) {
-        v = *reinterpret_cast<const u32x2_any *>(static_cast<const uint16_t *>(p) + at);
+    template <bool ONCE = false> __device__ __forceinline__ void load(const void *p, int64_t at) {
+        v = fetch<ONCE>(reinterpret_cast<const u32x2_any *>(static_cast<const uint16_t *>(p) + at));
     }
     __device__ __forceinline__ void load_first(const void *p, int64_t at, int n) {
         const uint16_t *e = static_cast<const uint16_t *>(p) + at;
@@ -42,9 +68,10 @@ template <> struct Span<1, 4> {
 };
 template <int S> struct Span<0, S> {
     f32x4 v[S / 4];
-    __device__ __forceinline__ void load(const void *p, int64_t at) {
+    template <bool ONCE = false> __device__ __forceinline__ void load(const void *p, int64_t at) {
 #pragma unroll
-        for (int i = 0; i < S / 4; ++i) v[i] = reinterpret_cast<const f32x4_any *>(static_cast<const float *>(p) + at)[i];
+        for (int i = 0; i < S / 4; ++i)
+            v[i] = fetch<ONCE>(reinterpret_cast<const f32x4_any *>(static_cast<const float *>(p) + at) + i);
     }
     __device__ __forceinline__ void load_first(const void *p, int64_t at, int n) {
 #pragma unroll
@@ -53,21 +80,22 @@ template <int S> struct Span<0, S> {
     __device__ __forceinline__ float get(int i) const { return v[i / 4][i % 4]; }
 };
 
-template <int DT, int S> __device__ __forceinline__ void store_span(void *p, int64_t at, const float (&v)[S]) {
+template <int DT, int S, bool ONCE = false> __device__ __forceinline__ void store_span(void *p, int64_t at, const float (&v)[S]) {
     if constexpr (DT == 0) {
 #pragma unroll
         for (int i = 0; i < S / 4; ++i)
-            reinterpret_cast<f32x4_any *>(static_cast<float *>(p) + at)[i] = f32x4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+            put<ONCE>(reinterpret_cast<f32x4_any *>(static_cast<float *>(p) + at) + i,
+                      f32x4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]});
     } else if constexpr (S == 8) {
         u32x4 r;
 #pragma unroll
         for (int i = 0; i < 4; ++i) r[i] = bf16x2_pack(v[2 * i], v[2 * i + 1]);
-        *reinterpret_cast<u32x4_any *>(static_cast<uint16_t *>(p) + at) = r;
+        put<ONCE>(reinterpret_cast<u32x4_any *>(static_cast<uint16_t *>(p) + at), r);
     } else {
         u32x2 r;
 #pragma unroll
         for (int i = 0; i < 2; ++i) r[i] = bf16x2_pack(v[2 * i], v[2 * i + 1]);
-        *reinterpret_cast<u32x2_any *>(static_cast<uint16_t *>(p) + at) = r;
+        put<ONCE>(reinterpret_cast<u32x2_any *>(static_cast<uint16_t *>(p) + at), r);
     }
 }
 template <int DT, int S> __device__ __forceinline__ void store_first(void *p, int64_t at, const float (&v)[S], int n) {
