@@ -371,10 +371,14 @@ int mb_embedding_fwd(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_
  *   tokens  token_type (ntokens)       ntokens below 2^31
  *   dy      dy_dtype (ntokens, dim)
  *   dweight out_dtype (vocab, dim)     must not overlap an input
- * The call allocates a stream-ordered workspace (hipMallocAsync), freed on the same stream.
+ *   workspace  device memory of mb_embedding_bwd_workspace(ntokens, vocab, dim) bytes (of a
+ *              negative mb_status where the sizes are refused), 16-byte aligned, that nothing else
+ *              uses until the call's work is done; NULL: the call allocates it on the stream
+ *              (hipMallocAsync) and frees it there, which costs the host about 8 us
  */
 int mb_embedding_bwd(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_type, int32_t dy_dtype, int32_t out_dtype,
-                     float scale, const void *tokens, const void *dy, void *dweight, void *stream);
+                     float scale, const void *tokens, const void *dy, void *dweight, void *workspace, void *stream);
+int64_t mb_embedding_bwd_workspace(int64_t ntokens, int64_t vocab, int64_t dim);
 
 /*
  * The backward of mb_conv1d_fwd: the gradients of sum(dy * y) + sum(dstate_out *
@@ -389,12 +393,13 @@ int mb_embedding_bwd(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_
  *   dstate_in   float (B, D, k-1)     NULL means not written
  * Outputs are overwritten (not accumulated) and must not overlap any other
  * argument; with no row or no timestep dw and dbias are zeros.  D, B * D and L
- * below 2^31.  Arithmetic is fp32; results are deterministic.  The call allocates a
- * stream-ordered workspace (hipMallocAsync), freed on the same stream.
+ * below 2^31.  Arithmetic is fp32; results are deterministic.
+ *   workspace   as for mb_embedding_bwd, of mb_conv1d_bwd_workspace(desc) bytes
  */
 int mb_conv1d_bwd(const mb_conv_desc *desc, const void *x, const float *w, const float *bias, const float *state_in,
                   const void *dy, const float *dstate_out, void *dx, float *dw, float *dbias, float *dstate_in,
-                  void *stream);
+                  void *workspace, void *stream);
+int64_t mb_conv1d_bwd_workspace(const mb_conv_desc *desc);
 
 /*
  * The global norm of a list of tensors (the gradients of a model):
@@ -405,12 +410,14 @@ int mb_conv1d_bwd(const mb_conv_desc *desc, const void *x, const float *w, const
  *   grads, sizes, dtypes   HOST arrays (count): device addresses, element counts, mb_dtype.
  *                  They are read before the call returns.
  *   norm           float, DEVICE memory, must not overlap a tensor
- * Squares and sums are fp64, in an order that the list alone fixes; the result is
- * rounded to fp32.  The call allocates a stream-ordered workspace (hipMallocAsync),
- * freed on the same stream.
+ *   workspace      as for mb_embedding_bwd, of mb_grad_norm_workspace(count) bytes
+ * Squares and sums are fp64, in an order that the sizes and the addresses' places between
+ * 16-byte boundaries fix; the result is rounded to fp32.  count below 2^31, and less than
+ * about 2^44 elements in all.
  */
 int mb_grad_norm(int64_t count, const void *const *grads, const int64_t *sizes, const int32_t *dtypes, float *norm,
-                 void *stream);
+                 void *workspace, void *stream);
+int64_t mb_grad_norm_workspace(int64_t count);
 
 /*
  * mb_grad_norm, then the tensors clipped by it:
@@ -425,9 +432,11 @@ int mb_grad_norm(int64_t count, const void *const *grads, const int64_t *sizes, 
  *                  Written tensors overlap neither each other, norm nor (unless in place) grads.
  *   max_norm, eps  finite, >= 0 (MB_ERR_UNSUPPORTED otherwise)
  *   norm           the norm before clipping
+ *   workspace      as for mb_grad_norm
  */
 int mb_clip_grad_norm(int64_t count, const void *const *grads, void *const *out, const int64_t *sizes,
-                      const int32_t *dtypes, float max_norm, float eps, float *norm, void *stream);
+                      const int32_t *dtypes, float max_norm, float eps, float *norm, void *workspace,
+                      void *stream);
 
 /*
  * Verification of drafted tokens against the target's probabilities, from given

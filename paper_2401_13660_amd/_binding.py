@@ -74,13 +74,16 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.mb_embedding_fwd.restype = ctypes.c_int
     lib.mb_embedding_fwd.argtypes = [i64] * 3 + [i32] * 3 + [f32] + [_VP] * 4
     lib.mb_embedding_bwd.restype = ctypes.c_int
-    lib.mb_embedding_bwd.argtypes = [i64] * 3 + [i32] * 3 + [f32] + [_VP] * 4
+    lib.mb_embedding_bwd.argtypes = [i64] * 3 + [i32] * 3 + [f32] + [_VP] * 5
     lib.mb_conv1d_bwd.restype = ctypes.c_int
-    lib.mb_conv1d_bwd.argtypes = [ctypes.POINTER(ConvDesc)] + [_VP] * 11
+    lib.mb_conv1d_bwd.argtypes = [ctypes.POINTER(ConvDesc)] + [_VP] * 12
     lib.mb_grad_norm.restype = ctypes.c_int
-    lib.mb_grad_norm.argtypes = [i64] + [_VP] * 5
+    lib.mb_grad_norm.argtypes = [i64] + [_VP] * 6
     lib.mb_clip_grad_norm.restype = ctypes.c_int
-    lib.mb_clip_grad_norm.argtypes = [i64] + [_VP] * 4 + [f32] * 2 + [_VP] * 2
+    lib.mb_clip_grad_norm.argtypes = [i64] + [_VP] * 4 + [f32] * 2 + [_VP] * 3
+    for size, args in ((lib.mb_embedding_bwd_workspace, [i64] * 3), (lib.mb_grad_norm_workspace, [i64]),
+                       (lib.mb_conv1d_bwd_workspace, [ctypes.POINTER(ConvDesc)])):
+        size.restype, size.argtypes = i64, args
     lib.mb_verify_sample.restype = ctypes.c_int
     lib.mb_verify_sample.argtypes = [i64] * 3 + [i32, f32] + [_VP] * 11
     lib.mb_status_string.restype = ctypes.c_char_p
@@ -502,6 +505,12 @@ def scan_bwd(u, delta, A, B, C, dy, D=None, dt_bias=None, z=None, h0=None, dh_la
     return g
 
 
+def _workspace(size, what, dev):
+    """torch's memory for a call's workspace of ``size`` bytes: reused as soon as the stream has passed the call."""
+    _check(min(size, 0), what)
+    return torch.empty(size, dtype=torch.uint8, device=dev)
+
+
 _TOKEN_TYPES = {torch.uint8: 0, torch.int32: 1, torch.int64: 2}
 
 
@@ -552,9 +561,10 @@ def embedding_bwd(tokens, dy, vocab, *, scale=1.0, out_dtype=torch.float32, out=
         out = torch.empty((vocab, d), dtype=out_dtype, device=dev)
     else:
         _need(out, "out", (vocab, d), None, dev)
+    ws = _workspace(lib.mb_embedding_bwd_workspace(tokens.numel(), vocab, d), "mb_embedding_bwd", dev)
     with _on_device(dev):
         st = lib.mb_embedding_bwd(tokens.numel(), vocab, d, code, _dt(dy.dtype), _dt(out.dtype), float(scale),
-                                  _ptr(tokens), _ptr(dy), _ptr(out), _stream(dev))
+                                  _ptr(tokens), _ptr(dy), _ptr(out), _ptr(ws), _stream(dev))
     _check(st, "mb_embedding_bwd")
     return out
 
@@ -585,10 +595,11 @@ def conv1d_bwd(x, w, dy, bias=None, state=None, dstate_out=None, *, apply_silu=T
          "dbias": torch.empty(dim, **f32) if bias is not None else None,
          "dstate": torch.empty((nb, dim, H), **f32)}
     desc = ConvDesc(nb, dim, L, K, _dt(x.dtype), _dt(dy.dtype), 1 if apply_silu else 0, 0, 0)
+    ws = _workspace(lib.mb_conv1d_bwd_workspace(ctypes.byref(desc)), "mb_conv1d_bwd", dev)
     with _on_device(dev):
         st = lib.mb_conv1d_bwd(ctypes.byref(desc), _ptr(x), _ptr(w), _ptr(bias), _ptr(state) if H else None, _ptr(dy),
                                _ptr(dstate_out) if H else None, _ptr(g["dx"]), _ptr(g["dw"]), _ptr(g["dbias"]),
-                               _ptr(g["dstate"]) if H else None, _stream(dev))
+                               _ptr(g["dstate"]) if H else None, _ptr(ws), _stream(dev))
     _check(st, "mb_conv1d_bwd")
     return g
 
@@ -615,8 +626,9 @@ def grad_norm(grads):
     lib = load_library()
     grads, dev, ptrs, sizes, types = _grad_list(grads)
     norm = torch.empty((), dtype=torch.float32, device=dev)
+    ws = _workspace(lib.mb_grad_norm_workspace(len(grads)), "mb_grad_norm", dev)
     with _on_device(dev):
-        st = lib.mb_grad_norm(len(grads), ptrs, sizes, types, _ptr(norm), _stream(dev))
+        st = lib.mb_grad_norm(len(grads), ptrs, sizes, types, _ptr(norm), _ptr(ws), _stream(dev))
     _check(st, "mb_grad_norm")
     return norm
 
@@ -636,9 +648,10 @@ def clip_grad_norm(grads, max_norm, *, eps=1e-6, out=None):
             _need(o, f"out {i}", t.shape, t.dtype, dev)
         optrs = (_VP * len(out))(*(o.data_ptr() for o in out))
     norm = torch.empty((), dtype=torch.float32, device=dev)
+    ws = _workspace(lib.mb_grad_norm_workspace(len(grads)), "mb_clip_grad_norm", dev)
     with _on_device(dev):
         st = lib.mb_clip_grad_norm(len(grads), ptrs, optrs, sizes, types, float(max_norm), float(eps), _ptr(norm),
-                                   _stream(dev))
+                                   _ptr(ws), _stream(dev))
     _check(st, "mb_clip_grad_norm")
     return norm
 

@@ -32,10 +32,23 @@ template <int NO, int NI> bool any_overlap(const Range (&outs)[NO], const Range 
     return false;
 }
 
-// Workgroups of a grid-stride launch: enough for `items`, at most 2^20.
-unsigned blocks_for(int64_t items) { return (unsigned)std::min<int64_t>(std::max<int64_t>(items, 1), 1 << 20); }
-
 int status(hipError_t e) { return e == hipSuccess ? MB_OK : MB_ERR_HIP; }
+
+hipStream_t st_of(void *stream) { return static_cast<hipStream_t>(stream); }
+
+// The caller's workspace, or memory allocated on the stream for the call (`at` null: it could not be).
+struct Workspace {
+    char *at;
+    hipStream_t st;
+    bool own;
+    Workspace(void *given, size_t bytes, hipStream_t stream) : at(static_cast<char *>(given)), st(stream), own(!given) {
+        if (own && hipMallocAsync(reinterpret_cast<void **>(&at), std::max<size_t>(bytes, 16), st) != hipSuccess) at = nullptr;
+    }
+    hipError_t done(hipError_t e) const {
+        const hipError_t f = own ? hipFreeAsync(at, st) : hipSuccess;
+        return e != hipSuccess ? e : f;
+    }
+};
 
 bool valid_token_type(int32_t t) { return t == MB_TOKEN_U8 || t == MB_TOKEN_I32 || t == MB_TOKEN_I64; }
 size_t token_size(int32_t t) { return t == MB_TOKEN_U8 ? 1 : t == MB_TOKEN_I32 ? 4 : 8; }
@@ -47,12 +60,81 @@ template <int TOK, int A> const void *embed_fwd_fn(int32_t out) {
 template <int TOK> const void *embed_fwd_fn(int32_t in, int32_t out) {
     return in == MB_F32 ? embed_fwd_fn<TOK, 0>(out) : embed_fwd_fn<TOK, 1>(out);
 }
-template <int TOK, int A> const void *embed_bwd_fn(int32_t out) {
-    return out == MB_F32 ? reinterpret_cast<const void *>(&mbs::embed::embed_bwd<TOK, A, 0>)
-                         : reinterpret_cast<const void *>(&mbs::embed::embed_bwd<TOK, A, 1>);
+// The workspace's areas, each on a 256-byte boundary.
+struct Areas {
+    size_t bytes = 0;
+    size_t add(size_t n) {
+        const size_t at = bytes;
+        bytes += (n + 255) / 256 * 256;
+        return at;
+    }
+};
+
+// The sort of an embedding's gradient and its workspace.
+struct EmbedPlan {
+    int64_t tile, tiles, chunks;
+    int passes;
+    size_t counts, valid, a, b, head, tail, bytes;
+    EmbedPlan(int64_t ntokens, int64_t vocab, int64_t dim) {
+        namespace E = mbs::embed;
+        // tokens per workgroup: 1,024, or what keeps the workgroups at kBins (each reads the counts of all)
+        tile = std::max<int64_t>(1024, ((ntokens + E::kBins - 1) / E::kBins + 1023) / 1024 * 1024);
+        tiles = (ntokens + tile - 1) / tile;
+        passes = 1;
+        while (passes < 4 && (vocab - 1) >> (8 * passes)) ++passes;
+        chunks = (ntokens + E::kChunk - 1) / E::kChunk;
+        Areas w;
+        counts = w.add((size_t)tiles * E::kBins * 4);
+        valid = w.add(4);
+        a = w.add((size_t)ntokens * sizeof(E::Pair));
+        b = w.add(passes > 1 ? (size_t)ntokens * sizeof(E::Pair) : 0);
+        head = w.add((size_t)chunks * (size_t)dim * 4);
+        tail = w.add((size_t)chunks * (size_t)dim * 4);
+        bytes = w.bytes;
+    }
+};
+
+template <int TOK, int OUT> hipError_t embed_sort(mbs::embed::BwdParams &p, const EmbedPlan &f, char *ws, hipStream_t st) {
+    namespace E = mbs::embed;
+    E::Pair *const ab[2] = {reinterpret_cast<E::Pair *>(ws + f.a), reinterpret_cast<E::Pair *>(ws + f.b)};
+    const int64_t fill = (p.vocab * p.dim + 4095) / 4096;           // workgroups that zero the table beside the first count
+    for (int k = 0; k < f.passes; ++k) {
+        p.shift = 8 * k;
+        p.from = k == 0 ? nullptr : ab[(k - 1) & 1];
+        p.to = ab[k & 1];
+        void *args[] = {&p};
+        const int64_t blocks = k == 0 ? std::max<int64_t>(f.tiles, std::min<int64_t>(fill, 2048)) : f.tiles;
+        hipError_t e = hipLaunchKernel(k == 0 ? reinterpret_cast<const void *>(&E::count_digits<TOK, OUT, true>)
+                                              : reinterpret_cast<const void *>(&E::count_digits<TOK, OUT, false>),
+                                       dim3((unsigned)std::max<int64_t>(blocks, 1)), dim3(E::kThreads), args, 0, st);
+        if (e != hipSuccess || f.tiles == 0) return e;
+        e = hipLaunchKernel(k == 0 ? reinterpret_cast<const void *>(&E::scatter<TOK, true>)
+                                   : reinterpret_cast<const void *>(&E::scatter<TOK, false>),
+                            dim3((unsigned)f.tiles), dim3(E::kThreads), args, 0, st);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
-template <int TOK> const void *embed_bwd_fn(int32_t in, int32_t out) {
-    return in == MB_F32 ? embed_bwd_fn<TOK, 0>(out) : embed_bwd_fn<TOK, 1>(out);
+
+template <int DY, int OUT> hipError_t embed_sum(mbs::embed::BwdParams &p, const EmbedPlan &f, hipStream_t st) {
+    namespace E = mbs::embed;
+    uint32_t cols = (uint32_t)((p.dim + 64 * E::kRowSpan<DY, OUT> - 1) / (64 * E::kRowSpan<DY, OUT>));
+    void *args[] = {&p, &cols};
+    hipError_t e = hipLaunchKernel(reinterpret_cast<const void *>(&E::sum_chunks<DY, OUT>),
+                                   dim3((unsigned)((f.chunks * cols + E::kWaves - 1) / E::kWaves)), dim3(E::kThreads), args, 0, st);
+    if (e != hipSuccess || f.chunks < 2) return e;
+    cols = (uint32_t)((p.dim + 255) / 256);
+    return hipLaunchKernel(reinterpret_cast<const void *>(&E::join_chunks<OUT>), dim3((unsigned)((f.chunks - 1) * cols)),
+                           dim3(64 * E::kJoinWaves), args, 0, st);
+}
+
+template <int OUT> hipError_t embed_bwd(mbs::embed::BwdParams &p, const EmbedPlan &f, int32_t token_type, int32_t dy_dtype,
+                                        char *ws, hipStream_t st) {
+    const hipError_t e = token_type == MB_TOKEN_U8    ? embed_sort<0, OUT>(p, f, ws, st)
+                         : token_type == MB_TOKEN_I32 ? embed_sort<1, OUT>(p, f, ws, st)
+                                                      : embed_sort<2, OUT>(p, f, ws, st);
+    if (e != hipSuccess || f.tiles == 0) return e;
+    return dy_dtype == MB_F32 ? embed_sum<0, OUT>(p, f, st) : embed_sum<1, OUT>(p, f, st);
 }
 
 // The checks that both directions share; the element counts of the tokens' and the table's rows.
@@ -78,7 +160,8 @@ template <int IN, int OUT, int K> hipError_t conv_bwd_k(mbs::convbwd::Params &p,
 }
 
 // Stretches per row: as many as bring the waves to 16 per SIMD.
-void conv_bwd_segments(mbs::convbwd::Params &p, int span) {
+void conv_bwd_segments(mbs::convbwd::Params &p, int32_t in_dtype, int32_t out_dtype) {
+    const int64_t span = in_dtype == MB_F32 && out_dtype == MB_F32 ? 4 : 8;
     const int64_t rows = p.batch * p.dim, tiles = std::max<int64_t>((p.seqlen + 64 * span - 1) / (64 * span), 1);
     const int64_t want = 4 * 256 * 16;
     const int64_t n = std::min(tiles, std::max<int64_t>(1, want / std::max<int64_t>(rows, 1)));
@@ -95,11 +178,20 @@ template <int IN, int OUT> hipError_t conv_bwd_dispatch(mbs::convbwd::Params &p,
     }
 }
 
-// The checks of a list of tensors; *total: their elements.
-int list_checks(int64_t count, const void *const *grads, const int64_t *sizes, const int32_t *dtypes, const float *norm) {
-    if (count < 0) return MB_ERR_SHAPE;
+// Partial sums, and the list where it does not fit the kernels' arguments.
+size_t clip_workspace(int64_t count) {
+    namespace C = mbs::clip;
+    return sizeof(double) * C::kBlocks + (count <= C::kInline ? 0 : sizeof(C::Entry) * (size_t)count);
+}
+
+// The checks of a list of tensors.
+int list_checks(int64_t count, const void *const *grads, const int64_t *sizes, const int32_t *dtypes, const float *norm,
+                const void *workspace) {
+    if (count < 0 || count >= (int64_t(1) << 31)) return MB_ERR_SHAPE;
     if (!norm || (count > 0 && (!grads || !sizes || !dtypes))) return MB_ERR_NULL;
-    if (!aligned(norm, 4)) return MB_ERR_ALIGN;
+    if (!aligned(norm, 4) || !aligned(workspace, 16)) return MB_ERR_ALIGN;
+    const size_t ws_b = workspace ? clip_workspace(count) : 0;
+    if (overlaps(norm, 4, workspace, ws_b)) return MB_ERR_ALIAS;
     int64_t total = 0;
     for (int64_t i = 0; i < count; ++i) {
         if (sizes[i] < 0 || sizes[i] > kMaxElems - total) return MB_ERR_SHAPE;
@@ -108,7 +200,8 @@ int list_checks(int64_t count, const void *const *grads, const int64_t *sizes, c
         if (sizes[i] > 0 && !grads[i]) return MB_ERR_NULL;
         const size_t e = dtype_size(dtypes[i]);
         if (!aligned(grads[i], e)) return MB_ERR_ALIGN;
-        if (overlaps(norm, 4, grads[i], (size_t)sizes[i] * e)) return MB_ERR_ALIAS;
+        if (overlaps(norm, 4, grads[i], (size_t)sizes[i] * e) || overlaps(workspace, ws_b, grads[i], (size_t)sizes[i] * e))
+            return MB_ERR_ALIAS;
     }
     return MB_OK;
 }
@@ -142,23 +235,70 @@ int list_alias(int64_t count, const void *const *grads, void *const *out, const 
     return bad ? MB_ERR_ALIAS : MB_OK;
 }
 
-hipError_t norm_partials(int64_t count, const void *const *grads, const int64_t *sizes, const int32_t *dtypes, double *part,
-                         hipStream_t st, int *nparts) {
+// The norm of a list and, where `scaled`, its clipping.
+int norm_and_clip(int64_t count, const void *const *grads, void *const *out, const int64_t *sizes, const int32_t *dtypes,
+                  bool scaled, float max_norm, float eps, float *norm, void *workspace, hipStream_t st) {
     namespace C = mbs::clip;
-    int first = 1;
+    int64_t used = 0, units = 0;
     for (int64_t i = 0; i < count; ++i) {
         if (sizes[i] == 0) continue;
-        const void *g = grads[i];
-        int64_t n = sizes[i];
-        void *args[] = {&g, &n, &part, &first};
-        const hipError_t e = hipLaunchKernel(dtypes[i] == MB_F32 ? reinterpret_cast<const void *>(&C::sum_squares<0>)
-                                                                 : reinterpret_cast<const void *>(&C::sum_squares<1>),
-                                             dim3(C::kBlocks), dim3(C::kThreads), args, 0, st);
-        if (e != hipSuccess) return e;
-        first = 0;
+        units += (sizes[i] + C::lead(grads[i], dtypes[i]) + C::kUnit - 1) / C::kUnit;
+        ++used;
+        if (units >= (int64_t(1) << 31) || used >= (int64_t(1) << 31)) return MB_ERR_SHAPE;
     }
-    *nparts = first ? 0 : C::kBlocks;
-    return hipSuccess;
+    // the entries of the tensors from *i on, at most n of them, empty ones left out
+    int64_t next = 0;
+    uint32_t unit = 0;
+    auto entries = [&](C::Entry *e, int n) {
+        int k = 0;
+        for (; next < count && k < n; ++next) {
+            if (sizes[next] == 0) continue;
+            const void *g = grads[next];
+            e[k++] = {g, out ? out[next] : const_cast<void *>(g), sizes[next], unit, dtypes[next]};
+            unit += (uint32_t)((sizes[next] + C::lead(g, dtypes[next]) + C::kUnit - 1) / C::kUnit);
+        }
+        return k;
+    };
+    const bool inlined = used <= C::kInline;
+    Workspace ws(workspace, clip_workspace(used), st);
+    if (!ws.at) return MB_ERR_HIP;
+    hipError_t e = hipSuccess;
+    C::Params p{};
+    p.count = (int32_t)used;
+    p.units = (uint32_t)units;
+    p.part = reinterpret_cast<double *>(ws.at);
+    p.norm = norm;
+    p.max_norm = max_norm;
+    p.eps = eps;
+    const dim3 grid((unsigned)std::min<int64_t>(std::max<int64_t>(units, 1), C::kBlocks)), block(C::kThreads);
+    C::Table<C::kInline> small{};
+    void *args[] = {&p, &small};
+    if (inlined) {
+        entries(small.e, C::kInline);
+    } else {
+        C::Entry *table = reinterpret_cast<C::Entry *>(ws.at + sizeof(double) * C::kBlocks);
+        p.table = table;
+        while (e == hipSuccess && next < count) {
+            C::Table<C::kFill> some{};
+            int n = entries(some.e, C::kFill);
+            void *fargs[] = {&some, &n, &table};
+            if (n > 0)
+                e = hipLaunchKernel(reinterpret_cast<const void *>(&C::fill_table), dim3(1), dim3(128), fargs, 0, st);
+            table += n;
+        }
+    }
+    if (e == hipSuccess)
+        e = hipLaunchKernel(inlined ? reinterpret_cast<const void *>(&C::sum_squares_inline)
+                                    : reinterpret_cast<const void *>(&C::sum_squares), grid, block, args, 0, st);
+    if (e == hipSuccess && scaled)
+        e = hipLaunchKernel(inlined ? reinterpret_cast<const void *>(&C::scale_inline)
+                                    : reinterpret_cast<const void *>(&C::scale), grid, block, args, 0, st);
+    if (e == hipSuccess && !scaled) {
+        int nparts = (int)grid.x;
+        void *nargs[] = {&p, &nparts};
+        e = hipLaunchKernel(reinterpret_cast<const void *>(&C::finish_norm), dim3(1), block, nargs, 0, st);
+    }
+    return status(ws.done(e));
 }
 
 }  // namespace
@@ -177,16 +317,20 @@ int mb_embedding_fwd(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_
     const Range outs[] = {{out, (size_t)row_elems * osz}};
     const Range ins[] = {{tokens, (size_t)ntokens * tsz}, {weight, (size_t)table_elems * wsz}};
     if (any_overlap(outs, ins)) return MB_ERR_ALIAS;
-    mbs::embed::FwdParams p{ntokens, vocab, dim, tokens, weight, out, scale};
+    // spans of a row, and rows per workgroup: 1,024 spans where that leaves 2,048 workgroups
+    const int64_t span = weight_dtype == MB_F32 && out_dtype == MB_F32 ? 4 : 8, spans = (dim + span - 1) / span;
+    const int64_t rows = std::max<int64_t>(1, std::min(1024 / spans, ntokens / 2048));
+    const int64_t blocks = (ntokens + rows - 1) / rows;
+    if (spans >= (int64_t(1) << 31) || blocks >= (int64_t(1) << 24)) return MB_ERR_SHAPE;
+    mbs::embed::FwdParams p{ntokens, vocab, dim, tokens, weight, out, scale, (int32_t)rows};
     const void *fn = token_type == MB_TOKEN_U8    ? embed_fwd_fn<0>(weight_dtype, out_dtype)
                      : token_type == MB_TOKEN_I32 ? embed_fwd_fn<1>(weight_dtype, out_dtype)
                                                   : embed_fwd_fn<2>(weight_dtype, out_dtype);
-    return status(launch(fn, dim3(blocks_for((row_elems + mbs::embed::kThreads - 1) / mbs::embed::kThreads)),
-                         dim3(mbs::embed::kThreads), &p, stream));
+    return status(launch(fn, dim3((unsigned)blocks), dim3(mbs::embed::kThreads), &p, stream));
 }
 
 int mb_embedding_bwd(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_type, int32_t dy_dtype, int32_t out_dtype,
-                     float scale, const void *tokens, const void *dy, void *dweight, void *stream) {
+                     float scale, const void *tokens, const void *dy, void *dweight, void *workspace, void *stream) {
     int64_t row_elems, table_elems;
     const int st = embed_checks(ntokens, vocab, dim, token_type, dy_dtype, out_dtype, &row_elems, &table_elems);
     if (st != MB_OK) return st;
@@ -195,20 +339,39 @@ int mb_embedding_bwd(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_
     if (!dweight || (ntokens > 0 && (!tokens || !dy))) return MB_ERR_NULL;
     const size_t tsz = token_size(token_type), ysz = dtype_size(dy_dtype), osz = dtype_size(out_dtype);
     if (!aligned(tokens, tsz) || !aligned(dy, ysz) || !aligned(dweight, osz)) return MB_ERR_ALIGN;
-    const Range outs[] = {{dweight, (size_t)table_elems * osz}};
+    if (!aligned(workspace, 16)) return MB_ERR_ALIGN;
+    const Range outs[] = {{dweight, (size_t)table_elems * osz},
+                          {workspace, workspace ? EmbedPlan(ntokens, vocab, dim).bytes : 0}};
     const Range ins[] = {{tokens, (size_t)ntokens * tsz}, {dy, (size_t)row_elems * ysz}};
     if (any_overlap(outs, ins)) return MB_ERR_ALIAS;
-    mbs::embed::BwdParams p{ntokens, vocab, dim, tokens, dy, dweight, scale};
-    const void *fn = token_type == MB_TOKEN_U8    ? embed_bwd_fn<0>(dy_dtype, out_dtype)
-                     : token_type == MB_TOKEN_I32 ? embed_bwd_fn<1>(dy_dtype, out_dtype)
-                                                  : embed_bwd_fn<2>(dy_dtype, out_dtype);
-    const int64_t tiles = (dim + mbs::embed::kThreads - 1) / mbs::embed::kThreads;
-    return status(launch(fn, dim3(blocks_for(vocab * tiles)), dim3(mbs::embed::kThreads), &p, stream));
+    const EmbedPlan f(ntokens, vocab, dim);
+    if (f.chunks * ((dim + 255) / 256) >= (int64_t(1) << 31)) return MB_ERR_SHAPE;
+    Workspace ws(workspace, f.bytes, st_of(stream));
+    if (!ws.at) return MB_ERR_HIP;
+    mbs::embed::BwdParams p{};
+    p.ntokens = ntokens; p.vocab = vocab; p.dim = dim;
+    p.tokens = tokens; p.dy = dy; p.dweight = dweight; p.scale = scale;
+    p.tile = (int32_t)f.tile; p.tiles = (int32_t)f.tiles;
+    p.counts = reinterpret_cast<uint32_t *>(ws.at + f.counts);
+    p.valid = reinterpret_cast<uint32_t *>(ws.at + f.valid);
+    p.head = reinterpret_cast<float *>(ws.at + f.head);
+    p.tail = reinterpret_cast<float *>(ws.at + f.tail);
+    const hipError_t e = out_dtype == MB_F32 ? embed_bwd<0>(p, f, token_type, dy_dtype, ws.at, st_of(stream))
+                                             : embed_bwd<1>(p, f, token_type, dy_dtype, ws.at, st_of(stream));
+    return status(ws.done(e));
+}
+
+int64_t mb_embedding_bwd_workspace(int64_t ntokens, int64_t vocab, int64_t dim) {
+    int64_t row_elems, table_elems;
+    const int st = embed_checks(ntokens, vocab, dim, MB_TOKEN_U8, MB_F32, MB_F32, &row_elems, &table_elems);
+    if (st != MB_OK) return st;
+    if (ntokens >= (int64_t(1) << 31)) return MB_ERR_SHAPE;
+    return (int64_t)EmbedPlan(ntokens, vocab, dim).bytes;
 }
 
 int mb_conv1d_bwd(const mb_conv_desc *desc, const void *x, const float *w, const float *bias, const float *state_in,
                   const void *dy, const float *dstate_out, void *dx, float *dw, float *dbias, float *dstate_in,
-                  void *stream) {
+                  void *workspace, void *stream) {
     if (!desc) return MB_ERR_NULL;
     const int64_t B = desc->batch, D = desc->dim, L = desc->seqlen, K = desc->width;
     if (B < 0 || D < 0 || L < 0) return MB_ERR_SHAPE;
@@ -228,79 +391,72 @@ int mb_conv1d_bwd(const mb_conv_desc *desc, const void *x, const float *w, const
     const size_t w_b = (size_t)(D * K) * 4, b_b = (size_t)D * 4, st_b = (size_t)(rows * (K - 1)) * 4;
     const Range ins[] = {{x, (size_t)elems * in_sz}, {w, w_b}, {bias, b_b}, {state_in, st_b}, {dy, (size_t)elems * out_sz},
                          {dstate_out, st_b}};
-    const Range outs[] = {{dx, (size_t)elems * out_sz}, {dw, w_b}, {dbias, bias ? b_b : 0}, {dstate_in, st_b}};
-    if (any_overlap(outs, ins)) return MB_ERR_ALIAS;
-
-    hipStream_t st = static_cast<hipStream_t>(stream);
     mbs::convbwd::Params p{};
     p.batch = B; p.dim = D; p.seqlen = L;
+    conv_bwd_segments(p, desc->in_dtype, desc->out_dtype);
+    const size_t part_b = (size_t)(padded * p.nseg) * 4;
+    if (!aligned(workspace, 16)) return MB_ERR_ALIGN;
+    const Range outs[] = {{dx, (size_t)elems * out_sz}, {dw, w_b}, {dbias, bias ? b_b : 0}, {dstate_in, st_b},
+                          {workspace, part_b}};
+    if (any_overlap(outs, ins)) return MB_ERR_ALIAS;
+
     p.x = x; p.w = w; p.bias = bias; p.state_in = state_in; p.dy = dy; p.dstate_out = dstate_out;
     p.dx = dx; p.dw = dw; p.dbias = bias ? dbias : nullptr; p.dstate_in = dstate_in;
     p.apply_silu = desc->apply_silu ? 1 : 0;
-    conv_bwd_segments(p, desc->in_dtype == MB_F32 && desc->out_dtype == MB_F32 ? 4 : 8);
-    hipError_t e = hipMallocAsync(reinterpret_cast<void **>(&p.part), (size_t)std::max<int64_t>(padded * p.nseg, 1) * 4, st);
-    if (e != hipSuccess) return MB_ERR_HIP;
+    Workspace ws(workspace, part_b, st_of(stream));
+    if (!ws.at) return MB_ERR_HIP;
+    p.part = reinterpret_cast<float *>(ws.at);
+    hipStream_t st = ws.st;
+    hipError_t e;
     if (desc->in_dtype == MB_F32)
         e = desc->out_dtype == MB_F32 ? conv_bwd_dispatch<0, 0>(p, (int)K, st) : conv_bwd_dispatch<0, 1>(p, (int)K, st);
     else
         e = desc->out_dtype == MB_F32 ? conv_bwd_dispatch<1, 0>(p, (int)K, st) : conv_bwd_dispatch<1, 1>(p, (int)K, st);
-    const hipError_t f = hipFreeAsync(p.part, st);
-    return status(e != hipSuccess ? e : f);
+    return status(ws.done(e));
+}
+
+int64_t mb_conv1d_bwd_workspace(const mb_conv_desc *desc) {
+    if (!desc) return MB_ERR_NULL;
+    const int64_t B = desc->batch, D = desc->dim, K = desc->width;
+    int64_t rows, padded;
+    if (B < 0 || D < 0 || desc->seqlen < 0 || !mul_ok(B, D, &rows) || rows >= (int64_t(1) << 31) || D >= (int64_t(1) << 31) ||
+        desc->seqlen >= (int64_t(1) << 31) || !mul_ok(rows, K + 1, &padded))
+        return MB_ERR_SHAPE;
+    if (!valid_dtype(desc->in_dtype) || !valid_dtype(desc->out_dtype)) return MB_ERR_DTYPE;
+    if (K < 1 || K > 4) return MB_ERR_UNSUPPORTED;
+    mbs::convbwd::Params p{};
+    p.batch = B; p.dim = D; p.seqlen = desc->seqlen;
+    conv_bwd_segments(p, desc->in_dtype, desc->out_dtype);
+    return padded * p.nseg * 4;
 }
 
 int mb_grad_norm(int64_t count, const void *const *grads, const int64_t *sizes, const int32_t *dtypes, float *norm,
-                 void *stream) {
-    namespace C = mbs::clip;
-    const int bad = list_checks(count, grads, sizes, dtypes, norm);
+                 void *workspace, void *stream) {
+    const int bad = list_checks(count, grads, sizes, dtypes, norm, workspace);
     if (bad != MB_OK) return bad;
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    double *part = nullptr;
-    if (hipMallocAsync(reinterpret_cast<void **>(&part), sizeof(double) * C::kBlocks, st) != hipSuccess) return MB_ERR_HIP;
-    int nparts = 0;
-    hipError_t e = norm_partials(count, grads, sizes, dtypes, part, st, &nparts);
-    float zero = 0.0f, *none = nullptr;
-    void *args[] = {&part, &nparts, &zero, &zero, &norm, &none};
-    if (e == hipSuccess)
-        e = hipLaunchKernel(reinterpret_cast<const void *>(&C::finish_norm), dim3(1), dim3(C::kThreads), args, 0, st);
-    const hipError_t f = hipFreeAsync(part, st);
-    return status(e != hipSuccess ? e : f);
+    return norm_and_clip(count, grads, nullptr, sizes, dtypes, false, 0.0f, 0.0f, norm, workspace, st_of(stream));
+}
+
+int64_t mb_grad_norm_workspace(int64_t count) {
+    return count < 0 || count >= (int64_t(1) << 31) ? MB_ERR_SHAPE : (int64_t)clip_workspace(count);
 }
 
 int mb_clip_grad_norm(int64_t count, const void *const *grads, void *const *out, const int64_t *sizes,
-                      const int32_t *dtypes, float max_norm, float eps, float *norm, void *stream) {
-    namespace C = mbs::clip;
-    int bad = list_checks(count, grads, sizes, dtypes, norm);
+                      const int32_t *dtypes, float max_norm, float eps, float *norm, void *workspace,
+                      void *stream) {
+    int bad = list_checks(count, grads, sizes, dtypes, norm, workspace);
     if (bad != MB_OK) return bad;
     if (!(max_norm >= 0.0f) || !(eps >= 0.0f) || std::isinf(max_norm) || std::isinf(eps)) return MB_ERR_UNSUPPORTED;
     for (int64_t i = 0; out && i < count; ++i) {
         if (sizes[i] > 0 && !out[i]) return MB_ERR_NULL;
         if (!aligned(out[i], dtype_size(dtypes[i]))) return MB_ERR_ALIGN;
-        if (overlaps(norm, 4, out[i], (size_t)sizes[i] * dtype_size(dtypes[i]))) return MB_ERR_ALIAS;
+        const size_t bytes = (size_t)sizes[i] * dtype_size(dtypes[i]);
+        if (overlaps(norm, 4, out[i], bytes) || (workspace && overlaps(workspace, clip_workspace(count), out[i], bytes)))
+            return MB_ERR_ALIAS;
     }
     bad = list_alias(count, grads, out, sizes, dtypes);
     if (bad != MB_OK) return bad;
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    double *part = nullptr;
-    if (hipMallocAsync(reinterpret_cast<void **>(&part), sizeof(double) * (C::kBlocks + 1), st) != hipSuccess)
-        return MB_ERR_HIP;
-    float *factor = reinterpret_cast<float *>(part + C::kBlocks);
-    int nparts = 0;
-    hipError_t e = norm_partials(count, grads, sizes, dtypes, part, st, &nparts);
-    void *args[] = {&part, &nparts, &max_norm, &eps, &norm, &factor};
-    if (e == hipSuccess)
-        e = hipLaunchKernel(reinterpret_cast<const void *>(&C::finish_norm), dim3(1), dim3(C::kThreads), args, 0, st);
-    for (int64_t i = 0; e == hipSuccess && i < count; ++i) {
-        if (sizes[i] == 0) continue;
-        const void *g = grads[i];
-        void *o = out ? out[i] : const_cast<void *>(g);
-        int64_t n = sizes[i];
-        void *sargs[] = {&g, &o, &n, &factor};
-        e = hipLaunchKernel(dtypes[i] == MB_F32 ? reinterpret_cast<const void *>(&C::scale_by<0>)
-                                                : reinterpret_cast<const void *>(&C::scale_by<1>),
-                            dim3(C::kBlocks), dim3(C::kThreads), sargs, 0, st);
-    }
-    const hipError_t f = hipFreeAsync(part, st);
-    return status(e != hipSuccess ? e : f);
+    return norm_and_clip(count, grads, out, sizes, dtypes, true, max_norm, eps, norm, workspace, st_of(stream));
 }
 
 int mb_verify_sample(int64_t batch, int64_t ndraft, int64_t vocab, int32_t logit_dtype, float temperature,

@@ -30,14 +30,15 @@ def test_embedding_rejects(name, over, code):
     v = dict(n=10, V=256, d=64, tok=1, it=1, ot=0, a=P["tokens"], b=P["weight"], c=P["out"])
     v.update(over)
     fn = getattr(mb.load_library(), name)
-    assert fn(v["n"], v["V"], v["d"], v["tok"], v["it"], v["ot"], 1.0, v["a"], v["b"], v["c"], None) == code
+    ws = [None] if name.endswith("bwd") else []
+    assert fn(v["n"], v["V"], v["d"], v["tok"], v["it"], v["ot"], 1.0, v["a"], v["b"], v["c"], *ws, None) == code
 
 
 def test_embedding_empty():
     lib = mb.load_library()
     assert lib.mb_embedding_fwd(0, 256, 64, 0, 0, 0, 1.0, None, None, None, None) == 0
     assert lib.mb_embedding_fwd(5, 256, 0, 0, 0, 0, 1.0, None, None, None, None) == 0
-    assert lib.mb_embedding_bwd(5, 0, 64, 0, 0, 0, 1.0, None, None, None, None) == 0
+    assert lib.mb_embedding_bwd(5, 0, 64, 0, 0, 0, 1.0, None, None, None, None, None) == 0
 
 
 @no_gpu_only
@@ -50,18 +51,18 @@ def test_embedding_empty():
     ({}, dict(dw=None), -1), ({}, dict(dbias=None), -1),
     ({}, dict(x=P["x"] + 1), -4), ({}, dict(dy=P["dy"] + 2), -4), ({}, dict(state=P["state"] + 2), -4),
     ({}, dict(dx=P["dy"]), -7), ({}, dict(dx=P["x"] + 16), -7), ({}, dict(dw=P["w"]), -7), ({}, dict(dsi=P["dso"]), -7),
-    ({}, dict(dsi=P["dx"] + 64), -7),
+    ({}, dict(dsi=P["dx"] + 64), -7), ({}, dict(ws=P["x"] + 8), -4), ({}, dict(ws=P["dy"] + 16), -7),
 ])
 def test_conv_bwd_rejects(desc, over, code):
     v = {k: P[k] for k in ("x", "w", "bias", "state", "dy", "dso", "dx", "dw", "dbias", "dsi")}
-    v.update(over)
+    v.update(dict(ws=None), **over)
     d = None
     if desc is not None:
         c = dict(batch=2, dim=8, seqlen=16, width=4, in_dtype=1, out_dtype=0, apply_silu=1, reserved=0, reserved2=0)
         c.update(desc)
         d = ctypes.byref(B.ConvDesc(**c))
     assert mb.load_library().mb_conv1d_bwd(d, v["x"], v["w"], v["bias"], v["state"], v["dy"], v["dso"], v["dx"], v["dw"],
-                                           v["dbias"], v["dsi"], None) == code
+                                           v["dbias"], v["dsi"], v["ws"], None) == code
 
 
 def _lists(ptrs, sizes, types):
@@ -88,8 +89,8 @@ A0 = 0x7000000000
 def test_grad_norm_rejects(count, ptrs, sizes, types, norm, code):
     lib = mb.load_library()
     p, s, t = _lists(ptrs, sizes, types)
-    assert lib.mb_grad_norm(count, p, s, t, norm, None) == code
-    assert lib.mb_clip_grad_norm(count, p, None, s, t, 1.0, 1e-6, norm, None) == code
+    assert lib.mb_grad_norm(count, p, s, t, norm, None, None) == code
+    assert lib.mb_clip_grad_norm(count, p, None, s, t, 1.0, 1e-6, norm, None, None) == code
 
 
 @no_gpu_only
@@ -112,7 +113,29 @@ def test_grad_norm_rejects(count, ptrs, sizes, types, norm, code):
 def test_clip_rejects(ptrs, out, max_norm, eps, code):
     p, s, t = _lists(ptrs, [16, 16], [0, 0])
     o = None if out is None else (ctypes.c_void_p * 2)(*out)
-    assert mb.load_library().mb_clip_grad_norm(2, p, o, s, t, max_norm, eps, P["norm"], None) == code
+    assert mb.load_library().mb_clip_grad_norm(2, p, o, s, t, max_norm, eps, P["norm"], None, None) == code
+
+
+@no_gpu_only
+def test_workspaces():
+    """Their sizes, and that one which overlaps or is not aligned is refused."""
+    lib = mb.load_library()
+    assert lib.mb_grad_norm_workspace(-1) == -2 and lib.mb_embedding_bwd_workspace(-1, 1, 1) == -2
+    assert lib.mb_embedding_bwd_workspace(1 << 31, 256, 64) == -2
+    assert lib.mb_conv1d_bwd_workspace(None) == -1
+    d = B.ConvDesc(4, 3584, 8192, 4, 1, 1, 1, 0, 0)
+    assert lib.mb_conv1d_bwd_workspace(ctypes.byref(d)) >= 4 * 3584 * 5 * 4
+    d.width = 5
+    assert lib.mb_conv1d_bwd_workspace(ctypes.byref(d)) == -5
+    assert 0 < lib.mb_grad_norm_workspace(1) < lib.mb_grad_norm_workspace(1000)
+    e = lambda ws: lib.mb_embedding_bwd(9, 5, 8, 1, 0, 0, 1.0, P["tokens"], P["dy"], P["out"], ws, None)  # noqa: E731
+    assert e(P["x"] + 8) == -4 and e(P["out"] + 16) == -7 and e(P["tokens"]) == -7
+    p, s, t = _lists([A0], [16], [0])
+    for ws, code in ((P["x"] + 8, -4), (A0 + 16, -7), (P["norm"], -7)):
+        assert lib.mb_grad_norm(1, p, s, t, P["norm"], ws, None) == code
+        assert lib.mb_clip_grad_norm(1, p, None, s, t, 1.0, 0.0, P["norm"], ws, None) == code
+    o = (ctypes.c_void_p * 1)(2 * A0)
+    assert lib.mb_clip_grad_norm(1, p, o, s, t, 1.0, 0.0, P["norm"], 2 * A0 + 16, None) == -7
 
 
 @no_gpu_only
