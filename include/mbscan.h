@@ -471,13 +471,16 @@ int mb_clip_grad_norm(int64_t count, const void *const *grads, void *const *out,
  *                                              a row that is no distribution), 0 for i >= len; NULL means
  *                                              not written
  *   temperature   > 0, it and its inverse finite (MB_ERR_UNSUPPORTED otherwise)
- * Outputs must not overlap each other or the inputs.  vocab >= 1; batch, ndraft and
- * vocab below 2^31 - 1.  Probabilities are fp32.
+ *   workspace     as for mb_embedding_bwd, of mb_verify_sample_workspace(batch, ndraft, vocab) bytes
+ *                 (none up to a vocabulary of 1,024)
+ * Outputs must not overlap each other or the inputs.  vocab >= 1; batch and ndraft
+ * below 2^31 - 16, vocab below 2^31 - 8192.  Probabilities are fp32.
  */
 int mb_verify_sample(int64_t batch, int64_t ndraft, int64_t vocab, int32_t logit_dtype, float temperature,
                      const void *logits, const void *draft_logits, const int32_t *draft, const int32_t *lengths,
                      const float *uniform, const float *noise, int32_t *accepted, int32_t *last_pos,
-                     int32_t *next_token, float *probs, void *stream);
+                     int32_t *next_token, float *probs, void *workspace, void *stream);
+int64_t mb_verify_sample_workspace(int64_t batch, int64_t ndraft, int64_t vocab);
 
 /* Static, NUL-terminated description of a status code (never NULL). */
 const char *mb_status_string(int status);

@@ -81,11 +81,11 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.mb_grad_norm.argtypes = [i64] + [_VP] * 6
     lib.mb_clip_grad_norm.restype = ctypes.c_int
     lib.mb_clip_grad_norm.argtypes = [i64] + [_VP] * 4 + [f32] * 2 + [_VP] * 3
-    for size, args in ((lib.mb_embedding_bwd_workspace, [i64] * 3), (lib.mb_grad_norm_workspace, [i64]),
+    for size, args in ((lib.mb_embedding_bwd_workspace, [i64] * 3), (lib.mb_grad_norm_workspace, [i64]), (lib.mb_verify_sample_workspace, [i64] * 3),
                        (lib.mb_conv1d_bwd_workspace, [ctypes.POINTER(ConvDesc)])):
         size.restype, size.argtypes = i64, args
     lib.mb_verify_sample.restype = ctypes.c_int
-    lib.mb_verify_sample.argtypes = [i64] * 3 + [i32, f32] + [_VP] * 11
+    lib.mb_verify_sample.argtypes = [i64] * 3 + [i32, f32] + [_VP] * 12
     lib.mb_status_string.restype = ctypes.c_char_p
     lib.mb_status_string.argtypes = [ctypes.c_int]
     lib.mb_abi_version.restype = ctypes.c_int
@@ -681,9 +681,11 @@ def verify_sample(logits, draft, uniform, noise, draft_logits=None, *, lengths=N
         _need(lengths, "lengths", (nb,), torch.int32, dev)
     accepted, last_pos, next_token = (torch.empty(nb, dtype=torch.int32, device=dev) for _ in range(3))
     probs = torch.empty((nb, n), dtype=torch.float32, device=dev) if return_probs else None
+    size = lib.mb_verify_sample_workspace(nb, n, V)
+    ws = _workspace(size, "mb_verify_sample", dev) if size else None
     with _on_device(dev):
         st = lib.mb_verify_sample(nb, n, V, _dt(logits.dtype), float(temperature), _ptr(logits), _ptr(draft_logits),
                                   _ptr(draft), _ptr(lengths), _ptr(uniform), _ptr(noise), _ptr(accepted),
-                                  _ptr(last_pos), _ptr(next_token), _ptr(probs), _stream(dev))
+                                  _ptr(last_pos), _ptr(next_token), _ptr(probs), _ptr(ws), _stream(dev))
     _check(st, "mb_verify_sample")
     return (accepted, last_pos, next_token, probs) if return_probs else (accepted, last_pos, next_token)

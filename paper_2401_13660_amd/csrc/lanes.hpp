@@ -3,6 +3,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "device_math.hpp"
 
 namespace mbs {
@@ -115,10 +117,21 @@ __device__ __forceinline__ float lane_value(float v, int lane) {
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
 }
 
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-    return v;
+// f over the 64 lanes' values (of 32 bits), the same in every lane: pairs, quads and rows of 16 by lane permutations,
+// then the rows'.
+template <class T, class F> __device__ __forceinline__ T wave_all(T v, F f) {
+    auto moved = [&](auto ctrl) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, 0xf, 0xf, true));
+    };
+    v = f(v, moved(std::integral_constant<int, 0xB1>{}));    // lanes 1 0 3 2
+    v = f(v, moved(std::integral_constant<int, 0x4E>{}));    // lanes 2 3 0 1
+    v = f(v, moved(std::integral_constant<int, 0x141>{}));   // half rows mirrored
+    v = f(v, moved(std::integral_constant<int, 0x140>{}));   // rows mirrored
+    auto row = [&](int lane) { return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane)); };
+    return f(f(row(0), row(16)), f(row(32), row(48)));
 }
+__device__ __forceinline__ float wave_sum(float v) { return wave_all(v, [](float a, float b) { return a + b; }); }
+__device__ __forceinline__ float wave_max(float v) { return wave_all(v, [](float a, float b) { return __builtin_fmaxf(a, b); }); }
+__device__ __forceinline__ int32_t wave_min(int32_t v) { return wave_all(v, [](int32_t a, int32_t b) { return min(a, b); }); }
 
 }  // namespace mbs

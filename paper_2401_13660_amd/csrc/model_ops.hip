@@ -137,6 +137,54 @@ template <int OUT> hipError_t embed_bwd(mbs::embed::BwdParams &p, const EmbedPla
     return dy_dtype == MB_F32 ? embed_sum<0, OUT>(p, f, st) : embed_sum<1, OUT>(p, f, st);
 }
 
+// Row and token numbers, and a last piece's tokens past the vocabulary, stay below 2^31.
+bool sample_sizes(int64_t batch, int64_t ndraft, int64_t vocab) {
+    constexpr int64_t most = int64_t(1) << 31;
+    return batch < most && ndraft < most - mbs::sample::kMaxWaves && vocab < most - mbs::sample::kPiece;
+}
+
+// The pieces of a large vocabulary's rows; none for a small one's.
+struct SamplePlan {
+    int64_t pieces = 0, blocks = 0;
+    size_t stats = 0, best = 0, bytes = 0;
+    SamplePlan(int64_t batch, int64_t ndraft, int64_t vocab) {
+        namespace S = mbs::sample;
+        if (vocab <= S::kSmallVocab) return;
+        pieces = (vocab + S::kPiece - 1) / S::kPiece;
+        blocks = batch * (2 * ndraft + 1) * pieces;
+        Areas w;
+        stats = w.add((size_t)blocks * sizeof(float2));
+        best = w.add((size_t)(batch * pieces) * sizeof(S::Best));
+        bytes = w.bytes;
+    }
+};
+
+template <int DT> hipError_t sample_launch(mbs::sample::Params &p, const SamplePlan &f, void *workspace, hipStream_t st) {
+    namespace S = mbs::sample;
+    void *args[] = {&p};
+    if (f.pieces == 0) {
+        // a wave per row, the row after the drafts included
+        const int waves = (int)std::min<int64_t>(p.ndraft + 1, S::kMaxWaves);
+        const void *fn = p.vocab <= 256 ? reinterpret_cast<const void *>(&S::verify_small<DT, 4>)
+                                        : reinterpret_cast<const void *>(&S::verify_small<DT, 16>);
+        return hipLaunchKernel(fn, dim3((unsigned)p.batch), dim3(64 * waves), args, 0, st);
+    }
+    Workspace ws(workspace, f.bytes, st);
+    if (!ws.at) return hipErrorOutOfMemory;
+    p.pieces = (int32_t)f.pieces;
+    p.stats = reinterpret_cast<float2 *>(ws.at + f.stats);
+    p.best = reinterpret_cast<S::Best *>(ws.at + f.best);
+    // without the drafter's logits its rows' workgroups end at once
+    hipError_t e = hipLaunchKernel(reinterpret_cast<const void *>(&S::piece_stats<DT>), dim3((unsigned)f.blocks),
+                                   dim3(S::kThreads), args, 0, st);
+    if (e == hipSuccess)
+        e = hipLaunchKernel(reinterpret_cast<const void *>(&S::decide_and_race<DT>), dim3((unsigned)(p.batch * f.pieces)),
+                            dim3(S::kThreads), args, 0, st);
+    if (e == hipSuccess)
+        e = hipLaunchKernel(reinterpret_cast<const void *>(&S::join_races), dim3((unsigned)p.batch), dim3(64), args, 0, st);
+    return ws.done(e);
+}
+
 // The checks that both directions share; the element counts of the tokens' and the table's rows.
 int embed_checks(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_type, int32_t in_dtype, int32_t out_dtype,
                  int64_t *row_elems, int64_t *table_elems) {
@@ -462,9 +510,9 @@ int mb_clip_grad_norm(int64_t count, const void *const *grads, void *const *out,
 int mb_verify_sample(int64_t batch, int64_t ndraft, int64_t vocab, int32_t logit_dtype, float temperature,
                      const void *logits, const void *draft_logits, const int32_t *draft, const int32_t *lengths,
                      const float *uniform, const float *noise, int32_t *accepted, int32_t *last_pos,
-                     int32_t *next_token, float *probs, void *stream) {
+                     int32_t *next_token, float *probs, void *workspace, void *stream) {
     if (batch < 0 || ndraft < 0 || vocab < 1) return MB_ERR_SHAPE;
-    if (ndraft >= (int64_t(1) << 31) - 1 || vocab >= (int64_t(1) << 31) - 1 || batch >= (int64_t(1) << 31)) return MB_ERR_SHAPE;
+    if (!sample_sizes(batch, ndraft, vocab)) return MB_ERR_SHAPE;
     if (!valid_dtype(logit_dtype)) return MB_ERR_DTYPE;
     const float inv_temp = 1.0f / temperature;
     if (!(temperature > 0.0f) || std::isinf(temperature) || std::isinf(inv_temp)) return MB_ERR_UNSUPPORTED;
@@ -482,7 +530,10 @@ int mb_verify_sample(int64_t batch, int64_t ndraft, int64_t vocab, int32_t logit
     const size_t b_b = (size_t)batch * 4, p_b = (size_t)pairs * 4;
     const Range ins[] = {{logits, (size_t)elems * lsz}, {draft_logits, (size_t)(pairs * vocab) * lsz}, {draft, p_b},
                          {lengths, b_b}, {uniform, p_b}, {noise, (size_t)noises * 4}};
-    const Range outs[] = {{accepted, b_b}, {last_pos, b_b}, {next_token, b_b}, {probs, p_b}};
+    const SamplePlan f(batch, ndraft, vocab);
+    if (f.blocks >= (int64_t(1) << 31)) return MB_ERR_SHAPE;
+    if (!aligned(workspace, 16)) return MB_ERR_ALIGN;
+    const Range outs[] = {{accepted, b_b}, {last_pos, b_b}, {next_token, b_b}, {probs, p_b}, {workspace, f.bytes}};
     if (any_overlap(outs, ins)) return MB_ERR_ALIAS;
     mbs::sample::Params p{};
     p.batch = batch; p.ndraft = ndraft; p.vocab = vocab;
@@ -490,9 +541,16 @@ int mb_verify_sample(int64_t batch, int64_t ndraft, int64_t vocab, int32_t logit
     p.uniform = uniform; p.noise = noise;
     p.accepted = accepted; p.last_pos = last_pos; p.next_token = next_token; p.probs = probs;
     p.inv_temp = inv_temp;
-    const void *fn = logit_dtype == MB_F32 ? reinterpret_cast<const void *>(&mbs::sample::verify_sample<0>)
-                                           : reinterpret_cast<const void *>(&mbs::sample::verify_sample<1>);
-    return status(launch(fn, dim3((unsigned)batch), dim3(64), &p, stream));
+    return status(logit_dtype == MB_F32 ? sample_launch<0>(p, f, workspace, st_of(stream))
+                                        : sample_launch<1>(p, f, workspace, st_of(stream)));
+}
+
+int64_t mb_verify_sample_workspace(int64_t batch, int64_t ndraft, int64_t vocab) {
+    int64_t rows, elems;
+    if (batch < 0 || ndraft < 0 || vocab < 1 || !sample_sizes(batch, ndraft, vocab) ||
+        !mul_ok(batch, ndraft + 1, &rows) || !mul_ok(rows, vocab, &elems))
+        return MB_ERR_SHAPE;
+    return (int64_t)SamplePlan(batch, ndraft, vocab).bytes;
 }
 
 }  // extern "C"

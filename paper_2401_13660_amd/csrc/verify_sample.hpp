@@ -16,14 +16,31 @@
 // exp((l - max) / T): the maximum is taken from the logits themselves, so that rows of the type's
 // lowest values stay distributions.  A row that is none (a NaN or +infinity in it, or nothing above
 // -infinity) accepts nothing, and no token follows it (-1).
+//
+// Up to kSmallVocab tokens (bytes): one workgroup per sequence, one wave per row, the row in
+// registers from one load to the token drawn; the wave whose row stops the sequence draws, and the
+// rows after it are only looked at where their probabilities are wanted.  Larger vocabularies: the
+// rows are cut into pieces of kPiece tokens whose maxima and sums one launch finds; a second one
+// joins them, decides, and races within each piece of the row that stops the sequence; a third one
+// joins the pieces' winners.
 #pragma once
 
 #include <hip/hip_runtime.h>
 
 #include "device_math.hpp"
+#include "lanes.hpp"
 
 namespace mbs {
 namespace sample {
+
+constexpr int kSmallVocab = 1024;
+constexpr int kMaxWaves = 16;
+constexpr int kThreads = 256;      // of a piece
+constexpr int kPieceSpans = 8;     // spans of 4 per thread
+constexpr int kPiece = kThreads * kPieceSpans * 4;
+constexpr int32_t kNobody = 0x7fffffff;
+
+struct Best { float left, whole; int32_t left_at, whole_at; };
 
 struct Params {
     int64_t batch, ndraft, vocab;
@@ -38,113 +55,346 @@ struct Params {
     int32_t *next_token;          // (batch)
     float *probs;                 // (batch, ndraft) or null: the target's of the drafted tokens
     float inv_temp;
+    int32_t pieces;               // per row, of a large vocabulary
+    float2 *stats;                // (batch, 2 ndraft + 1, pieces): maximum and sum; the target's rows, then the drafter's
+    Best *best;                   // (batch, pieces)
 };
 
-// A row's softmax: e^((l - max) / T) times inv is a probability; ok: the row is a distribution.
-struct Row {
-    float max, inv;
-    bool ok;
-    // Rounded before anything is taken from it: fused into p - q it would leave the rounding of q where p equals q.
-    __device__ __forceinline__ float prob(float l, float inv_temp) const {
-#pragma clang fp contract(off)
-        return expf((l - max) * inv_temp) * inv;
-    }
-};
-
-// Maxima and sums of pieces of a row.  A piece with nothing above -infinity adds nothing.
-struct Piece {
-    float max = -__builtin_inff(), sum = 0.0f;
-    __device__ __forceinline__ void add(float l, float inv_temp) { join(Piece{l, l == -__builtin_inff() ? 0.0f : 1.0f}, inv_temp); }
-    __device__ __forceinline__ void join(Piece o, float inv_temp) {
-        const float m = __builtin_fmaxf(max, o.max);
-        // a piece without a sum stays out; infinities and NaN make a NaN of the sum
-        float s = 0.0f;
-        if (sum != 0.0f) s += sum * expf((max - m) * inv_temp);
-        if (o.sum != 0.0f) s += o.sum * expf((o.max - m) * inv_temp);
-        max = m;
-        sum = s;
-    }
-    __device__ __forceinline__ Row row() const {
-        const bool ok = sum > 0.0f && sum < __builtin_inff();
-        return Row{max, 1.0f / sum, ok};
-    }
-};
-
-template <int DT> __device__ Row row_of(const void *base, int64_t at, int64_t vocab, float inv_temp) {
-    Piece a;
-    for (int64_t y = threadIdx.x & 63; y < vocab; y += 64) a.add(Act<DT>::ld(base, at + y), inv_temp);
-    for (int off = 32; off > 0; off >>= 1) {
-        Piece o;
-        o.max = __shfl_xor(a.max, off, 64);
-        o.sum = __shfl_xor(a.sum, off, 64);
-        a.join(o, inv_temp);
-    }
-    return a.row();
+__device__ __forceinline__ int64_t length_of(const Params &p, int64_t b) {
+    const int64_t len = p.lengths ? p.lengths[b] : p.ndraft;
+    return len < 0 ? 0 : len > p.ndraft ? p.ndraft : len;
 }
 
-// One wave per sequence, row after row.
+// e^((l - max) / T).  expf's own error is an ulp or so; a plain 2^x of the scaled argument would add the rounding of
+// that argument, up to 40 ulp for the logits met here.
+__device__ __forceinline__ float weight(float l, float max, float inv_temp) { return expf((l - max) * inv_temp); }
+
+// Probabilities are rounded before anything is taken from them: fused into p - q the product would leave the rounding
+// of q where p equals q.
+__device__ __forceinline__ float rounded_product(float a, float b) {
+#pragma clang fp contract(off)
+    return a * b;
+}
+
+// A row's softmax.  ok: the row is a distribution.  The sum is 0 where nothing is above -infinity, and NaN with a NaN
+// or +infinity in the row.
+struct Row {
+    float max = 0.0f, inv = 0.0f;
+    bool ok = false;
+    __device__ __forceinline__ void set(float m, float sum) {
+        max = m;
+        inv = 1.0f / sum;
+        ok = sum > 0.0f && sum < __builtin_inff();
+    }
+    __device__ __forceinline__ float prob(float l, float inv_temp) const {
+        return rounded_product(weight(l, max, inv_temp), inv);
+    }
+};
+
+// The candidate with the largest score, the lowest of them; scores are above 0.
+struct Race {
+    float score = 0.0f;
+    int32_t at = kNobody;
+    __device__ __forceinline__ void run(float r, float noise, int32_t y) {
+        const float s = r / noise;
+        if (r > 0.0f && s > score) {
+            score = s;
+            at = y;
+        }
+    }
+    __device__ __forceinline__ void join(float s, int32_t y) {
+        if (y != kNobody && (s > score || (s == score && y < at))) {
+            score = s;
+            at = y;
+        }
+    }
+    __device__ __forceinline__ void join_wave() {
+        const float s = wave_max(score);
+        at = wave_min(score == s ? at : kNobody);
+        score = s;
+    }
+};
+
+__device__ __forceinline__ void write_outcome(const Params &p, int64_t b, int64_t c) {
+    p.accepted[b] = (int32_t)c;
+    if (p.last_pos) p.last_pos[b] = (int32_t)c - 1;
+}
+
+// ---- small vocabularies ---------------------------------------------------------
+
+// A row in a wave's registers: lane l holds tokens 256 j + 4 l + i.
+template <int DT, int KPL> struct RowInLanes {
+    Span<DT, 4> s[KPL / 4];
+    float v[KPL];                                       // logits, then weights
+    Row row;
+    __device__ __forceinline__ void load(const void *base, int64_t at, int vocab, int lane) {
+#pragma unroll
+        for (int j = 0; j < KPL / 4; ++j) {
+            const int y = 256 * j + 4 * lane;
+            if (y + 4 <= vocab) s[j].load(base, at + y);
+            else s[j].load_first(base, at + y, max(vocab - y, 0));
+        }
+    }
+    __device__ __forceinline__ void softmax(int vocab, int lane, float inv_temp) {
+        float m = -__builtin_inff();
+#pragma unroll
+        for (int k = 0; k < KPL; ++k) {
+            v[k] = 256 * (k / 4) + 4 * lane + k % 4 < vocab ? s[k / 4].get(k % 4) : -__builtin_inff();
+            m = __builtin_fmaxf(m, v[k]);
+        }
+        m = wave_max(m);
+        // nothing above -infinity: weights of 0, not of NaN
+        const float at = m == -__builtin_inff() ? 0.0f : m;
+        float sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < KPL; ++k) {
+            v[k] = weight(v[k], at, inv_temp);
+            sum += v[k];
+        }
+        row.set(m, wave_sum(sum));
+    }
+    __device__ __forceinline__ float prob(int k) const { return rounded_product(v[k], row.inv); }
+    // of one token, the same in every lane
+    __device__ __forceinline__ float prob_of(int x) const {
+        float r = 0.0f;
+#pragma unroll
+        for (int k = 0; k < KPL; ++k) r = 256 * (k / 4) + k % 4 == (x & ~255) + x % 4 ? prob(k) : r;
+        return lane_value(r, (x & 255) >> 2);
+    }
+};
+
+template <int DT, int KPL>
+__global__ __launch_bounds__(64 * kMaxWaves) void verify_small(Params p) {
+    __shared__ int stop;
+    const int64_t b = blockIdx.x, n = p.ndraft;
+    const int V = (int)p.vocab, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int len = (int)length_of(p, b);
+    if (threadIdx.x == 0) stop = kNobody;
+    if (p.probs)
+        for (int64_t i = len + (int64_t)threadIdx.x; i < n; i += blockDim.x) p.probs[b * n + i] = 0.0f;
+    RowInLanes<0, KPL> noise;
+    noise.load(p.noise, b * V, V, lane);
+    __syncthreads();
+    int c = kNobody;                                    // the row that stops the sequence, once it is known
+    for (int base = 0; base <= len; base += waves) {
+        const int i = base + wave;
+        const bool open = c == kNobody, here = i < len || (i == len && open);
+        const bool have_q = open && i < len && p.draft_logits;
+        RowInLanes<DT, KPL> t, q;
+        int x = -1;
+        if (here) {
+            t.load(p.logits, (b * (n + 1) + i) * V, V, lane);
+            if (have_q) q.load(p.draft_logits, (b * n + i) * V, V, lane);
+            bool passes = false;
+            if (i < len) {
+                x = __builtin_amdgcn_readfirstlane(p.draft[b * n + i]);
+                const float u = p.uniform[b * n + i];
+                t.softmax(V, lane, p.inv_temp);
+                const bool valid = x >= 0 && x < V && t.row.ok;
+                const float px = valid ? t.prob_of(x) : 0.0f;
+                float qx = 1.0f;
+                if (have_q) q.softmax(V, lane, p.inv_temp);
+                if (have_q && valid) qx = q.prob_of(x);
+                passes = valid && (!have_q || q.row.ok) && u * qx < px;
+                if (p.probs && lane == 0) p.probs[b * n + i] = px;
+            } else {
+                t.softmax(V, lane, p.inv_temp);
+            }
+            if (open && !passes && lane == 0) atomicMin(&stop, i);
+        }
+        __syncthreads();
+        c = stop;
+        if (open && here && i == c) {
+            Race race;
+            if (t.row.ok) {
+                const bool less_q = have_q && q.row.ok;
+#pragma unroll
+                for (int k = 0; k < KPL; ++k) {
+                    const int y = 256 * (k / 4) + 4 * lane + k % 4;
+                    float left = t.prob(k);
+                    if (less_q) left -= q.prob(k);
+                    else if (!have_q && y == x) left = 0.0f;
+                    race.run(y < V ? left : 0.0f, noise.s[k / 4].get(k % 4), y);
+                }
+                race.join_wave();
+                if (race.at == kNobody) {
+#pragma unroll
+                    for (int k = 0; k < KPL; ++k) {
+                        const int y = 256 * (k / 4) + 4 * lane + k % 4;
+                        race.run(y < V ? t.prob(k) : 0.0f, noise.s[k / 4].get(k % 4), y);
+                    }
+                    race.join_wave();
+                }
+            }
+            if (lane == 0) {
+                write_outcome(p, b, c);
+                p.next_token[b] = race.at == kNobody ? -1 : race.at;
+            }
+        }
+        if (c != kNobody && !p.probs) break;
+        __syncthreads();                                // every wave has read it before a later row may set it
+    }
+}
+
+// ---- large vocabularies -----------------------------------------------------------
+
+// A thread's share of a piece: spans of 4, 256 threads side by side.
+template <int DT> struct PieceInLanes {
+    Span<DT, 4> s[kPieceSpans];
+    __device__ __forceinline__ static int token(int piece, int k) {
+        return piece * kPiece + (k * kThreads + (int)threadIdx.x) * 4;
+    }
+    __device__ __forceinline__ void load(const void *base, int64_t at, int piece, int64_t vocab) {
+#pragma unroll
+        for (int k = 0; k < kPieceSpans; ++k) {
+            const int64_t y = token(piece, k);
+            if (y + 4 <= vocab) s[k].load(base, at + y);
+            else s[k].load_first(base, at + y, (int)max(vocab - y, (int64_t)0));
+        }
+    }
+    __device__ __forceinline__ float get(int piece, int k, int i, int64_t vocab) const {
+        return token(piece, k) + i < vocab ? s[k].get(i) : -__builtin_inff();
+    }
+};
+
+__device__ __forceinline__ float block_all(float v, float *red, bool sum) {
+    v = sum ? wave_sum(v) : wave_max(v);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return sum ? (red[0] + red[1]) + (red[2] + red[3])
+               : __builtin_fmaxf(__builtin_fmaxf(red[0], red[1]), __builtin_fmaxf(red[2], red[3]));
+}
+
 template <int DT>
-__global__ __launch_bounds__(64) void verify_sample(Params p) {
-    const int64_t b = blockIdx.x, V = p.vocab, n = p.ndraft;
-    const int lane = threadIdx.x;
-    int64_t len = p.lengths ? p.lengths[b] : n;
-    len = len < 0 ? 0 : len > n ? n : len;
-    int64_t c = -1;
-    for (int64_t i = 0; i < n; ++i) {
-        if (i >= len || (c >= 0 && !p.probs)) {
-            if (p.probs && lane == 0) p.probs[b * n + i] = 0.0f;
-            continue;
-        }
-        const int64_t at = (b * (n + 1) + i) * V, qat = (b * n + i) * V;
-        const int64_t x = p.draft[b * n + i];
-        const bool in_range = x >= 0 && x < V;
-        const Row t = row_of<DT>(p.logits, at, V, p.inv_temp);
-        const float px = in_range && t.ok ? t.prob(Act<DT>::ld(p.logits, at + x), p.inv_temp) : 0.0f;
-        float qx = 1.0f;
-        bool ok = in_range && t.ok;
-        if (p.draft_logits) {
-            const Row q = row_of<DT>(p.draft_logits, qat, V, p.inv_temp);
-            ok = ok && q.ok;
-            if (ok) qx = q.prob(Act<DT>::ld(p.draft_logits, qat + x), p.inv_temp);
-        }
-        if (lane == 0 && p.probs) p.probs[b * n + i] = px;
-        if (c < 0 && !(ok && p.uniform[b * n + i] * qx < px)) c = i;
+__global__ __launch_bounds__(kThreads) void piece_stats(Params p) {
+    __shared__ float red[kThreads / 64];
+    const int64_t rows = 2 * p.ndraft + 1, row = blockIdx.x / p.pieces, b = row / rows, i = row - b * rows;
+    const int piece = (int)(blockIdx.x - row * p.pieces);
+    const bool target = i <= p.ndraft;
+    const int64_t at = target ? i : i - (p.ndraft + 1), len = length_of(p, b);
+    if (target ? at > len : at >= len || !p.draft_logits) return;
+    PieceInLanes<DT> v;
+    v.load(target ? p.logits : p.draft_logits, (target ? b * (p.ndraft + 1) + at : b * p.ndraft + at) * p.vocab, piece, p.vocab);
+    float m = -__builtin_inff();
+#pragma unroll
+    for (int k = 0; k < kPieceSpans; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) m = __builtin_fmaxf(m, v.get(piece, k, j, p.vocab));
+    m = block_all(m, red, false);
+    const float from = m == -__builtin_inff() ? 0.0f : m;
+    float sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kPieceSpans; ++k) {
+        float part = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) part += weight(v.get(piece, k, j, p.vocab), from, p.inv_temp);
+        sum += part;
     }
-    if (c < 0) c = len;
-    const int64_t at = (b * (n + 1) + c) * V, qat = (b * n + c) * V;
-    const Row t = row_of<DT>(p.logits, at, V, p.inv_temp);
-    Row q{0.0f, 0.0f, false};
-    int64_t x = -1;
-    if (c < len) {
-        x = p.draft[b * n + c];
-        if (p.draft_logits) q = row_of<DT>(p.draft_logits, qat, V, p.inv_temp);
-    }
-    // the best of what is left of p, and of p itself
-    float best = 0.0f, best_p = 0.0f;
-    int64_t who = -1, who_p = -1;
-    if (t.ok)
-        for (int64_t y = lane; y < V; y += 64) {
-            const float pr = t.prob(Act<DT>::ld(p.logits, at + y), p.inv_temp), e = p.noise[b * V + y];
-            float left = pr;
-            if (c < len && p.draft_logits) left = q.ok ? pr - q.prob(Act<DT>::ld(p.draft_logits, qat + y), p.inv_temp) : pr;
-            else if (y == x) left = 0.0f;
-            if (left > 0.0f && left / e > best) { best = left / e; who = y; }
-            if (pr / e > best_p) { best_p = pr / e; who_p = y; }
+    sum = block_all(sum, red, true);
+    if (threadIdx.x == 0) p.stats[row * p.pieces + piece] = make_float2(m, sum);
+}
+
+// Row i of a sequence (the target's first, then the drafter's) from its pieces.
+__device__ __forceinline__ Row join_row(const Params &p, int64_t b, int64_t i) {
+    const float2 *s = p.stats + (b * (2 * p.ndraft + 1) + i) * p.pieces;
+    float m = -__builtin_inff(), sum = 0.0f;
+    for (int k = 0; k < p.pieces; ++k) m = __builtin_fmaxf(m, s[k].x);
+    // a piece with nothing above -infinity adds nothing; one that holds a NaN or +infinity adds NaN
+    for (int k = 0; k < p.pieces; ++k) sum += s[k].y == 0.0f ? 0.0f : rounded_product(s[k].y, weight(s[k].x, m, p.inv_temp));
+    Row r;
+    r.set(m, sum);
+    return r;
+}
+
+template <int DT>
+__global__ __launch_bounds__(kThreads) void decide_and_race(Params p) {
+    __shared__ int stop;
+    __shared__ float scores[2][kThreads / 64];
+    __shared__ int32_t who[2][kThreads / 64];
+    const int64_t b = blockIdx.x / p.pieces, n = p.ndraft, V = p.vocab;
+    const int piece = (int)(blockIdx.x - b * p.pieces);
+    const int len = (int)length_of(p, b);
+    if (threadIdx.x == 0) stop = len;
+    __syncthreads();
+    const bool probs = p.probs && piece == 0;
+    for (int64_t i = threadIdx.x; i < (probs ? n : (int64_t)len); i += kThreads) {
+        float px = 0.0f;
+        if (i < len) {
+            const int64_t x = p.draft[b * n + i];
+            const Row t = join_row(p, b, i);
+            const bool valid = x >= 0 && x < V && t.ok;
+            if (valid) px = t.prob(Act<DT>::ld(p.logits, (b * (n + 1) + i) * V + x), p.inv_temp);
+            float qx = 1.0f;
+            bool ok = valid;
+            if (p.draft_logits) {
+                const Row q = join_row(p, b, n + 1 + i);
+                ok = valid && q.ok;
+                if (ok) qx = q.prob(Act<DT>::ld(p.draft_logits, (b * n + i) * V + x), p.inv_temp);
+            }
+            if (!(ok && p.uniform[b * n + i] * qx < px)) atomicMin(&stop, (int)i);
         }
-    auto reduce = [](float &v, int64_t &w) {
-        for (int off = 32; off > 0; off >>= 1) {
-            const float ov = __shfl_xor(v, off, 64);
-            const int64_t ow = __shfl_xor(w, off, 64);
-            if (ow >= 0 && (w < 0 || ov > v || (ov == v && ow < w))) { v = ov; w = ow; }
-        }
-    };
-    reduce(best, who);
-    reduce(best_p, who_p);
-    if (lane == 0) {
-        p.accepted[b] = (int32_t)c;
-        if (p.last_pos) p.last_pos[b] = (int32_t)c - 1;
-        p.next_token[b] = (int32_t)(who >= 0 ? who : who_p);
+        if (probs) p.probs[b * n + i] = px;
     }
+    __syncthreads();
+    const int c = stop;
+    if (piece == 0 && threadIdx.x == 0) write_outcome(p, b, c);
+
+    const Row t = join_row(p, b, c);
+    Race left, whole;
+    if (t.ok) {
+        const bool have_q = c < len && p.draft_logits;
+        Row q;
+        if (have_q) q = join_row(p, b, n + 1 + c);
+        const bool less_q = have_q && q.ok;
+        const int64_t x = c < len && !p.draft_logits ? p.draft[b * n + c] : -1;
+        PieceInLanes<DT> tl, ql;
+        PieceInLanes<0> e;
+        tl.load(p.logits, (b * (n + 1) + c) * V, piece, V);
+        if (less_q) ql.load(p.draft_logits, (b * n + c) * V, piece, V);
+        e.load(p.noise, b * V, piece, V);
+#pragma unroll
+        for (int k = 0; k < kPieceSpans; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int y = PieceInLanes<DT>::token(piece, k) + j;
+                if (y >= V) continue;
+                const float pr = t.prob(tl.s[k].get(j), p.inv_temp), noise = e.s[k].get(j);
+                whole.run(pr, noise, y);
+                left.run(less_q ? pr - q.prob(ql.s[k].get(j), p.inv_temp) : y == x ? 0.0f : pr, noise, y);
+            }
+    }
+    left.join_wave();
+    whole.join_wave();
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) {
+        scores[0][wave] = left.score;
+        scores[1][wave] = whole.score;
+        who[0][wave] = left.at;
+        who[1][wave] = whole.at;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kThreads / 64; ++w) {
+            left.join(scores[0][w], who[0][w]);
+            whole.join(scores[1][w], who[1][w]);
+        }
+        p.best[b * p.pieces + piece] = Best{left.score, whole.score, left.at, whole.at};
+    }
+}
+
+__global__ __launch_bounds__(64) void join_races(Params p) {
+    const int64_t b = blockIdx.x;
+    Race left, whole;
+    for (int k = threadIdx.x; k < p.pieces; k += 64) {
+        const Best o = p.best[b * p.pieces + k];
+        left.join(o.left, o.left_at);
+        whole.join(o.whole, o.whole_at);
+    }
+    left.join_wave();
+    whole.join_wave();
+    if (threadIdx.x == 0) p.next_token[b] = left.at != kNobody ? left.at : whole.at != kNobody ? whole.at : -1;
 }
 
 }  // namespace sample

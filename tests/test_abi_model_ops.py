@@ -127,6 +127,8 @@ def test_workspaces():
     assert lib.mb_conv1d_bwd_workspace(ctypes.byref(d)) >= 4 * 3584 * 5 * 4
     d.width = 5
     assert lib.mb_conv1d_bwd_workspace(ctypes.byref(d)) == -5
+    assert lib.mb_verify_sample_workspace(2, 3, 1024) == 0 < lib.mb_verify_sample_workspace(2, 3, 1025)
+    assert lib.mb_verify_sample_workspace(2, 3, 0) == -2 and lib.mb_verify_sample_workspace(1 << 31, 3, 5) == -2
     assert 0 < lib.mb_grad_norm_workspace(1) < lib.mb_grad_norm_workspace(1000)
     e = lambda ws: lib.mb_embedding_bwd(9, 5, 8, 1, 0, 0, 1.0, P["tokens"], P["dy"], P["out"], ws, None)  # noqa: E731
     assert e(P["x"] + 8) == -4 and e(P["out"] + 16) == -7 and e(P["tokens"]) == -7
@@ -149,13 +151,14 @@ def test_workspaces():
     (dict(probs=P["probs"] + 1), -4),
     (dict(accepted=P["draft"]), -7), (dict(next=P["accepted"]), -7), (dict(probs=P["uniform"] + 4), -7),
     (dict(last=P["noise"]), -7), (dict(next=P["logits"] + 64), -7),
+    (dict(ws=P["x"] + 8, V=2000), -4), (dict(ws=P["noise"], V=2000), -7), (dict(ws=P["next"], V=2000), -7),
 ])
 def test_verify_sample_rejects(over, code):
     v = dict(P, b=2, n=3, V=256, dt=1, T=1.0)
     v.update(over)
     assert mb.load_library().mb_verify_sample(
         v["b"], v["n"], v["V"], v["dt"], v["T"], v["logits"], v["dlogits"], v["draft"], v["lengths"], v["uniform"],
-        v["noise"], v["accepted"], v["last"], v["next"], v["probs"], None) == code
+        v["noise"], v["accepted"], v["last"], v["next"], v["probs"], v.get("ws"), None) == code
 
 
 def test_binding_refuses_cpu_tensors_and_wrong_arguments():
