@@ -114,7 +114,11 @@ def _load_fast(lib):
         return None
     at = [ctypes.cast(fn, _VP).value for fn in (lib.mb_scan_fwd, lib.mb_scan_fwd_states, lib.mb_scan_fwd_ckpt,
                                                 lib.mb_scan_step, lib.mb_conv1d_fwd, lib.mb_conv1d_step,
-                                                lib.mb_verify_rank)]
+                                                lib.mb_verify_rank, lib.mb_embedding_fwd, lib.mb_embedding_bwd,
+                                                lib.mb_embedding_bwd_workspace, lib.mb_conv1d_bwd,
+                                                lib.mb_conv1d_bwd_workspace, lib.mb_grad_norm,
+                                                lib.mb_grad_norm_workspace, lib.mb_clip_grad_norm,
+                                                lib.mb_verify_sample, lib.mb_verify_sample_workspace)]
     _fastcall.setup(*at, _cur_device, _raw_stream, torch.nn.Parameter)
     return _fastcall
 
@@ -527,6 +531,10 @@ def embedding_fwd(tokens, weight, *, scale=1.0, out_dtype=None, out=None):
     Returns tokens.shape + (dim,) in ``out_dtype`` (weight's by default).  A negative token (padding) gives
     zeros, a token >= vocab NaN."""
     lib = load_library()
+    if _fast is not None:
+        res = _fast.embedding_fwd(tokens, weight, scale, out_dtype, out)
+        if res is not None:
+            return _done(res, "mb_embedding_fwd")
     if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
         raise MBScanError("weight must be a (vocab, dim) tensor")
     V, d = weight.shape
@@ -549,6 +557,10 @@ def embedding_bwd(tokens, dy, vocab, *, scale=1.0, out_dtype=torch.float32, out=
     """The gradient of embedding_fwd's table: (vocab, dim) in ``out_dtype``, row v the sum of scale * dy over
     the tokens equal to v (the same bits on every call).  dy: tokens.shape + (dim,), fp32 or bf16."""
     lib = load_library()
+    if _fast is not None:
+        res = _fast.embedding_bwd(tokens, dy, vocab, scale, out_dtype, out)
+        if res is not None:
+            return _done(res, "mb_embedding_bwd")
     if not isinstance(dy, torch.Tensor) or dy.dim() < 1:
         raise MBScanError("dy must be a tensor of the tokens' shape and a last dimension dim")
     dev, d = dy.device, dy.shape[-1]
@@ -576,6 +588,10 @@ def conv1d_bwd(x, w, dy, bias=None, state=None, dstate_out=None, *, apply_silu=T
     (batch, dim, k-1) fp32 or None.  Returns a dict: dx (dy's dtype), dw (dim, k), dbias (dim,) or None,
     and dstate (batch, dim, k-1), fp32 but the first."""
     lib = load_library()
+    if _fast is not None:
+        res = _fast.conv1d_bwd(x, w, dy, bias, state, dstate_out, apply_silu)
+        if res is not None:
+            return dict(zip(("dx", "dw", "dbias", "dstate"), _done(res, "mb_conv1d_bwd")))
     if not isinstance(x, torch.Tensor) or x.dim() != 3:
         raise MBScanError("x must be a (batch, dim, L) tensor")
     nb, dim, L = x.shape
@@ -606,9 +622,7 @@ def conv1d_bwd(x, w, dy, bias=None, state=None, dstate_out=None, *, apply_silu=T
 
 def _grad_list(grads):
     """The tensors of a list, one GPU's and dense: their device, and host arrays of addresses, sizes and types."""
-    if isinstance(grads, torch.Tensor):
-        grads = [grads]
-    grads = list(grads)
+    grads = [grads] if isinstance(grads, torch.Tensor) else list(grads)
     if not grads:
         raise MBScanError("the list of tensors is empty")
     dev = grads[0].device if isinstance(grads[0], torch.Tensor) else None
@@ -624,6 +638,10 @@ def _grad_list(grads):
 def grad_norm(grads):
     """The 2-norm of all elements of a list of fp32 and bf16 tensors: a 0-dimensional fp32 tensor on their GPU."""
     lib = load_library()
+    if _fast is not None:
+        res = _fast.grad_norm(grads)
+        if res is not None:
+            return _done(res, "mb_grad_norm")
     grads, dev, ptrs, sizes, types = _grad_list(grads)
     norm = torch.empty((), dtype=torch.float32, device=dev)
     ws = _workspace(lib.mb_grad_norm_workspace(len(grads)), "mb_grad_norm", dev)
@@ -638,6 +656,10 @@ def clip_grad_norm(grads, max_norm, *, eps=1e-6, out=None):
     into ``out`` (tensors of the same shapes and types).  Returns the norm before clipping, a 0-dimensional
     fp32 tensor on the GPU."""
     lib = load_library()
+    if _fast is not None:
+        res = _fast.clip_grad_norm(grads, max_norm, eps, out)
+        if res is not None:
+            return _done(res, "mb_clip_grad_norm")
     grads, dev, ptrs, sizes, types = _grad_list(grads)
     optrs = None
     if out is not None:
@@ -667,6 +689,10 @@ def verify_sample(logits, draft, uniform, noise, draft_logits=None, *, lengths=N
     Returns (accepted, last_pos, next_token), each int32 (batch,), and with ``return_probs`` the target's
     probabilities of the drafted tokens, fp32 (batch, ndraft).  With ndraft = 0 it samples the next token."""
     lib = load_library()
+    if _fast is not None:
+        res = _fast.verify_sample(logits, draft, uniform, noise, draft_logits, lengths, temperature, return_probs)
+        if res is not None:
+            return _done(res, "mb_verify_sample")
     if not isinstance(logits, torch.Tensor) or logits.dim() != 3 or logits.shape[1] < 1:
         raise MBScanError("logits must be a (batch, ndraft + 1, vocab) tensor")
     nb, n, V = logits.shape[0], logits.shape[1] - 1, logits.shape[2]

@@ -20,6 +20,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <initializer_list>
+#include <vector>
 
 #include "mbscan.h"
 
@@ -32,6 +33,16 @@ decltype(&mb_scan_step) scan_step_fn;
 decltype(&mb_conv1d_fwd) conv1d_fwd_fn;
 decltype(&mb_conv1d_step) conv1d_step_fn;
 decltype(&mb_verify_rank) verify_rank_fn;
+decltype(&mb_embedding_fwd) embedding_fwd_fn;
+decltype(&mb_embedding_bwd) embedding_bwd_fn;
+decltype(&mb_embedding_bwd_workspace) embedding_bwd_workspace_fn;
+decltype(&mb_conv1d_bwd) conv1d_bwd_fn;
+decltype(&mb_conv1d_bwd_workspace) conv1d_bwd_workspace_fn;
+decltype(&mb_grad_norm) grad_norm_fn;
+decltype(&mb_grad_norm_workspace) grad_norm_workspace_fn;
+decltype(&mb_clip_grad_norm) clip_grad_norm_fn;
+decltype(&mb_verify_sample) verify_sample_fn;
+decltype(&mb_verify_sample_workspace) verify_sample_workspace_fn;
 PyObject *current_device, *raw_stream, *parameter_type;   // torch's accessors and nn.Parameter
 
 // A plain dense tensor on the GPU (no subclass, no transform's wrapper), or null.
@@ -69,9 +80,9 @@ struct Call {
         return t;
     }
     // A required tensor of this shape and type; its data.
-    void *need(PyObject *o, std::initializer_list<int64_t> shape, at::ScalarType type) {
+    void *need(PyObject *o, at::IntArrayRef shape, at::ScalarType type) {
         const at::Tensor *t = ok ? plain(o) : nullptr;
-        if (!t || t->scalar_type() != type || t->device() != dev || t->sizes() != at::IntArrayRef(shape) ||
+        if (!t || t->scalar_type() != type || t->device() != dev || t->sizes() != shape ||
             !t->is_contiguous()) {
             ok = false;
             return nullptr;
@@ -79,12 +90,12 @@ struct Call {
         return t->data_ptr();
     }
     // The same, or None: null.
-    void *maybe(PyObject *o, std::initializer_list<int64_t> shape, at::ScalarType type) {
+    void *maybe(PyObject *o, at::IntArrayRef shape, at::ScalarType type) {
         return o == Py_None ? nullptr : need(o, shape, type);
     }
     static bool act(at::ScalarType t) { return t == at::kFloat || t == at::kBFloat16; }
     // An output given by the caller (any activation type), or its type when it is None.
-    void *given(PyObject *o, std::initializer_list<int64_t> shape, at::ScalarType &type) {
+    void *given(PyObject *o, at::IntArrayRef shape, at::ScalarType &type) {
         if (o == Py_None) return nullptr;
         const at::Tensor *t = ok ? plain(o) : nullptr;
         if (!t || !act(t->scalar_type())) { ok = false; return nullptr; }
@@ -95,9 +106,11 @@ struct Call {
         if (!THPDtype_Check(o) || !act(reinterpret_cast<THPDtype *>(o)->scalar_type)) ok = false;
         else type = reinterpret_cast<THPDtype *>(o)->scalar_type;
     }
-    at::Tensor fresh(std::initializer_list<int64_t> shape, at::ScalarType type) const {
-        return at::empty(at::IntArrayRef(shape), at::TensorOptions().dtype(type).device(dev));
+    at::Tensor fresh(at::IntArrayRef shape, at::ScalarType type) const {
+        return at::empty(shape, at::TensorOptions().dtype(type).device(dev));
     }
+    // A call's workspace of this size (a negative status: the call itself will refuse, and needs none).
+    at::Tensor workspace(int64_t size) const { return size > 0 ? fresh({size}, at::kByte) : at::Tensor(); }
 };
 
 int32_t code(at::ScalarType t) { return t == at::kBFloat16 ? MB_BF16 : MB_F32; }
@@ -324,30 +337,263 @@ PyObject *verify_rank(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
     });
 }
 
+void *data(const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
+
+// A real number as a float; ok becomes false where it is none.
+float real(PyObject *o, bool &ok) {
+    const double v = PyFloat_CheckExact(o) ? PyFloat_AS_DOUBLE(o) : PyLong_CheckExact(o) ? PyLong_AsDouble(o) : (ok = false, 0.0);
+    if (PyErr_Occurred()) { PyErr_Clear(); ok = false; }
+    return (float)v;
+}
+
+int token_code(at::ScalarType t) {
+    return t == at::kByte ? MB_TOKEN_U8 : t == at::kInt ? MB_TOKEN_I32 : t == at::kLong ? MB_TOKEN_I64 : -1;
+}
+
+// tokens, weight, scale, out_dtype, out
+PyObject *embedding_fwd(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    ARGS(5)
+    return guarded([&]() -> PyObject * {
+        Call c;
+        const at::Tensor *w = c.first(a[1], 2);
+        const at::Tensor *t = c.ok ? plain(a[0]) : nullptr;
+        if (!t || !Call::act(w->scalar_type()) || token_code(t->scalar_type()) < 0) Py_RETURN_NONE;
+        const int64_t V = w->size(0), d = w->size(1);
+        c10::SmallVector<int64_t, 5> shape(t->sizes().begin(), t->sizes().end());
+        void *tp = c.need(a[0], shape, t->scalar_type()), *wp = c.need(a[1], {V, d}, w->scalar_type());
+        shape.push_back(d);
+        const float scale = real(a[2], c.ok);
+        at::ScalarType ot = w->scalar_type();
+        if (a[4] == Py_None && a[3] != Py_None) c.dtype(a[3], ot);
+        void *op = c.given(a[4], shape, ot);
+        PLAIN_OR_NONE(c);
+        at::Tensor out;
+        if (a[4] == Py_None) op = (out = c.fresh(shape, ot)).data_ptr();
+        const int st = unlocked([&] {
+            return embedding_fwd_fn(t->numel(), V, d, token_code(t->scalar_type()), code(w->scalar_type()), code(ot), scale, tp,
+                                    wp, op, c.stream);
+        });
+        if (st != MB_OK) return PyLong_FromLong(st);
+        return a[4] == Py_None ? wrap(std::move(out)) : same(a[4]);
+    });
+}
+
+// tokens, dy, vocab, scale, out_dtype, out
+PyObject *embedding_bwd(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    ARGS(6)
+    return guarded([&]() -> PyObject * {
+        if (!PyLong_CheckExact(a[2])) Py_RETURN_NONE;
+        int over = 0;
+        const long long V = PyLong_AsLongLongAndOverflow(a[2], &over);
+        if (over || V < 0) Py_RETURN_NONE;
+        Call c;
+        const at::Tensor *t = plain(a[0]);
+        if (!t || token_code(t->scalar_type()) < 0) Py_RETURN_NONE;
+        const at::Tensor *dy = c.first(a[1], t->dim() + 1);
+        if (!c.ok || !Call::act(dy->scalar_type())) Py_RETURN_NONE;
+        const int64_t d = dy->size(-1);
+        c10::SmallVector<int64_t, 5> shape(t->sizes().begin(), t->sizes().end());
+        void *tp = c.need(a[0], shape, t->scalar_type());
+        shape.push_back(d);
+        void *yp = c.need(a[1], shape, dy->scalar_type());
+        const float scale = real(a[3], c.ok);
+        at::ScalarType ot = at::kFloat;
+        if (a[5] == Py_None) c.dtype(a[4], ot);
+        void *op = c.given(a[5], {V, d}, ot);
+        PLAIN_OR_NONE(c);
+        at::Tensor out, ws = c.workspace(embedding_bwd_workspace_fn(t->numel(), V, d));
+        if (a[5] == Py_None) op = (out = c.fresh({V, d}, ot)).data_ptr();
+        const int st = unlocked([&] {
+            return embedding_bwd_fn(t->numel(), V, d, token_code(t->scalar_type()), code(dy->scalar_type()), code(ot), scale, tp,
+                                    yp, op, data(ws), c.stream);
+        });
+        if (st != MB_OK) return PyLong_FromLong(st);
+        return a[5] == Py_None ? wrap(std::move(out)) : same(a[5]);
+    });
+}
+
+// x, w, dy, bias, state, dstate_out, apply_silu: dx, dw, dbias, dstate
+PyObject *conv1d_bwd(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    ARGS(7)
+    return guarded([&]() -> PyObject * {
+        Call c;
+        const at::Tensor *x = c.first(a[0], 3);
+        const at::Tensor *w = c.ok ? plain(a[1]) : nullptr, *dy = c.ok ? plain(a[2]) : nullptr;
+        if (!w || !dy || w->dim() != 2 || w->size(1) < 2 || !Call::act(x->scalar_type()) || !Call::act(dy->scalar_type()))
+            Py_RETURN_NONE;
+        const int64_t nb = x->size(0), dim = x->size(1), L = x->size(2), K = w->size(1);
+        const auto in = x->scalar_type(), ot = dy->scalar_type();
+        void *xp = c.need(a[0], {nb, dim, L}, in), *wp = c.need(a[1], {dim, K}, at::kFloat);
+        void *yp = c.need(a[2], {nb, dim, L}, ot), *bp = c.maybe(a[3], {dim}, at::kFloat);
+        void *sp = c.maybe(a[4], {nb, dim, K - 1}, at::kFloat), *dp = c.maybe(a[5], {nb, dim, K - 1}, at::kFloat);
+        const int silu = PyObject_IsTrue(a[6]);
+        if (silu < 0 || K > INT32_MAX) { PyErr_Clear(); c.ok = false; }
+        PLAIN_OR_NONE(c);
+        const mb_conv_desc desc{nb, dim, L, (int32_t)K, code(in), code(ot), silu, 0, 0};
+        at::Tensor dx = c.fresh({nb, dim, L}, ot), dw = c.fresh({dim, K}, at::kFloat), db;
+        at::Tensor ds = c.fresh({nb, dim, K - 1}, at::kFloat), ws = c.workspace(conv1d_bwd_workspace_fn(&desc));
+        if (bp) db = c.fresh({dim}, at::kFloat);
+        const int st = unlocked([&] {
+            return conv1d_bwd_fn(&desc, xp, f(wp), f(bp), f(sp), yp, f(dp), dx.data_ptr(), static_cast<float *>(dw.data_ptr()),
+                                 static_cast<float *>(data(db)), static_cast<float *>(ds.data_ptr()), data(ws), c.stream);
+        });
+        if (st != MB_OK) return PyLong_FromLong(st);
+        PyObject *t = PyTuple_New(4);
+        PyTuple_SET_ITEM(t, 0, wrap(std::move(dx)));
+        PyTuple_SET_ITEM(t, 1, wrap(std::move(dw)));
+        PyTuple_SET_ITEM(t, 2, bp ? wrap(std::move(db)) : same(Py_None));
+        PyTuple_SET_ITEM(t, 3, wrap(std::move(ds)));
+        return t;
+    });
+}
+
+// A list or tuple of dense fp32 and bf16 tensors on one device, as the library takes it.
+struct TensorList {
+    std::vector<const void *> at;
+    std::vector<int64_t> sizes;
+    std::vector<int32_t> types;
+    static bool is_list(PyObject *o) { return PyList_CheckExact(o) || PyTuple_CheckExact(o); }
+    // `like`: the tensors' shapes and types have to be that list's
+    TensorList(Call &c, PyObject *o, PyObject *like = nullptr) {
+        const Py_ssize_t n = PySequence_Fast_GET_SIZE(o);
+        PyObject **item = PySequence_Fast_ITEMS(o), **other = like ? PySequence_Fast_ITEMS(like) : nullptr;
+        if (like && PySequence_Fast_GET_SIZE(like) != n) c.ok = false;
+        at.reserve(n);
+        if (!like) { sizes.reserve(n); types.reserve(n); }
+        for (Py_ssize_t i = 0; c.ok && i < n; ++i) {
+            const at::Tensor *t = plain(item[i]);
+            if (t && i == 0 && !like) t = c.first(item[i], t->dim());
+            if (!t || !c.ok || !Call::act(t->scalar_type()) || t->device() != c.dev || !t->is_contiguous()) { c.ok = false; return; }
+            if (like) {
+                const at::Tensor &g = THPVariable_Unpack(other[i]);
+                if (t->scalar_type() != g.scalar_type() || t->sizes() != g.sizes()) { c.ok = false; return; }
+            } else {
+                sizes.push_back(t->numel());
+                types.push_back(code(t->scalar_type()));
+            }
+            at.push_back(t->data_ptr());
+        }
+    }
+};
+
+// grads
+PyObject *grad_norm(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    ARGS(1)
+    return guarded([&]() -> PyObject * {
+        if (!TensorList::is_list(a[0]) || PySequence_Fast_GET_SIZE(a[0]) == 0) Py_RETURN_NONE;
+        Call c;
+        const TensorList g(c, a[0]);
+        PLAIN_OR_NONE(c);
+        const int64_t n = (int64_t)g.at.size();
+        at::Tensor norm = c.fresh({}, at::kFloat), ws = c.workspace(grad_norm_workspace_fn(n));
+        const int st = unlocked([&] {
+            return grad_norm_fn(n, g.at.data(), g.sizes.data(), g.types.data(), static_cast<float *>(norm.data_ptr()), data(ws),
+                                c.stream);
+        });
+        return st != MB_OK ? PyLong_FromLong(st) : wrap(std::move(norm));
+    });
+}
+
+// grads, max_norm, eps, out
+PyObject *clip_grad_norm(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    ARGS(4)
+    return guarded([&]() -> PyObject * {
+        if (!TensorList::is_list(a[0]) || PySequence_Fast_GET_SIZE(a[0]) == 0) Py_RETURN_NONE;
+        if (a[3] != Py_None && !TensorList::is_list(a[3])) Py_RETURN_NONE;
+        Call c;
+        const TensorList g(c, a[0]);
+        const float max_norm = real(a[1], c.ok), eps = real(a[2], c.ok);
+        PLAIN_OR_NONE(c);
+        std::vector<void *> out;
+        if (a[3] != Py_None) {
+            const TensorList o(c, a[3], a[0]);
+            PLAIN_OR_NONE(c);
+            for (const void *p : o.at) out.push_back(const_cast<void *>(p));
+        }
+        const int64_t n = (int64_t)g.at.size();
+        at::Tensor norm = c.fresh({}, at::kFloat), ws = c.workspace(grad_norm_workspace_fn(n));
+        const int st = unlocked([&] {
+            return clip_grad_norm_fn(n, g.at.data(), a[3] != Py_None ? out.data() : nullptr, g.sizes.data(), g.types.data(),
+                                     max_norm, eps, static_cast<float *>(norm.data_ptr()), data(ws), c.stream);
+        });
+        return st != MB_OK ? PyLong_FromLong(st) : wrap(std::move(norm));
+    });
+}
+
+// logits, draft, uniform, noise, draft_logits, lengths, temperature, return_probs
+PyObject *verify_sample(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    ARGS(8)
+    return guarded([&]() -> PyObject * {
+        Call c;
+        const at::Tensor *lg = c.first(a[0], 3);
+        if (!c.ok || !Call::act(lg->scalar_type()) || lg->size(1) < 1) Py_RETURN_NONE;
+        const int64_t nb = lg->size(0), n = lg->size(1) - 1, V = lg->size(2);
+        const auto act = lg->scalar_type();
+        void *lp = c.need(a[0], {nb, n + 1, V}, act), *dp = c.need(a[1], {nb, n}, at::kInt);
+        void *up = c.need(a[2], {nb, n}, at::kFloat), *np = c.need(a[3], {nb, V}, at::kFloat);
+        void *qp = c.maybe(a[4], {nb, n, V}, act), *sp = c.maybe(a[5], {nb}, at::kInt);
+        const float temperature = real(a[6], c.ok);
+        const int want = PyObject_IsTrue(a[7]);
+        if (want < 0) { PyErr_Clear(); c.ok = false; }
+        PLAIN_OR_NONE(c);
+        at::Tensor acc = c.fresh({nb}, at::kInt), pos = c.fresh({nb}, at::kInt), next = c.fresh({nb}, at::kInt), probs;
+        if (want) probs = c.fresh({nb, n}, at::kFloat);
+        at::Tensor ws = c.workspace(verify_sample_workspace_fn(nb, n, V));
+        const int st = unlocked([&] {
+            return verify_sample_fn(nb, n, V, code(act), temperature, lp, qp, static_cast<const int32_t *>(dp),
+                                    static_cast<const int32_t *>(sp), f(up), f(np), static_cast<int32_t *>(acc.data_ptr()),
+                                    static_cast<int32_t *>(pos.data_ptr()), static_cast<int32_t *>(next.data_ptr()),
+                                    static_cast<float *>(data(probs)), data(ws), c.stream);
+        });
+        if (st != MB_OK) return PyLong_FromLong(st);
+        PyObject *t = PyTuple_New(want ? 4 : 3);
+        PyTuple_SET_ITEM(t, 0, wrap(std::move(acc)));
+        PyTuple_SET_ITEM(t, 1, wrap(std::move(pos)));
+        PyTuple_SET_ITEM(t, 2, wrap(std::move(next)));
+        if (want) PyTuple_SET_ITEM(t, 3, wrap(std::move(probs)));
+        return t;
+    });
+}
+
 // setup(function addresses in the order below, current_device, raw_stream, Parameter)
 PyObject *setup(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
-    ARGS(10)
-    void *at[7];
-    for (int i = 0; i < 7; ++i) {
+    constexpr int kFunctions = 17;
+    ARGS(kFunctions + 3)
+    void *at[kFunctions];
+    for (int i = 0; i < kFunctions; ++i) {
         at[i] = PyLong_AsVoidPtr(a[i]);
         if (!at[i]) return PyErr_Occurred() ? nullptr : (PyErr_SetString(PyExc_ValueError, "null address"), nullptr);
     }
-    scan_fwd_fn = reinterpret_cast<decltype(scan_fwd_fn)>(at[0]);
-    scan_fwd_states_fn = reinterpret_cast<decltype(scan_fwd_states_fn)>(at[1]);
-    scan_fwd_ckpt_fn = reinterpret_cast<decltype(scan_fwd_ckpt_fn)>(at[2]);
-    scan_step_fn = reinterpret_cast<decltype(scan_step_fn)>(at[3]);
-    conv1d_fwd_fn = reinterpret_cast<decltype(conv1d_fwd_fn)>(at[4]);
-    conv1d_step_fn = reinterpret_cast<decltype(conv1d_step_fn)>(at[5]);
-    verify_rank_fn = reinterpret_cast<decltype(verify_rank_fn)>(at[6]);
-    current_device = same(a[7]);
-    raw_stream = same(a[8]);
-    parameter_type = same(a[9]);
+    int k = 0;
+    auto take = [&](auto &fn) { fn = reinterpret_cast<std::decay_t<decltype(fn)>>(at[k++]); };
+    take(scan_fwd_fn);
+    take(scan_fwd_states_fn);
+    take(scan_fwd_ckpt_fn);
+    take(scan_step_fn);
+    take(conv1d_fwd_fn);
+    take(conv1d_step_fn);
+    take(verify_rank_fn);
+    take(embedding_fwd_fn);
+    take(embedding_bwd_fn);
+    take(embedding_bwd_workspace_fn);
+    take(conv1d_bwd_fn);
+    take(conv1d_bwd_workspace_fn);
+    take(grad_norm_fn);
+    take(grad_norm_workspace_fn);
+    take(clip_grad_norm_fn);
+    take(verify_sample_fn);
+    take(verify_sample_workspace_fn);
+    current_device = same(a[k]);
+    raw_stream = same(a[k + 1]);
+    parameter_type = same(a[k + 2]);
     Py_RETURN_NONE;
 }
 
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(setup),  METHOD(scan_step),   METHOD(scan_fwd),
                          METHOD(conv1d), METHOD(conv1d_step), METHOD(verify_rank),
+                         METHOD(embedding_fwd), METHOD(embedding_bwd), METHOD(conv1d_bwd),
+                         METHOD(grad_norm), METHOD(clip_grad_norm), METHOD(verify_sample),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
