@@ -287,9 +287,10 @@ int list_alias(int64_t count, const void *const *grads, void *const *out, const 
 int norm_and_clip(int64_t count, const void *const *grads, void *const *out, const int64_t *sizes, const int32_t *dtypes,
                   bool scaled, float max_norm, float eps, float *norm, void *workspace, hipStream_t st) {
     namespace C = mbs::clip;
-    int64_t used = 0, units = 0;
+    int64_t used = 0, units = 0, bytes = 0;
     for (int64_t i = 0; i < count; ++i) {
         if (sizes[i] == 0) continue;
+        bytes += sizes[i] * (int64_t)dtype_size(dtypes[i]);
         units += (sizes[i] + C::lead(grads[i], dtypes[i]) + C::kUnit - 1) / C::kUnit;
         ++used;
         if (units >= (int64_t(1) << 31) || used >= (int64_t(1) << 31)) return MB_ERR_SHAPE;
@@ -319,6 +320,8 @@ int norm_and_clip(int64_t count, const void *const *grads, void *const *out, con
     p.max_norm = max_norm;
     p.eps = eps;
     const dim3 grid((unsigned)std::min<int64_t>(std::max<int64_t>(units, 1), C::kBlocks)), block(C::kThreads);
+    // kCached bytes in units of the list's mean size, for each workgroup
+    p.cached = (uint32_t)(scaled ? C::kCached / (std::max<int64_t>(bytes / std::max<int64_t>(units, 1), 1) * grid.x) : 0);
     C::Table<C::kInline> small{};
     void *args[] = {&p, &small};
     if (inlined) {
