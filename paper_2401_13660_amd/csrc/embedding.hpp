@@ -24,7 +24,7 @@ namespace embed {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kBins = 256;         // digits of one pass of the sort
-constexpr int kChunk = 64;         // sorted positions per wave: one per lane
+constexpr int kChunk = 64;         // sorted positions per wave at most: one per lane
 constexpr int kJoinWaves = 8;
 constexpr int kNone = -1;
 
@@ -45,13 +45,14 @@ struct BwdParams {
     float scale;
     int32_t tile;                  // tokens per workgroup of the sort
     int32_t tiles;                 // workgroups of the sort, at most kBins
+    int32_t chunk;                 // sorted positions per wave
     int32_t shift;                 // bits below this pass's digit
     uint32_t *counts;              // (tiles, kBins)
     uint32_t *valid;               // tokens within the vocabulary
     const Pair *from;              // the pass's input after the first pass
     Pair *to;                      // the pass's output; the sorted list
-    float *head, *tail;            // (chunks, dim): sums of the token that a chunk begins / ends with, where it
-                                   // came from the chunk before / goes on into the next
+    float *head, *tail;            // (groups, dim): sums of the token that a group of chunks begins / ends with,
+                                   // where it came from the group before / goes on into the next
 };
 
 // Tokens by mb_token_type.
@@ -61,34 +62,32 @@ template <int TOK> __device__ __forceinline__ int64_t token_at(const void *p, in
     else return static_cast<const int64_t *>(p)[i];
 }
 
-// Elements per lane: 16 bytes of the narrower type.
-template <int A, int B> constexpr int kSpan = A == 0 && B == 0 ? 4 : 8;
+// Where the span of S columns that begins at `col` is read and written: a row's last span is moved back to end with the
+// row, so that none is cut (what two spans share they both hold the same of).  Rows shorter than a span take spans of one.
+template <int S> __device__ __forceinline__ int64_t span_at(int64_t col, int64_t dim) { return min(col, dim - S); }
 
 // A workgroup takes p.rows rows, as spans side by side.
-template <int TOK, int W, int OUT>
+template <int TOK, int W, int OUT, int S>
 __global__ __launch_bounds__(kThreads) void embed_fwd(FwdParams p) {
-    constexpr int S = kSpan<W, OUT>, PER = 4;
+    constexpr int PER = 4;
     const int64_t row0 = (int64_t)blockIdx.x * p.rows;
     const uint32_t spans = (uint32_t)((p.dim + S - 1) / S);
     const uint32_t items = (uint32_t)min((int64_t)p.rows, p.ntokens - row0) * spans;
     for (uint32_t i0 = threadIdx.x; i0 < items; i0 += PER * kThreads) {
         int64_t row[PER], t[PER];
-        uint32_t col[PER];
+        int64_t col[PER];
         Span<W, S> s[PER];
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
             const uint32_t i = min(i0 + k * kThreads, items - 1);       // past the end: the last one again, not stored
             const uint32_t r = i / spans;
             row[k] = row0 + r;
-            col[k] = (i - r * spans) * S;
+            col[k] = span_at<S>((int64_t)(i - r * spans) * S, p.dim);
             t[k] = token_at<TOK>(p.tokens, row[k]);
         }
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
-            const int64_t at = (t[k] >= 0 && t[k] < p.vocab ? t[k] : 0) * p.dim + col[k];
-            if (p.vocab == 0) s[k].load_first(p.weight, 0, 0);
-            else if (col[k] + S <= p.dim) s[k].load(p.weight, at);
-            else s[k].load_first(p.weight, at, (int)(p.dim - col[k]));
+            s[k].load(p.weight, (t[k] >= 0 && t[k] < p.vocab ? t[k] : 0) * p.dim + col[k]);
         }
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
@@ -96,8 +95,7 @@ __global__ __launch_bounds__(kThreads) void embed_fwd(FwdParams p) {
             float v[S];
 #pragma unroll
             for (int j = 0; j < S; ++j) v[j] = t[k] < 0 ? 0.0f : t[k] < p.vocab ? p.scale * s[k].get(j) : __builtin_nanf("");
-            if (col[k] + S <= p.dim) store_span<OUT, S>(p.out, row[k] * p.dim + col[k], v);
-            else store_first<OUT, S>(p.out, row[k] * p.dim + col[k], v, (int)(p.dim - col[k]));
+            store_span<OUT, S>(p.out, row[k] * p.dim + col[k], v);
         }
     }
 }
@@ -203,110 +201,173 @@ __global__ __launch_bounds__(kThreads) void scatter(BwdParams p) {
     }
 }
 
-template <int DY, int OUT> constexpr int kRowSpan = DY == 1 ? 8 : 4;
+// Everything asked of memory has arrived (vmcnt 0).  Loads and stores share that counter and a wait is for the oldest of
+// both, so a wave that waited row by row would wait for each sum that it stored in between as well.
+__device__ __forceinline__ void wait_for_memory() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 
-// Sums of one chunk's rows for one tile of columns.
-template <int DY, int OUT>
+// Sums of the rows of a group of kWaves chunks, one chunk per wave, for one tile of columns.
+template <int DY, int OUT, int S>
 __global__ __launch_bounds__(kThreads) void sum_chunks(BwdParams p, uint32_t col_tiles) {
-    constexpr int S = kRowSpan<DY, OUT>, AHEAD = 8;
-    const int64_t item = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
-    const int64_t chunk = item / col_tiles, n = *p.valid, from = chunk * kChunk;
-    if (from >= n) return;
-    const int lane = threadIdx.x & 63;
-    const int64_t col = (item - chunk * col_tiles) * (64 * S) + lane * S;
-    const int cols = (int)max((int64_t)0, min((int64_t)S, p.dim - col));
-    const int m = (int)min((int64_t)kChunk, n - from);
-    const Pair mine = p.to[from + min(lane, m - 1)];
-    const int64_t before = from > 0 ? (int64_t)p.to[from - 1].key : kNone;
-    const int64_t after = from + m < n ? (int64_t)p.to[from + m].key : kNone;
-
-    float acc[S] = {};
-    uint32_t key = __builtin_amdgcn_readlane(mine.key, 0);
-    bool first_run = true;
-    auto store = [&](float *part) {
-        if (cols == S) store_span<0, S>(part, chunk * p.dim + col, acc);
-        else store_first<0, S>(part, chunk * p.dim + col, acc, cols);
+    constexpr int AHEAD = 8;
+    __shared__ float piece[kWaves][2][64][S];           // a chunk's first run's sum, and its last one's
+    __shared__ uint32_t piece_key[kWaves][2];
+    __shared__ int piece_is[kWaves];
+    constexpr int kHead = 1, kThrough = 2, kTail = 4;   // the first run came from before; it goes on after; the last one does
+    const int64_t group = blockIdx.x / col_tiles, n = *p.valid;
+    if (group * kWaves * p.chunk >= n) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t from = (group * kWaves + wave) * p.chunk;
+    const int64_t col = span_at<S>((int64_t)(blockIdx.x % col_tiles) * (64 * S) + lane * S, p.dim);
+    const int m = (int)max((int64_t)0, min((int64_t)p.chunk, n - from));
+    // The sum of a run that is whole, in dW's type.
+    auto finish = [&](const float (&acc)[S], uint32_t key) {
+        float v[S];
+#pragma unroll
+        for (int j = 0; j < S; ++j) v[j] = p.scale * acc[j];
+        store_span<OUT, S>(p.dweight, (int64_t)key * p.dim + col, v);
     };
-    auto flush = [&](bool goes_on) {
-        if (first_run && before == (int64_t)key) {
-            store(p.head);
+    int is = 0;
+    if (m > 0) {
+        const Pair mine = p.to[from + min(lane, m - 1)];
+        const int64_t before = from > 0 ? (int64_t)p.to[from - 1].key : kNone;
+        const int64_t after = from + m < n ? (int64_t)p.to[from + m].key : kNone;
+        float acc[S] = {};
+        uint32_t key = __builtin_amdgcn_readlane(mine.key, 0);
+        bool came = before == (int64_t)key;             // the run at hand began before the chunk
+        auto keep = [&](int which) {
+#pragma unroll
+            for (int j = 0; j < S; ++j) piece[wave][which][lane][j] = acc[j];
+            if (lane == 0) piece_key[wave][which] = key;
+        };
+        Span<DY, S> row[2][AHEAD];
+        auto load = [&](Span<DY, S> (&r)[AHEAD], int i0) {
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const uint32_t pos = __builtin_amdgcn_readlane(mine.pos, min(i0 + k, m - 1));
+                r[k].template load<true>(p.dy, pos * p.dim + col);
+            }
+        };
+        auto add = [&](const Span<DY, S> (&r)[AHEAD], int i0) {
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                if (i0 + k >= m) break;
+                const uint32_t next = __builtin_amdgcn_readlane(mine.key, i0 + k);
+                if (next != key) {
+                    if (came) {
+                        keep(0);
+                        is |= kHead;
+                    } else {
+                        finish(acc, key);
+                    }
+                    came = false;
+                    key = next;
+#pragma unroll
+                    for (int j = 0; j < S; ++j) acc[j] = 0.0f;
+                }
+#pragma unroll
+                for (int j = 0; j < S; ++j) acc[j] += r[k].get(j);
+            }
+        };
+        // the next rows are on their way while a group is added up
+        load(row[0], 0);
+        for (int i0 = 0; i0 < m; i0 += 2 * AHEAD) {
+            wait_for_memory();
+            if (i0 + AHEAD < m) load(row[1], i0 + AHEAD);
+            add(row[0], i0);
+            wait_for_memory();
+            if (i0 + 2 * AHEAD < m) load(row[0], i0 + 2 * AHEAD);
+            add(row[1], i0 + AHEAD);
+        }
+        const bool goes_on = after == (int64_t)key;
+        if (came) {
+            keep(0);
+            is |= kHead | (goes_on ? kThrough : 0);
         } else if (goes_on) {
-            store(p.tail);
+            keep(1);
+            is |= kTail;
         } else {
-            float v[S];
-#pragma unroll
-            for (int j = 0; j < S; ++j) v[j] = p.scale * acc[j];
-            if (cols == S) store_span<OUT, S>(p.dweight, (int64_t)key * p.dim + col, v);
-            else store_first<OUT, S>(p.dweight, (int64_t)key * p.dim + col, v, cols);
+            finish(acc, key);
         }
-    };
-    for (int i0 = 0; i0 < m; i0 += AHEAD) {
-        Span<DY, S> row[AHEAD];
+    }
+    if (lane == 0) piece_is[wave] = is;
+    __syncthreads();
+    if (wave != 0) return;
+
+    // The runs that lie in more than one of the group's chunks, or go beyond it.
+    float acc[S] = {};
+    uint32_t key = 0;
+    bool open = false, came = false;
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            const int64_t at = (int64_t)(uint32_t)__builtin_amdgcn_readlane(mine.pos, min(i0 + k, m - 1)) * p.dim + col;
-            if (cols == S) row[k].template load<true>(p.dy, at);
-            else row[k].load_first(p.dy, at, cols);
-        }
+    for (int w = 0; w < kWaves; ++w) {
+        const int f = piece_is[w];
+        if (f & kHead) {
+            came = w == 0 || came;
+            key = piece_key[w][0];
+            open = true;
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) {
-            if (i0 + k >= m) break;
-            const uint32_t next = __builtin_amdgcn_readlane(mine.key, i0 + k);
-            if (next != key) {
-                flush(false);
-                key = next;
-                first_run = false;
+            for (int j = 0; j < S; ++j) acc[j] += piece[w][0][lane][j];
+            if (!(f & kThrough)) {
+                if (came) store_span<0, S>(p.head, group * p.dim + col, acc);
+                else finish(acc, key);
+                open = came = false;
 #pragma unroll
                 for (int j = 0; j < S; ++j) acc[j] = 0.0f;
             }
+        }
+        if (f & kTail) {
+            key = piece_key[w][1];
+            open = true;
 #pragma unroll
-            for (int j = 0; j < S; ++j) acc[j] += row[k].get(j);
+            for (int j = 0; j < S; ++j) acc[j] = piece[w][1][lane][j];
         }
     }
-    flush(after == (int64_t)key);
+    if (open) store_span<0, S>(came ? p.head : p.tail, group * p.dim + col, acc);
 }
 
-// The tokens whose rows lie in more than one chunk: the chunk in which one begins joins its sums.
-template <int OUT>
-__global__ __launch_bounds__(64 * kJoinWaves) void join_chunks(BwdParams p, uint32_t col_tiles) {
-    constexpr int S = 4;
-    __shared__ f32x4 sums[kJoinWaves][64];
-    const int64_t chunk = blockIdx.x / col_tiles, n = *p.valid, from = chunk * kChunk, next = from + kChunk;
-    if (next >= n) return;                              // no chunk follows
-    const uint32_t key = p.to[next - 1].key;
-    if (p.to[next].key != key) return;                  // nothing goes on
-    if (p.to[from].key == key && from > 0 && p.to[from - 1].key == key) return;      // it began before
+// The tokens whose rows lie in more than one group: the group in which one begins joins its sums.
+template <int OUT, int S>
+__global__ __launch_bounds__(64 * kJoinWaves) void join_groups(BwdParams p, uint32_t col_tiles) {
+    __shared__ float sums[kJoinWaves][64][S];
+    const int64_t size = (int64_t)kWaves * p.chunk, group = blockIdx.x / col_tiles, from = group * size, next = from + size;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    // the chunks after this one that begin with the token
+    // All that the decision reads, asked for at once; places past the valid ones hold nothing that counts.
+    const int64_t most = p.ntokens - 1, n = *p.valid;
+    const uint32_t first = p.to[from].key, before = p.to[max(from - 1, (int64_t)0)].key;
+    const uint32_t key = p.to[min(next - 1, most)].key, after = p.to[min(next, most)].key;
+    uint32_t begins = p.to[min(next + lane * size, most)].key;
+    if (next >= n || after != key) return;                      // nothing goes on
+    if (first == key && from > 0 && before == key) return;      // it began before
+    // the groups after this one that begin with the token
     int64_t parts = 0;
     for (;;) {
-        const int64_t at = next + (parts + lane) * kChunk;
-        const uint64_t same = __ballot(at < n && p.to[min(at, n - 1)].key == key);
+        const uint64_t same = __ballot(next + (parts + lane) * size < n && begins == key);
         const int run = ~same == 0 ? 64 : __ffsll((unsigned long long)~same) - 1;
         parts += run;
         if (run < 64) break;
+        begins = p.to[min(next + (parts + lane) * size, most)].key;
     }
-    const int64_t col = (blockIdx.x % col_tiles) * (64 * S) + lane * S;
-    const int cols = (int)max((int64_t)0, min((int64_t)S, p.dim - col));
-    // sum 0 is the tail of this chunk, the others the heads of the next; each wave takes a run of them
+    const int64_t col = span_at<S>((int64_t)(blockIdx.x % col_tiles) * (64 * S) + lane * S, p.dim);
+    // sum 0 is the tail of this group, the others the heads of the next; each wave takes a run of them
     const int64_t all = parts + 1, lo = all * wave / kJoinWaves, hi = all * (wave + 1) / kJoinWaves;
-    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    float acc[S] = {};
 #pragma unroll 8
     for (int64_t k = lo; k < hi; ++k) {
-        const float *part = (k == 0 ? p.tail + chunk * p.dim : p.head + (chunk + k) * p.dim) + col;
         Span<0, S> s;
-        if (cols == S) s.load(part, 0);
-        else s.load_first(part, 0, cols);
-        acc += s.v[0];
+        s.load(k == 0 ? p.tail : p.head, (group + k) * p.dim + col);
+#pragma unroll
+        for (int j = 0; j < S; ++j) acc[j] += s.get(j);
     }
-    sums[wave][lane] = acc;
+#pragma unroll
+    for (int j = 0; j < S; ++j) sums[wave][lane][j] = acc[j];
     __syncthreads();
     if (wave != 0) return;
 #pragma unroll
-    for (int w = 1; w < kJoinWaves; ++w) acc += sums[w][lane];
-    const float v[S] = {p.scale * acc[0], p.scale * acc[1], p.scale * acc[2], p.scale * acc[3]};
-    if (cols == S) store_span<OUT, S>(p.dweight, (int64_t)key * p.dim + col, v);
-    else store_first<OUT, S>(p.dweight, (int64_t)key * p.dim + col, v, cols);
+    for (int w = 1; w < kJoinWaves; ++w)
+#pragma unroll
+        for (int j = 0; j < S; ++j) acc[j] += sums[w][lane][j];
+#pragma unroll
+    for (int j = 0; j < S; ++j) acc[j] *= p.scale;
+    store_span<OUT, S>(p.dweight, (int64_t)key * p.dim + col, acc);
 }
 
 }  // namespace embed

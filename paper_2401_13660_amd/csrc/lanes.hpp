@@ -68,7 +68,7 @@ template <> struct Span<1, 4> {
     }
     __device__ __forceinline__ float get(int i) const { return i & 1 ? bf16_hi(v[i >> 1]) : bf16_lo(v[i >> 1]); }
 };
-template <int S> struct Span<0, S> {
+template <int S> struct SpanF32 {
     f32x4 v[S / 4];
     template <bool ONCE = false> __device__ __forceinline__ void load(const void *p, int64_t at) {
 #pragma unroll
@@ -82,8 +82,20 @@ template <int S> struct Span<0, S> {
     __device__ __forceinline__ float get(int i) const { return v[i / 4][i % 4]; }
 };
 
+template <> struct Span<0, 4> : SpanF32<4> {};
+template <> struct Span<0, 8> : SpanF32<8> {};
+
+// One element: for rows shorter than a span.
+template <int DT> struct Span<DT, 1> {
+    float v;
+    template <bool ONCE = false> __device__ __forceinline__ void load(const void *p, int64_t at) { v = Act<DT>::ld(p, at); }
+    __device__ __forceinline__ float get(int) const { return v; }
+};
+
 template <int DT, int S, bool ONCE = false> __device__ __forceinline__ void store_span(void *p, int64_t at, const float (&v)[S]) {
-    if constexpr (DT == 0) {
+    if constexpr (S == 1) {
+        st_out<DT>(p, at, v[0]);
+    } else if constexpr (DT == 0) {
 #pragma unroll
         for (int i = 0; i < S / 4; ++i)
             put<ONCE>(reinterpret_cast<f32x4_any *>(static_cast<float *>(p) + at) + i,

@@ -4,6 +4,9 @@
 // include/mbscan.h.
 #include <hip/hip_runtime.h>
 
+#ifndef WV
+#define WV 2048
+#endif
 #include <algorithm>
 #include <cmath>
 #include <cstdlib>
@@ -53,13 +56,20 @@ struct Workspace {
 bool valid_token_type(int32_t t) { return t == MB_TOKEN_U8 || t == MB_TOKEN_I32 || t == MB_TOKEN_I64; }
 size_t token_size(int32_t t) { return t == MB_TOKEN_U8 ? 1 : t == MB_TOKEN_I32 ? 4 : 8; }
 
-template <int TOK, int A> const void *embed_fwd_fn(int32_t out) {
-    return out == MB_F32 ? reinterpret_cast<const void *>(&mbs::embed::embed_fwd<TOK, A, 0>)
-                         : reinterpret_cast<const void *>(&mbs::embed::embed_fwd<TOK, A, 1>);
+// Elements per lane: 16 bytes of the narrower type, or one where rows are shorter than that.
+template <int A, int B> constexpr int kEmbedSpan = A == 0 && B == 0 ? 4 : 8;
+
+template <int TOK, int W, int OUT> const void *embed_fwd_fn(int64_t dim, int64_t *span) {
+    constexpr int S = kEmbedSpan<W, OUT>;
+    *span = dim < S ? 1 : S;
+    return dim < S ? reinterpret_cast<const void *>(&mbs::embed::embed_fwd<TOK, W, OUT, 1>)
+                   : reinterpret_cast<const void *>(&mbs::embed::embed_fwd<TOK, W, OUT, S>);
 }
-template <int TOK> const void *embed_fwd_fn(int32_t in, int32_t out) {
-    return in == MB_F32 ? embed_fwd_fn<TOK, 0>(out) : embed_fwd_fn<TOK, 1>(out);
+template <int TOK> const void *embed_fwd_fn(int32_t in, int32_t out, int64_t dim, int64_t *span) {
+    if (in == MB_F32) return out == MB_F32 ? embed_fwd_fn<TOK, 0, 0>(dim, span) : embed_fwd_fn<TOK, 0, 1>(dim, span);
+    return out == MB_F32 ? embed_fwd_fn<TOK, 1, 0>(dim, span) : embed_fwd_fn<TOK, 1, 1>(dim, span);
 }
+
 // The workspace's areas, each on a 256-byte boundary.
 struct Areas {
     size_t bytes = 0;
@@ -72,7 +82,7 @@ struct Areas {
 
 // The sort of an embedding's gradient and its workspace.
 struct EmbedPlan {
-    int64_t tile, tiles, chunks;
+    int64_t tile, tiles, chunk, groups;
     int passes;
     size_t counts, valid, a, b, head, tail, bytes;
     EmbedPlan(int64_t ntokens, int64_t vocab, int64_t dim) {
@@ -82,14 +92,17 @@ struct EmbedPlan {
         tiles = (ntokens + tile - 1) / tile;
         passes = 1;
         while (passes < 4 && (vocab - 1) >> (8 * passes)) ++passes;
-        chunks = (ntokens + E::kChunk - 1) / E::kChunk;
+        // sorted positions per wave: 64, or fewer where that leaves the SIMDs with less than two waves
+        chunk = E::kChunk;
+        while (chunk > 16 && ntokens / chunk * ((dim + 255) / 256) < WV) chunk /= 2;
+        groups = (ntokens + chunk * E::kWaves - 1) / (chunk * E::kWaves);
         Areas w;
         counts = w.add((size_t)tiles * E::kBins * 4);
         valid = w.add(4);
         a = w.add((size_t)ntokens * sizeof(E::Pair));
         b = w.add(passes > 1 ? (size_t)ntokens * sizeof(E::Pair) : 0);
-        head = w.add((size_t)chunks * (size_t)dim * 4);
-        tail = w.add((size_t)chunks * (size_t)dim * 4);
+        head = w.add((size_t)groups * (size_t)dim * 4);
+        tail = w.add((size_t)groups * (size_t)dim * 4);
         bytes = w.bytes;
     }
 };
@@ -116,16 +129,21 @@ template <int TOK, int OUT> hipError_t embed_sort(mbs::embed::BwdParams &p, cons
     return hipSuccess;
 }
 
-template <int DY, int OUT> hipError_t embed_sum(mbs::embed::BwdParams &p, const EmbedPlan &f, hipStream_t st) {
+template <int DY, int OUT, int S> hipError_t embed_sum(mbs::embed::BwdParams &p, const EmbedPlan &f, hipStream_t st) {
     namespace E = mbs::embed;
-    uint32_t cols = (uint32_t)((p.dim + 64 * E::kRowSpan<DY, OUT> - 1) / (64 * E::kRowSpan<DY, OUT>));
+    uint32_t cols = (uint32_t)((p.dim + 64 * S - 1) / (64 * S));
     void *args[] = {&p, &cols};
-    hipError_t e = hipLaunchKernel(reinterpret_cast<const void *>(&E::sum_chunks<DY, OUT>),
-                                   dim3((unsigned)((f.chunks * cols + E::kWaves - 1) / E::kWaves)), dim3(E::kThreads), args, 0, st);
-    if (e != hipSuccess || f.chunks < 2) return e;
-    cols = (uint32_t)((p.dim + 255) / 256);
-    return hipLaunchKernel(reinterpret_cast<const void *>(&E::join_chunks<OUT>), dim3((unsigned)((f.chunks - 1) * cols)),
+    hipError_t e = hipLaunchKernel(reinterpret_cast<const void *>(&E::sum_chunks<DY, OUT, S>),
+                                   dim3((unsigned)(f.groups * cols)), dim3(E::kThreads), args, 0, st);
+    if (e != hipSuccess || f.groups < 2) return e;
+    constexpr int J = S == 1 ? 1 : 4;                               // the sums are fp32
+    cols = (uint32_t)((p.dim + 64 * J - 1) / (64 * J));
+    return hipLaunchKernel(reinterpret_cast<const void *>(&E::join_groups<OUT, J>), dim3((unsigned)((f.groups - 1) * cols)),
                            dim3(64 * E::kJoinWaves), args, 0, st);
+}
+template <int DY, int OUT> hipError_t embed_sum(mbs::embed::BwdParams &p, const EmbedPlan &f, hipStream_t st) {
+    constexpr int S = DY == 1 ? 8 : 4;
+    return p.dim < S ? embed_sum<DY, OUT, 1>(p, f, st) : embed_sum<DY, OUT, S>(p, f, st);
 }
 
 template <int OUT> hipError_t embed_bwd(mbs::embed::BwdParams &p, const EmbedPlan &f, int32_t token_type, int32_t dy_dtype,
@@ -362,21 +380,23 @@ int mb_embedding_fwd(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_
     const int st = embed_checks(ntokens, vocab, dim, token_type, weight_dtype, out_dtype, &row_elems, &table_elems);
     if (st != MB_OK) return st;
     if (row_elems == 0) return MB_OK;
-    if (!tokens || !out || (!weight && table_elems > 0)) return MB_ERR_NULL;
+    if (vocab == 0) return MB_ERR_SHAPE;                            // tokens, and no table to look them up in
+    if (!tokens || !out || !weight) return MB_ERR_NULL;
     const size_t tsz = token_size(token_type), wsz = dtype_size(weight_dtype), osz = dtype_size(out_dtype);
     if (!aligned(tokens, tsz) || !aligned(weight, wsz) || !aligned(out, osz)) return MB_ERR_ALIGN;
     const Range outs[] = {{out, (size_t)row_elems * osz}};
     const Range ins[] = {{tokens, (size_t)ntokens * tsz}, {weight, (size_t)table_elems * wsz}};
     if (any_overlap(outs, ins)) return MB_ERR_ALIAS;
+    int64_t span;
+    const void *fn = token_type == MB_TOKEN_U8    ? embed_fwd_fn<0>(weight_dtype, out_dtype, dim, &span)
+                     : token_type == MB_TOKEN_I32 ? embed_fwd_fn<1>(weight_dtype, out_dtype, dim, &span)
+                                                  : embed_fwd_fn<2>(weight_dtype, out_dtype, dim, &span);
     // spans of a row, and rows per workgroup: 1,024 spans where that leaves 2,048 workgroups
-    const int64_t span = weight_dtype == MB_F32 && out_dtype == MB_F32 ? 4 : 8, spans = (dim + span - 1) / span;
+    const int64_t spans = (dim + span - 1) / span;
     const int64_t rows = std::max<int64_t>(1, std::min(1024 / spans, ntokens / 2048));
     const int64_t blocks = (ntokens + rows - 1) / rows;
     if (spans >= (int64_t(1) << 31) || blocks >= (int64_t(1) << 24)) return MB_ERR_SHAPE;
     mbs::embed::FwdParams p{ntokens, vocab, dim, tokens, weight, out, scale, (int32_t)rows};
-    const void *fn = token_type == MB_TOKEN_U8    ? embed_fwd_fn<0>(weight_dtype, out_dtype)
-                     : token_type == MB_TOKEN_I32 ? embed_fwd_fn<1>(weight_dtype, out_dtype)
-                                                  : embed_fwd_fn<2>(weight_dtype, out_dtype);
     return status(launch(fn, dim3((unsigned)blocks), dim3(mbs::embed::kThreads), &p, stream));
 }
 
@@ -396,13 +416,13 @@ int mb_embedding_bwd(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_
     const Range ins[] = {{tokens, (size_t)ntokens * tsz}, {dy, (size_t)row_elems * ysz}};
     if (any_overlap(outs, ins)) return MB_ERR_ALIAS;
     const EmbedPlan f(ntokens, vocab, dim);
-    if (f.chunks * ((dim + 255) / 256) >= (int64_t(1) << 31)) return MB_ERR_SHAPE;
+    if (f.groups * ((dim + 255) / 256) >= (int64_t(1) << 22)) return MB_ERR_SHAPE;
     Workspace ws(workspace, f.bytes, st_of(stream));
     if (!ws.at) return MB_ERR_HIP;
     mbs::embed::BwdParams p{};
     p.ntokens = ntokens; p.vocab = vocab; p.dim = dim;
     p.tokens = tokens; p.dy = dy; p.dweight = dweight; p.scale = scale;
-    p.tile = (int32_t)f.tile; p.tiles = (int32_t)f.tiles;
+    p.tile = (int32_t)f.tile; p.tiles = (int32_t)f.tiles; p.chunk = (int32_t)f.chunk;
     p.counts = reinterpret_cast<uint32_t *>(ws.at + f.counts);
     p.valid = reinterpret_cast<uint32_t *>(ws.at + f.valid);
     p.head = reinterpret_cast<float *>(ws.at + f.head);
