@@ -46,6 +46,7 @@ struct BwdParams {
     int32_t tile;                  // tokens per workgroup of the sort
     int32_t tiles;                 // workgroups of the sort, at most kBins
     int32_t chunk;                 // sorted positions per wave
+    int64_t zero_from, zero_to;    // elements of dweight that the launch sets to zero on the side
     int32_t shift;                 // bits below this pass's digit
     uint32_t *counts;              // (tiles, kBins)
     uint32_t *valid;               // tokens within the vocabulary
@@ -110,93 +111,123 @@ template <int TOK, bool FIRST> __device__ __forceinline__ int64_t key_at(const B
     }
 }
 
-// Digits of the workgroup's places, counted; with the first pass the table is zeroed on the side (workgroups past the
-// sort's do nothing else).
-template <int TOK, int OUT, bool FIRST>
-__global__ __launch_bounds__(kThreads) void count_digits(BwdParams p) {
-    __shared__ uint32_t count[kBins];
-    const int64_t n = FIRST ? p.ntokens : (int64_t)*p.valid;
-    if ((int)blockIdx.x < p.tiles) {
-        count[threadIdx.x] = 0;
-        __syncthreads();
-        const int64_t from = (int64_t)blockIdx.x * p.tile, to = min(from + p.tile, n);
-        for (int64_t i = from + threadIdx.x; i < to; i += kThreads) {
-            const int64_t key = key_at<TOK, FIRST>(p, i);
-            if (key != kNone) atomicAdd(&count[(key >> p.shift) & (kBins - 1)], 1u);
-        }
-        __syncthreads();
-        p.counts[blockIdx.x * kBins + threadIdx.x] = count[threadIdx.x];
+// The places of a wave in a step of the sort: kPlaces per lane, 64 side by side, in order.
+constexpr int kPlaces = 4;
+constexpr int kStep = kThreads * kPlaces;
+
+template <int TOK, bool FIRST> struct Keys {
+    int64_t at[kPlaces];
+    __device__ __forceinline__ void load(const BwdParams &p, int64_t from, int64_t n) {
+        from += (threadIdx.x >> 6) * (64 * kPlaces) + (threadIdx.x & 63);
+#pragma unroll
+        for (int k = 0; k < kPlaces; ++k) at[k] = from + 64 * k < n ? key_at<TOK, FIRST>(p, from + 64 * k) : kNone;
     }
-    if constexpr (FIRST) {
-        constexpr int S = OUT == 1 ? 8 : 4;
-        const int64_t elems = p.vocab * p.dim, step = (int64_t)gridDim.x * kThreads * S;
-        const float zeros[S] = {};
-        for (int64_t i = ((int64_t)blockIdx.x * kThreads + threadIdx.x) * S; i < elems; i += step) {
-            if (i + S <= elems) store_span<OUT, S>(p.dweight, i, zeros);
-            else store_first<OUT, S>(p.dweight, i, zeros, (int)(elems - i));
-        }
+};
+
+// A share of the table set to zero, by the workgroups of a launch past the sort's: the sort's few workgroups leave the
+// chip to it.
+template <int OUT> __device__ __forceinline__ void zero_share(const BwdParams &p) {
+    constexpr int S = OUT == 1 ? 8 : 4;
+    const int64_t step = (int64_t)(gridDim.x - p.tiles) * kThreads * S;
+    const float zeros[S] = {};
+    for (int64_t i = p.zero_from + ((int64_t)(blockIdx.x - p.tiles) * kThreads + threadIdx.x) * S; i < p.zero_to; i += step) {
+        if (i + S <= p.zero_to) store_span<OUT, S>(p.dweight, i, zeros);
+        else store_first<OUT, S>(p.dweight, i, zeros, (int)(p.zero_to - i));
     }
 }
 
+// Digits of the workgroup's places, counted.
+template <int TOK, int OUT, bool FIRST>
+__global__ __launch_bounds__(kThreads) void count_digits(BwdParams p) {
+    if ((int)blockIdx.x >= p.tiles) return zero_share<OUT>(p);
+    __shared__ uint32_t count[kBins];
+    const int64_t n = FIRST ? p.ntokens : (int64_t)*p.valid;
+    const int64_t from = (int64_t)blockIdx.x * p.tile, to = min(from + p.tile, n);
+    count[threadIdx.x] = 0;
+    for (int64_t i = from; i < to || i == from; i += kStep) {
+        Keys<TOK, FIRST> keys;
+        keys.load(p, i, to);
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kPlaces; ++k)
+            if (keys.at[k] != kNone) atomicAdd(&count[(keys.at[k] >> p.shift) & (kBins - 1)], 1u);
+    }
+    __syncthreads();
+    p.counts[blockIdx.x * kBins + threadIdx.x] = count[threadIdx.x];
+}
+
 // Each place's key and position to the place that its digit gives it.  Every workgroup adds up the counts for itself:
-// the digits below (over all workgroups), then the workgroups and the waves before, then the places before.
-template <int TOK, bool FIRST>
+// the digits below (over all workgroups), then the workgroups, steps and waves before, then the places before.
+template <int TOK, int OUT, bool FIRST>
 __global__ __launch_bounds__(kThreads) void scatter(BwdParams p) {
-    __shared__ uint32_t at[kWaves][kBins], scan[kBins];
+    if ((int)blockIdx.x >= p.tiles) return zero_share<OUT>(p);
+    __shared__ uint32_t at[kWaves][kBins], waves[kWaves];
     const int d = threadIdx.x, wave = d >> 6, lane = d & 63;
     const int64_t n = FIRST ? p.ntokens : (int64_t)*p.valid;
+    const int64_t from = (int64_t)blockIdx.x * p.tile, to = min(from + p.tile, n);
+    Keys<TOK, FIRST> keys;
+    keys.load(p, from, to);
     uint32_t total = 0, before = 0;
-#pragma unroll 8
+#pragma unroll 16
     for (int g = 0; g < p.tiles; ++g) {
         const uint32_t c = p.counts[g * kBins + d];
         total += c;
         before += g < (int)blockIdx.x ? c : 0u;
     }
-    scan[d] = total;
+    // the digits below: within the wave, then the waves before
+    uint32_t below = total;
+#pragma unroll
+    for (int off = 1; off < 64; off *= 2) {
+        const uint32_t v = __shfl_up(below, off, 64);
+        below += lane >= off ? v : 0u;
+    }
+    if (lane == 63) waves[wave] = below;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) at[w][d] = 0;
     __syncthreads();
 #pragma unroll
-    for (int off = 1; off < kBins; off *= 2) {
-        const uint32_t v = d >= off ? scan[d - off] : 0u;
-        __syncthreads();
-        scan[d] += v;
-        __syncthreads();
-    }
-    if (FIRST && blockIdx.x == 0 && d == kBins - 1) *p.valid = scan[d];
-    before += scan[d] - total;
-    // the wave's own places: a quarter of the workgroup's, in order
-    const int64_t part = p.tile / kWaves, from = (int64_t)blockIdx.x * p.tile + wave * part, to = min(from + part, n);
-    for (int64_t i = from + lane; i < to; i += 64) {
-        const int64_t key = key_at<TOK, FIRST>(p, i);
-        if (key != kNone) atomicAdd(&at[wave][(key >> p.shift) & (kBins - 1)], 1u);
-    }
-    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) below += w < wave ? waves[w] : 0u;
+    if (FIRST && blockIdx.x == 0 && d == kBins - 1) *p.valid = below;
+    before += below - total;
+
+    for (int64_t i0 = from; i0 < to; i0 += kStep) {
+        if (i0 > from) {
+            keys.load(p, i0, to);
+            __syncthreads();                            // the last step's places are taken
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        const uint32_t c = at[w][d];
-        at[w][d] = before;
-        before += c;
-    }
-    __syncthreads();
-    for (int64_t i0 = from; i0 < to; i0 += 64) {
-        const int64_t i = i0 + lane;
-        const int64_t key = i < to ? key_at<TOK, FIRST>(p, i) : kNone;
-        const uint32_t digit = (uint32_t)(key >> p.shift) & (kBins - 1);
-        // the lanes of the same digit
-        uint64_t same = __ballot(key != kNone);
-#pragma unroll
-        for (int b = 0; b < 8; ++b) {
-            const uint64_t set = __ballot((digit >> b) & 1);
-            same &= (digit >> b) & 1 ? set : ~set;
+            for (int w = 0; w < kWaves; ++w) at[w][d] = 0;
+            __syncthreads();
         }
-        if (key != kNone) {
-            const int first = __ffsll((unsigned long long)same) - 1;
-            uint32_t base = 0;
-            if (lane == first) base = atomicAdd(&at[wave][digit], (uint32_t)__popcll(same));
-            base = __shfl(base, first, 64);
-            const uint32_t dest = base + __popcll(same & ((1ull << lane) - 1));
-            p.to[dest] = Pair{(uint32_t)key, FIRST ? (uint32_t)i : p.from[i].pos};
+#pragma unroll
+        for (int k = 0; k < kPlaces; ++k)
+            if (keys.at[k] != kNone) atomicAdd(&at[wave][(keys.at[k] >> p.shift) & (kBins - 1)], 1u);
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const uint32_t c = at[w][d];
+            at[w][d] = before;
+            before += c;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kPlaces; ++k) {
+            const int64_t key = keys.at[k];
+            const uint32_t digit = (uint32_t)(key >> p.shift) & (kBins - 1);
+            // the lanes of the same digit
+            uint64_t same = __ballot(key != kNone);
+#pragma unroll
+            for (int b = 0; b < 8; ++b) {
+                const uint64_t set = __ballot((digit >> b) & 1);
+                same &= (digit >> b) & 1 ? set : ~set;
+            }
+            if (key != kNone) {
+                const int first = __ffsll((unsigned long long)same) - 1;
+                uint32_t base = 0;
+                if (lane == first) base = atomicAdd(&at[wave][digit], (uint32_t)__popcll(same));
+                base = __shfl(base, first, 64);
+                const int64_t i = i0 + wave * (64 * kPlaces) + 64 * k + lane;
+                p.to[base + __popcll(same & ((1ull << lane) - 1))] = Pair{(uint32_t)key, FIRST ? (uint32_t)i : p.from[i].pos};
+            }
         }
     }
 }

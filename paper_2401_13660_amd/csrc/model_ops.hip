@@ -4,9 +4,6 @@
 // include/mbscan.h.
 #include <hip/hip_runtime.h>
 
-#ifndef WV
-#define WV 2048
-#endif
 #include <algorithm>
 #include <cmath>
 #include <cstdlib>
@@ -94,7 +91,7 @@ struct EmbedPlan {
         while (passes < 4 && (vocab - 1) >> (8 * passes)) ++passes;
         // sorted positions per wave: 64, or fewer where that leaves the SIMDs with less than two waves
         chunk = E::kChunk;
-        while (chunk > 16 && ntokens / chunk * ((dim + 255) / 256) < WV) chunk /= 2;
+        while (chunk > 16 && ntokens / chunk * ((dim + 255) / 256) < 2048) chunk /= 2;
         groups = (ntokens + chunk * E::kWaves - 1) / (chunk * E::kWaves);
         Areas w;
         counts = w.add((size_t)tiles * E::kBins * 4);
@@ -110,20 +107,30 @@ struct EmbedPlan {
 template <int TOK, int OUT> hipError_t embed_sort(mbs::embed::BwdParams &p, const EmbedPlan &f, char *ws, hipStream_t st) {
     namespace E = mbs::embed;
     E::Pair *const ab[2] = {reinterpret_cast<E::Pair *>(ws + f.a), reinterpret_cast<E::Pair *>(ws + f.b)};
-    const int64_t fill = (p.vocab * p.dim + 4095) / 4096;           // workgroups that zero the table beside the first count
+    // the table is set to zero in equal shares beside the launches of the sort; 16-byte shares keep the stores aligned
+    const int64_t elems = p.vocab * p.dim, launches = f.tiles > 0 ? 2 * f.passes : 1;
+    const int64_t share = ((elems + launches - 1) / launches + 63) / 64 * 64;
+    const int64_t zeroing = std::min<int64_t>((share + 4095) / 4096, 2048);     // workgroups of at least 4,096 elements
+    const dim3 grid((unsigned)(f.tiles + zeroing)), block(E::kThreads);
+    p.zero_from = p.zero_to = 0;
+    auto next_share = [&] {
+        p.zero_from = p.zero_to;
+        p.zero_to = std::min(p.zero_from + share, elems);
+    };
+    void *args[] = {&p};
     for (int k = 0; k < f.passes; ++k) {
         p.shift = 8 * k;
         p.from = k == 0 ? nullptr : ab[(k - 1) & 1];
         p.to = ab[k & 1];
-        void *args[] = {&p};
-        const int64_t blocks = k == 0 ? std::max<int64_t>(f.tiles, std::min<int64_t>(fill, 2048)) : f.tiles;
+        next_share();
         hipError_t e = hipLaunchKernel(k == 0 ? reinterpret_cast<const void *>(&E::count_digits<TOK, OUT, true>)
                                               : reinterpret_cast<const void *>(&E::count_digits<TOK, OUT, false>),
-                                       dim3((unsigned)std::max<int64_t>(blocks, 1)), dim3(E::kThreads), args, 0, st);
+                                       grid, block, args, 0, st);
         if (e != hipSuccess || f.tiles == 0) return e;
-        e = hipLaunchKernel(k == 0 ? reinterpret_cast<const void *>(&E::scatter<TOK, true>)
-                                   : reinterpret_cast<const void *>(&E::scatter<TOK, false>),
-                            dim3((unsigned)f.tiles), dim3(E::kThreads), args, 0, st);
+        next_share();
+        e = hipLaunchKernel(k == 0 ? reinterpret_cast<const void *>(&E::scatter<TOK, OUT, true>)
+                                   : reinterpret_cast<const void *>(&E::scatter<TOK, OUT, false>),
+                            grid, block, args, 0, st);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
