@@ -167,12 +167,27 @@ __global__ __launch_bounds__(kThreads) void scatter(BwdParams p) {
     const int64_t from = (int64_t)blockIdx.x * p.tile, to = min(from + p.tile, n);
     Keys<TOK, FIRST> keys;
     keys.load(p, from, to);
+    auto count_step = [&] {
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) at[w][d] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kPlaces; ++k)
+            if (keys.at[k] != kNone) atomicAdd(&at[wave][(keys.at[k] >> p.shift) & (kBins - 1)], 1u);
+        __syncthreads();
+    };
+    count_step();
     uint32_t total = 0, before = 0;
+    if (p.tiles == 1) {                                 // one workgroup and one step: its own counts are all there are
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) total += at[w][d];
+    } else {
 #pragma unroll 16
-    for (int g = 0; g < p.tiles; ++g) {
-        const uint32_t c = p.counts[g * kBins + d];
-        total += c;
-        before += g < (int)blockIdx.x ? c : 0u;
+        for (int g = 0; g < p.tiles; ++g) {
+            const uint32_t c = p.counts[g * kBins + d];
+            total += c;
+            before += g < (int)blockIdx.x ? c : 0u;
+        }
     }
     // the digits below: within the wave, then the waves before
     uint32_t below = total;
@@ -182,8 +197,6 @@ __global__ __launch_bounds__(kThreads) void scatter(BwdParams p) {
         below += lane >= off ? v : 0u;
     }
     if (lane == 63) waves[wave] = below;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) at[w][d] = 0;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) below += w < wave ? waves[w] : 0u;
@@ -194,14 +207,8 @@ __global__ __launch_bounds__(kThreads) void scatter(BwdParams p) {
         if (i0 > from) {
             keys.load(p, i0, to);
             __syncthreads();                            // the last step's places are taken
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) at[w][d] = 0;
-            __syncthreads();
+            count_step();
         }
-#pragma unroll
-        for (int k = 0; k < kPlaces; ++k)
-            if (keys.at[k] != kNone) atomicAdd(&at[wave][(keys.at[k] >> p.shift) & (kBins - 1)], 1u);
-        __syncthreads();
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
             const uint32_t c = at[w][d];

@@ -108,7 +108,7 @@ template <int TOK, int OUT> hipError_t embed_sort(mbs::embed::BwdParams &p, cons
     namespace E = mbs::embed;
     E::Pair *const ab[2] = {reinterpret_cast<E::Pair *>(ws + f.a), reinterpret_cast<E::Pair *>(ws + f.b)};
     // the table is set to zero in equal shares beside the launches of the sort; 16-byte shares keep the stores aligned
-    const int64_t elems = p.vocab * p.dim, launches = f.tiles > 0 ? 2 * f.passes : 1;
+    const int64_t elems = p.vocab * p.dim, launches = f.tiles == 0 ? 1 : f.tiles == 1 ? f.passes : 2 * f.passes;
     const int64_t share = ((elems + launches - 1) / launches + 63) / 64 * 64;
     const int64_t zeroing = std::min<int64_t>((share + 4095) / 4096, 2048);     // workgroups of at least 4,096 elements
     const dim3 grid((unsigned)(f.tiles + zeroing)), block(E::kThreads);
@@ -122,11 +122,14 @@ template <int TOK, int OUT> hipError_t embed_sort(mbs::embed::BwdParams &p, cons
         p.shift = 8 * k;
         p.from = k == 0 ? nullptr : ab[(k - 1) & 1];
         p.to = ab[k & 1];
-        next_share();
-        hipError_t e = hipLaunchKernel(k == 0 ? reinterpret_cast<const void *>(&E::count_digits<TOK, OUT, true>)
-                                              : reinterpret_cast<const void *>(&E::count_digits<TOK, OUT, false>),
-                                       grid, block, args, 0, st);
-        if (e != hipSuccess || f.tiles == 0) return e;
+        hipError_t e = hipSuccess;
+        if (f.tiles != 1) {
+            next_share();
+            e = hipLaunchKernel(k == 0 ? reinterpret_cast<const void *>(&E::count_digits<TOK, OUT, true>)
+                                       : reinterpret_cast<const void *>(&E::count_digits<TOK, OUT, false>),
+                                grid, block, args, 0, st);
+            if (e != hipSuccess || f.tiles == 0) return e;
+        }
         next_share();
         e = hipLaunchKernel(k == 0 ? reinterpret_cast<const void *>(&E::scatter<TOK, OUT, true>)
                                    : reinterpret_cast<const void *>(&E::scatter<TOK, OUT, false>),
@@ -170,16 +173,17 @@ bool sample_sizes(int64_t batch, int64_t ndraft, int64_t vocab) {
 
 // The pieces of a large vocabulary's rows; none for a small one's.
 struct SamplePlan {
-    int64_t pieces = 0, blocks = 0;
+    int64_t pieces = 0, race_pieces = 0, blocks = 0;
     size_t stats = 0, best = 0, bytes = 0;
     SamplePlan(int64_t batch, int64_t ndraft, int64_t vocab) {
         namespace S = mbs::sample;
         if (vocab <= S::kSmallVocab) return;
         pieces = (vocab + S::kPiece - 1) / S::kPiece;
+        race_pieces = (vocab + S::kRacePiece - 1) / S::kRacePiece;
         blocks = batch * (2 * ndraft + 1) * pieces;
         Areas w;
         stats = w.add((size_t)blocks * sizeof(float2));
-        best = w.add((size_t)(batch * pieces) * sizeof(S::Best));
+        best = w.add((size_t)(batch * race_pieces) * sizeof(S::Best));
         bytes = w.bytes;
     }
 };
@@ -197,13 +201,14 @@ template <int DT> hipError_t sample_launch(mbs::sample::Params &p, const SampleP
     Workspace ws(workspace, f.bytes, st);
     if (!ws.at) return hipErrorOutOfMemory;
     p.pieces = (int32_t)f.pieces;
+    p.race_pieces = (int32_t)f.race_pieces;
     p.stats = reinterpret_cast<float2 *>(ws.at + f.stats);
     p.best = reinterpret_cast<S::Best *>(ws.at + f.best);
     // without the drafter's logits its rows' workgroups end at once
     hipError_t e = hipLaunchKernel(reinterpret_cast<const void *>(&S::piece_stats<DT>), dim3((unsigned)f.blocks),
                                    dim3(S::kThreads), args, 0, st);
     if (e == hipSuccess)
-        e = hipLaunchKernel(reinterpret_cast<const void *>(&S::decide_and_race<DT>), dim3((unsigned)(p.batch * f.pieces)),
+        e = hipLaunchKernel(reinterpret_cast<const void *>(&S::decide_and_race<DT>), dim3((unsigned)(p.batch * f.race_pieces)),
                             dim3(S::kThreads), args, 0, st);
     if (e == hipSuccess)
         e = hipLaunchKernel(reinterpret_cast<const void *>(&S::join_races), dim3((unsigned)p.batch), dim3(64), args, 0, st);
@@ -561,7 +566,7 @@ int mb_verify_sample(int64_t batch, int64_t ndraft, int64_t vocab, int32_t logit
     const Range ins[] = {{logits, (size_t)elems * lsz}, {draft_logits, (size_t)(pairs * vocab) * lsz}, {draft, p_b},
                          {lengths, b_b}, {uniform, p_b}, {noise, (size_t)noises * 4}};
     const SamplePlan f(batch, ndraft, vocab);
-    if (f.blocks >= (int64_t(1) << 31)) return MB_ERR_SHAPE;
+    if (f.blocks >= (int64_t(1) << 23) || batch * f.race_pieces >= (int64_t(1) << 23)) return MB_ERR_SHAPE;
     if (!aligned(workspace, 16)) return MB_ERR_ALIGN;
     const Range outs[] = {{accepted, b_b}, {last_pos, b_b}, {next_token, b_b}, {probs, p_b}, {workspace, f.bytes}};
     if (any_overlap(outs, ins)) return MB_ERR_ALIAS;

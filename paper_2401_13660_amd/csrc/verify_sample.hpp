@@ -36,8 +36,10 @@ namespace sample {
 constexpr int kSmallVocab = 1024;
 constexpr int kMaxWaves = 16;
 constexpr int kThreads = 256;      // of a piece
-constexpr int kPieceSpans = 8;     // spans of 4 per thread
+constexpr int kPieceSpans = 8;     // spans of 4 per thread where maxima and sums are found
+constexpr int kRaceSpans = 2;      // and where the race is run, two exponentials and a division per token
 constexpr int kPiece = kThreads * kPieceSpans * 4;
+constexpr int kRacePiece = kThreads * kRaceSpans * 4;
 constexpr int32_t kNobody = 0x7fffffff;
 
 struct Best { float left, whole; int32_t left_at, whole_at; };
@@ -55,9 +57,9 @@ struct Params {
     int32_t *next_token;          // (batch)
     float *probs;                 // (batch, ndraft) or null: the target's of the drafted tokens
     float inv_temp;
-    int32_t pieces;               // per row, of a large vocabulary
+    int32_t pieces, race_pieces;  // per row, of a large vocabulary
     float2 *stats;                // (batch, 2 ndraft + 1, pieces): maximum and sum; the target's rows, then the drafter's
-    Best *best;                   // (batch, pieces)
+    Best *best;                   // (batch, race_pieces)
 };
 
 __device__ __forceinline__ int64_t length_of(const Params &p, int64_t b) {
@@ -240,14 +242,14 @@ __global__ __launch_bounds__(64 * kMaxWaves) void verify_small(Params p) {
 // ---- large vocabularies -----------------------------------------------------------
 
 // A thread's share of a piece: spans of 4, 256 threads side by side.
-template <int DT> struct PieceInLanes {
-    Span<DT, 4> s[kPieceSpans];
+template <int DT, int SPANS> struct PieceInLanes {
+    Span<DT, 4> s[SPANS];
     __device__ __forceinline__ static int token(int piece, int k) {
-        return piece * kPiece + (k * kThreads + (int)threadIdx.x) * 4;
+        return (piece * SPANS + k) * (kThreads * 4) + (int)threadIdx.x * 4;
     }
     __device__ __forceinline__ void load(const void *base, int64_t at, int piece, int64_t vocab) {
 #pragma unroll
-        for (int k = 0; k < kPieceSpans; ++k) {
+        for (int k = 0; k < SPANS; ++k) {
             const int64_t y = token(piece, k);
             if (y + 4 <= vocab) s[k].load(base, at + y);
             else s[k].load_first(base, at + y, (int)max(vocab - y, (int64_t)0));
@@ -275,7 +277,7 @@ __global__ __launch_bounds__(kThreads) void piece_stats(Params p) {
     const bool target = i <= p.ndraft;
     const int64_t at = target ? i : i - (p.ndraft + 1), len = length_of(p, b);
     if (target ? at > len : at >= len || !p.draft_logits) return;
-    PieceInLanes<DT> v;
+    PieceInLanes<DT, kPieceSpans> v;
     v.load(target ? p.logits : p.draft_logits, (target ? b * (p.ndraft + 1) + at : b * p.ndraft + at) * p.vocab, piece, p.vocab);
     float m = -__builtin_inff();
 #pragma unroll
@@ -296,99 +298,105 @@ __global__ __launch_bounds__(kThreads) void piece_stats(Params p) {
     if (threadIdx.x == 0) p.stats[row * p.pieces + piece] = make_float2(m, sum);
 }
 
-// Row i of a sequence (the target's first, then the drafter's) from its pieces.
+// Row i of a sequence (the target's first, then the drafter's) from its pieces; a wave's lanes together.
 __device__ __forceinline__ Row join_row(const Params &p, int64_t b, int64_t i) {
     const float2 *s = p.stats + (b * (2 * p.ndraft + 1) + i) * p.pieces;
+    const int lane = threadIdx.x & 63;
     float m = -__builtin_inff(), sum = 0.0f;
-    for (int k = 0; k < p.pieces; ++k) m = __builtin_fmaxf(m, s[k].x);
+    for (int k = lane; k < p.pieces; k += 64) m = __builtin_fmaxf(m, s[k].x);
+    m = wave_max(m);
     // a piece with nothing above -infinity adds nothing; one that holds a NaN or +infinity adds NaN
-    for (int k = 0; k < p.pieces; ++k) sum += s[k].y == 0.0f ? 0.0f : rounded_product(s[k].y, weight(s[k].x, m, p.inv_temp));
+    for (int k = lane; k < p.pieces; k += 64)
+        sum += s[k].y == 0.0f ? 0.0f : rounded_product(s[k].y, weight(s[k].x, m, p.inv_temp));
     Row r;
-    r.set(m, sum);
+    r.set(m, wave_sum(sum));
     return r;
 }
 
 template <int DT>
 __global__ __launch_bounds__(kThreads) void decide_and_race(Params p) {
     __shared__ int stop;
-    __shared__ float scores[2][kThreads / 64];
-    __shared__ int32_t who[2][kThreads / 64];
-    const int64_t b = blockIdx.x / p.pieces, n = p.ndraft, V = p.vocab;
-    const int piece = (int)(blockIdx.x - b * p.pieces);
+    __shared__ float scores[kThreads / 64];
+    __shared__ int32_t who[kThreads / 64];
+    const int64_t b = blockIdx.x / p.race_pieces, n = p.ndraft, V = p.vocab;
+    const int piece = (int)(blockIdx.x - b * p.race_pieces);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int len = (int)length_of(p, b);
     if (threadIdx.x == 0) stop = len;
+    PieceInLanes<0, kRaceSpans> e;
+    e.load(p.noise, b * V, piece, V);
     __syncthreads();
     const bool probs = p.probs && piece == 0;
-    for (int64_t i = threadIdx.x; i < (probs ? n : (int64_t)len); i += kThreads) {
-        float px = 0.0f;
-        if (i < len) {
-            const int64_t x = p.draft[b * n + i];
-            const Row t = join_row(p, b, i);
-            const bool valid = x >= 0 && x < V && t.ok;
-            if (valid) px = t.prob(Act<DT>::ld(p.logits, (b * (n + 1) + i) * V + x), p.inv_temp);
-            float qx = 1.0f;
-            bool ok = valid;
-            if (p.draft_logits) {
-                const Row q = join_row(p, b, n + 1 + i);
-                ok = valid && q.ok;
-                if (ok) qx = q.prob(Act<DT>::ld(p.draft_logits, (b * n + i) * V + x), p.inv_temp);
-            }
-            if (!(ok && p.uniform[b * n + i] * qx < px)) atomicMin(&stop, (int)i);
+    for (int i = wave; i < len; i += kThreads / 64) {   // a row per wave
+        const int64_t x = p.draft[b * n + i];
+        const bool in_range = x >= 0 && x < V;
+        const float u = p.uniform[b * n + i];
+        const float lx = in_range ? Act<DT>::ld(p.logits, (b * (n + 1) + i) * V + x) : 0.0f;
+        const float mx = in_range && p.draft_logits ? Act<DT>::ld(p.draft_logits, (b * n + i) * V + x) : 0.0f;
+        const Row t = join_row(p, b, i);
+        bool ok = in_range && t.ok;
+        const float px = ok ? t.prob(lx, p.inv_temp) : 0.0f;
+        float qx = 1.0f;
+        if (p.draft_logits) {
+            const Row q = join_row(p, b, n + 1 + i);
+            ok = ok && q.ok;
+            if (ok) qx = q.prob(mx, p.inv_temp);
         }
-        if (probs) p.probs[b * n + i] = px;
+        if (lane == 0) {
+            if (!(ok && u * qx < px)) atomicMin(&stop, i);
+            if (probs) p.probs[b * n + i] = px;
+        }
     }
+    if (probs)
+        for (int64_t i = len + (int64_t)threadIdx.x; i < n; i += kThreads) p.probs[b * n + i] = 0.0f;
     __syncthreads();
     const int c = stop;
     if (piece == 0 && threadIdx.x == 0) write_outcome(p, b, c);
 
+    const bool have_q = c < len && p.draft_logits;
+    PieceInLanes<DT, kRaceSpans> tl, ql;
+    tl.load(p.logits, (b * (n + 1) + c) * V, piece, V);
+    if (have_q) ql.load(p.draft_logits, (b * n + c) * V, piece, V);
+    const int64_t x = c < len && !p.draft_logits ? p.draft[b * n + c] : -1;
     const Row t = join_row(p, b, c);
-    Race left, whole;
-    if (t.ok) {
-        const bool have_q = c < len && p.draft_logits;
-        Row q;
-        if (have_q) q = join_row(p, b, n + 1 + c);
-        const bool less_q = have_q && q.ok;
-        const int64_t x = c < len && !p.draft_logits ? p.draft[b * n + c] : -1;
-        PieceInLanes<DT> tl, ql;
-        PieceInLanes<0> e;
-        tl.load(p.logits, (b * (n + 1) + c) * V, piece, V);
-        if (less_q) ql.load(p.draft_logits, (b * n + c) * V, piece, V);
-        e.load(p.noise, b * V, piece, V);
+    Row q;
+    if (have_q) q = join_row(p, b, n + 1 + c);
+    // the race of what is left of the target, or (second) of the target itself, within the workgroup
+    auto race = [&](bool whole) {
+        Race r;
+        if (t.ok) {
 #pragma unroll
-        for (int k = 0; k < kPieceSpans; ++k)
+            for (int k = 0; k < kRaceSpans; ++k)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int y = PieceInLanes<DT>::token(piece, k) + j;
-                if (y >= V) continue;
-                const float pr = t.prob(tl.s[k].get(j), p.inv_temp), noise = e.s[k].get(j);
-                whole.run(pr, noise, y);
-                left.run(less_q ? pr - q.prob(ql.s[k].get(j), p.inv_temp) : y == x ? 0.0f : pr, noise, y);
-            }
-    }
-    left.join_wave();
-    whole.join_wave();
-    const int wave = threadIdx.x >> 6;
-    if ((threadIdx.x & 63) == 0) {
-        scores[0][wave] = left.score;
-        scores[1][wave] = whole.score;
-        who[0][wave] = left.at;
-        who[1][wave] = whole.at;
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < kThreads / 64; ++w) {
-            left.join(scores[0][w], who[0][w]);
-            whole.join(scores[1][w], who[1][w]);
+                for (int j = 0; j < 4; ++j) {
+                    const int y = PieceInLanes<DT, kRaceSpans>::token(piece, k) + j;
+                    float left = t.prob(tl.s[k].get(j), p.inv_temp);
+                    if (!whole && q.ok) left -= q.prob(ql.s[k].get(j), p.inv_temp);
+                    if (!whole && y == x) left = 0.0f;
+                    r.run(y < V ? left : 0.0f, e.s[k].get(j), y);
+                }
         }
-        p.best[b * p.pieces + piece] = Best{left.score, whole.score, left.at, whole.at};
-    }
+        r.join_wave();
+        __syncthreads();
+        if (lane == 0) {
+            scores[wave] = r.score;
+            who[wave] = r.at;
+        }
+        __syncthreads();
+        for (int w = 0; w < kThreads / 64; ++w) r.join(scores[w], who[w]);
+        return r;
+    };
+    const Race left = race(false);
+    Race whole;
+    if (left.at == kNobody) whole = race(true);         // needed only where no piece of the row has anything left
+    if (threadIdx.x == 0) p.best[b * p.race_pieces + piece] = Best{left.score, whole.score, left.at, whole.at};
 }
 
 __global__ __launch_bounds__(64) void join_races(Params p) {
     const int64_t b = blockIdx.x;
     Race left, whole;
-    for (int k = threadIdx.x; k < p.pieces; k += 64) {
-        const Best o = p.best[b * p.pieces + k];
+    for (int k = threadIdx.x; k < p.race_pieces; k += 64) {
+        const Best o = p.best[b * p.race_pieces + k];
         left.join(o.left, o.left_at);
         whole.join(o.whole, o.whole_at);
     }
