@@ -352,7 +352,7 @@ typedef enum {
  * that the host cannot see: its row is NaN.
  *
  *   tokens  token_type (ntokens)      any leading shape, flattened
- *   weight  weight_dtype (vocab, dim) vocab below 2^31
+ *   weight  weight_dtype (vocab, dim) vocab below 2^31, and not 0 where there are tokens
  *   out     out_dtype (ntokens, dim)  must not overlap an input
  * One fp32 product per element, rounded once to out_dtype.
  */
@@ -392,8 +392,8 @@ int64_t mb_embedding_bwd_workspace(int64_t ntokens, int64_t vocab, int64_t dim);
  *   dbias       float (D)             required when bias is given, else ignored
  *   dstate_in   float (B, D, k-1)     NULL means not written
  * Outputs are overwritten (not accumulated) and must not overlap any other
- * argument; with no row or no timestep dw and dbias are zeros.  D, B * D and L
- * below 2^31.  Arithmetic is fp32; results are deterministic.
+ * argument; with no row or no timestep dw and dbias are zeros.  B * D below
+ * 2^26, D and L below 2^31.  Arithmetic is fp32; results are deterministic.
  *   workspace   as for mb_embedding_bwd, of mb_conv1d_bwd_workspace(desc) bytes
  */
 int mb_conv1d_bwd(const mb_conv_desc *desc, const void *x, const float *w, const float *bias, const float *state_in,
@@ -473,8 +473,9 @@ int mb_clip_grad_norm(int64_t count, const void *const *grads, void *const *out,
  *   temperature   > 0, it and its inverse finite (MB_ERR_UNSUPPORTED otherwise)
  *   workspace     as for mb_embedding_bwd, of mb_verify_sample_workspace(batch, ndraft, vocab) bytes
  *                 (none up to a vocabulary of 1,024)
- * Outputs must not overlap each other or the inputs.  vocab >= 1; batch and ndraft
- * below 2^31 - 16, vocab below 2^31 - 8192.  Probabilities are fp32.
+ * Outputs must not overlap each other or the inputs.  vocab >= 1, below
+ * 2^31 - 8192; batch below 2^22; batch * (2 ndraft + 1) * (vocab / 8192 + 1) below 2^23 where vocab
+ * is above 1,024.  Probabilities are fp32.
  */
 int mb_verify_sample(int64_t batch, int64_t ndraft, int64_t vocab, int32_t logit_dtype, float temperature,
                      const void *logits, const void *draft_logits, const int32_t *draft, const int32_t *lengths,

@@ -59,7 +59,8 @@ __device__ __forceinline__ float silu_slope(float pre) {
     return s * __builtin_fmaf(pre, 1.0f - s, 1.0f);
 }
 
-template <int IN, int OUT, int K>
+// CUT: L is no multiple of the span, so a row's last span is cut.
+template <int IN, int OUT, int K, bool CUT>
 __global__ __launch_bounds__(kThreads) void conv1d_bwd(Params p) {
     constexpr int H = K - 1, HH = H > 0 ? H : 1, S = kSpan<IN, OUT>, T = 64 * S;
     const int64_t L = p.seqlen, rows = p.batch * p.dim;
@@ -102,9 +103,9 @@ __global__ __launch_bounds__(kThreads) void conv1d_bwd(Params p) {
     float halo = 0.0f;                                          // lane j < H: the input H - j before the tile
     auto load = [&](int tile) {
         const int64_t t = (int64_t)tile * T + lane * S;
-        if ((int64_t)(tile + 1) * T <= L) {
-            xs.template load<true>(p.x, base + t);
-            ys.template load<true>(p.dy, base + t);
+        if (L >= S) {                                   // a span past the row's end: the last whole one, shifted below
+            xs.template load<true>(p.x, base + min(t, L - S));
+            ys.template load<true>(p.dy, base + min(t, L - S));
         } else {
             const int n = (int)max((int64_t)0, min(L - t, (int64_t)S));
             xs.load_first(p.x, base + t, n);
@@ -118,10 +119,27 @@ __global__ __launch_bounds__(kThreads) void conv1d_bwd(Params p) {
     for (int tile = last; tile >= first; --tile) {
         const int64_t t0 = (int64_t)tile * T + lane * S;
         float xin[H + S], g[S + HH];
+        const bool whole = (int64_t)(tile + 1) * T <= L;
 #pragma unroll
-        for (int i = 0; i < S; ++i) xin[H + i] = xs.get(i);
+        for (int i = 0; i < S; ++i) {
+            xin[H + i] = xs.get(i);
+            g[i] = ys.get(i);
+        }
+        if (!whole && L >= S) {
+            // zeros past the end; a cut span, read where the row's last whole one lies, moves to its place
+            const int64_t past = max(t0 + S - L, (int64_t)0);
 #pragma unroll
-        for (int i = 0; i < S; ++i) g[i] = ys.get(i);
+            for (int i = 0; i < S; ++i) {
+                float xi = 0.0f, gi = 0.0f;
+#pragma unroll
+                for (int k = i; k < (CUT ? S : i + 1); ++k) {
+                    xi = past == k - i ? xin[H + k] : xi;
+                    gi = past == k - i ? g[k] : gi;
+                }
+                xin[H + i] = xi;
+                g[i] = gi;
+            }
+        }
 #pragma unroll
         for (int j = 0; j < H; ++j) xin[j] = from_lane_before(xin[S + j], lane_value(halo, j));
         if (tile > first) load(tile - 1);
@@ -135,8 +153,7 @@ __global__ __launch_bounds__(kThreads) void conv1d_bwd(Params p) {
                 g[i] *= silu_slope(pre);
             }
         }
-        const bool whole = (int64_t)(tile + 1) * T <= L;
-        if (!whole) {
+        if (!whole) {                                   // nor does an infinity beside the end reach past it
 #pragma unroll
             for (int i = 0; i < S; ++i) g[i] = t0 + i < L ? g[i] : 0.0f;
         }
@@ -163,8 +180,8 @@ __global__ __launch_bounds__(kThreads) void conv1d_bwd(Params p) {
             for (int i = 0; i < S; ++i)
                 if (t0 + i >= L - H && t0 + i < L) dx[i] += p.dstate_out[row * H + t0 + i + H - L];
         }
-        if (whole) store_span<OUT, S, true>(p.dx, base + t0, dx);
-        else store_first<OUT, S>(p.dx, base + t0, dx, (int)max((int64_t)0, min(L - t0, (int64_t)S)));
+        if (t0 + S <= L) store_span<OUT, S, true>(p.dx, base + t0, dx);
+        else if (CUT) store_first<OUT, S>(p.dx, base + t0, dx, (int)max((int64_t)0, L - t0));
     }
 
     if (H > 0 && first == 0 && p.dstate_in && lane < H) {

@@ -168,6 +168,8 @@ template <int OUT> hipError_t embed_bwd(mbs::embed::BwdParams &p, const EmbedPla
 // Row and token numbers, and a last piece's tokens past the vocabulary, stay below 2^31.
 bool sample_sizes(int64_t batch, int64_t ndraft, int64_t vocab) {
     constexpr int64_t most = int64_t(1) << 31;
+    // and a launch has less than 2^32 threads
+    if (vocab <= mbs::sample::kSmallVocab && batch >= most / (32 * mbs::sample::kMaxWaves)) return false;
     return batch < most && ndraft < most - mbs::sample::kMaxWaves && vocab < most - mbs::sample::kPiece;
 }
 
@@ -230,20 +232,23 @@ template <int IN, int OUT, int K> hipError_t conv_bwd_k(mbs::convbwd::Params &p,
     hipError_t e = hipSuccess;
     const int64_t waves = p.batch * p.dim * p.nseg;
     if (waves > 0)
-        e = hipLaunchKernel(reinterpret_cast<const void *>(&C::conv1d_bwd<IN, OUT, K>),
+        e = hipLaunchKernel(p.seqlen % C::kSpan<IN, OUT> ? reinterpret_cast<const void *>(&C::conv1d_bwd<IN, OUT, K, true>)
+                                                         : reinterpret_cast<const void *>(&C::conv1d_bwd<IN, OUT, K, false>),
                             dim3((unsigned)((waves + C::kWaves - 1) / C::kWaves)), dim3(C::kThreads), args, 0, st);
     if (e != hipSuccess) return e;
     return hipLaunchKernel(reinterpret_cast<const void *>(&C::conv1d_bwd_finish<K>),
                            dim3((unsigned)((p.dim * (K + 1) + C::kThreads - 1) / C::kThreads)), dim3(C::kThreads), args, 0, st);
 }
 
-// Stretches per row: as many as bring the waves to 16 per SIMD.
+// Stretches per row: enough for 4 waves per SIMD.  (2, 1536, 1021) fp32 in one, two and four stretches per row took 13.6,
+// 11.7 and 13.6 us, (1, 2048, 2047) in two, four and eight 14.7, 16.6 and 18.1 (with the finish): more waves hide more
+// latency, but each computes its edge again and leaves partial sums.
 void conv_bwd_segments(mbs::convbwd::Params &p, int32_t in_dtype, int32_t out_dtype) {
     const int64_t span = in_dtype == MB_F32 && out_dtype == MB_F32 ? 4 : 8;
     const int64_t rows = p.batch * p.dim, tiles = std::max<int64_t>((p.seqlen + 64 * span - 1) / (64 * span), 1);
-    const int64_t want = 4 * 256 * 16;
-    const int64_t n = std::min(tiles, std::max<int64_t>(1, want / std::max<int64_t>(rows, 1)));
-    p.seg_tiles = (int32_t)((tiles + n - 1) / n);
+    const int64_t want = 4 * 256 * 4;
+    const int64_t n = std::min(tiles, (want + rows - 1) / std::max<int64_t>(rows, 1));
+    p.seg_tiles = (int32_t)((tiles + n - 1) / std::max<int64_t>(n, 1));
     p.nseg = (tiles + p.seg_tiles - 1) / p.seg_tiles;
 }
 
@@ -477,6 +482,8 @@ int mb_conv1d_bwd(const mb_conv_desc *desc, const void *x, const float *w, const
     mbs::convbwd::Params p{};
     p.batch = B; p.dim = D; p.seqlen = L;
     conv_bwd_segments(p, desc->in_dtype, desc->out_dtype);
+    // a wave per row and stretch, and at most 2^32 threads in a launch
+    if (rows * p.nseg >= (int64_t(1) << 26)) return MB_ERR_SHAPE;
     const size_t part_b = (size_t)(padded * p.nseg) * 4;
     if (!aligned(workspace, 16)) return MB_ERR_ALIGN;
     const Range outs[] = {{dx, (size_t)elems * out_sz}, {dw, w_b}, {dbias, bias ? b_b : 0}, {dstate_in, st_b},

@@ -20,7 +20,7 @@ P = {k: 0x100000000 * (i + 1) for i, k in enumerate(
 @no_gpu_only
 @pytest.mark.parametrize("name", ["mb_embedding_fwd", "mb_embedding_bwd"])
 @pytest.mark.parametrize("over,code", [
-    (dict(n=-1), -2), (dict(V=-1), -2), (dict(V=1 << 31), -2), (dict(n=1 << 50, d=1 << 20), -2),
+    (dict(n=-1), -2), (dict(V=-1), -2), (dict(V=1 << 31), -2), (dict(n=1 << 31), -2), (dict(n=1 << 50, d=1 << 20), -2),
     (dict(tok=3), -3), (dict(it=2), -3), (dict(ot=-1), -3),
     (dict(a=None), -1), (dict(b=None), -1), (dict(c=None), -1),
     (dict(a=P["tokens"] + 2), -4), (dict(b=P["weight"] + 1), -4), (dict(c=P["out"] + 2), -4),
@@ -44,7 +44,7 @@ def test_embedding_empty():
 @no_gpu_only
 @pytest.mark.parametrize("desc,over,code", [
     (None, {}, -1),
-    (dict(batch=-1), {}, -2), (dict(seqlen=-1), {}, -2), (dict(seqlen=1 << 31), {}, -2), (dict(dim=1 << 31), {}, -2),
+    (dict(batch=-1), {}, -2), (dict(seqlen=-1), {}, -2), (dict(seqlen=1 << 31), {}, -2), (dict(dim=1 << 31), {}, -2), (dict(dim=1 << 25), {}, -2),
     (dict(in_dtype=5), {}, -3), (dict(out_dtype=5), {}, -3),
     (dict(width=0), {}, -5), (dict(width=5), {}, -5), (dict(reserved=1), {}, -5), (dict(reserved2=1), {}, -5),
     ({}, dict(x=None), -1), ({}, dict(w=None), -1), ({}, dict(dy=None), -1), ({}, dict(dx=None), -1),
@@ -143,7 +143,7 @@ def test_workspaces():
 @no_gpu_only
 @pytest.mark.parametrize("over,code", [
     (dict(b=-1), -2), (dict(n=-1), -2), (dict(V=0), -2), (dict(V=(1 << 31) - 1), -2), (dict(n=(1 << 31) - 1), -2),
-    (dict(b=1 << 31), -2), (dict(b=1 << 30, n=1 << 20, V=1 << 20), -2), (dict(dt=2), -3),
+    (dict(b=1 << 31), -2), (dict(b=1 << 22), -2), (dict(b=1 << 20, n=4, V=2000), -2), (dict(b=1 << 30, n=1 << 20, V=1 << 20), -2), (dict(dt=2), -3),
     (dict(T=0.0), -5), (dict(T=-1.0), -5), (dict(T=float("nan")), -5), (dict(T=float("inf")), -5), (dict(T=1e-44), -5),
     (dict(logits=None), -1), (dict(noise=None), -1), (dict(draft=None), -1), (dict(uniform=None), -1),
     (dict(accepted=None), -1), (dict(next=None), -1),
