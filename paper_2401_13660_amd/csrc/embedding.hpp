@@ -44,9 +44,10 @@ struct BwdParams {
     void *dweight;
     float scale;
     int32_t tile;                  // tokens per workgroup of the sort
-    int32_t tiles;                 // workgroups of the sort, at most kBins
+    int32_t tiles;                 // workgroups of the sort, at most kBins (1: sort_small)
     int32_t chunk;                 // sorted positions per wave
     int64_t zero_from, zero_to;    // elements of dweight that the launch sets to zero on the side
+    int32_t passes;                // 8 bits each
     int32_t shift;                 // bits below this pass's digit
     uint32_t *counts;              // (tiles, kBins)
     uint32_t *valid;               // tokens within the vocabulary
@@ -128,12 +129,23 @@ template <int TOK, bool FIRST> struct Keys {
 // chip to it.
 template <int OUT> __device__ __forceinline__ void zero_share(const BwdParams &p) {
     constexpr int S = OUT == 1 ? 8 : 4;
-    const int64_t step = (int64_t)(gridDim.x - p.tiles) * kThreads * S;
+    const int64_t step = (int64_t)(gridDim.x - p.tiles) * blockDim.x * S;
     const float zeros[S] = {};
-    for (int64_t i = p.zero_from + ((int64_t)(blockIdx.x - p.tiles) * kThreads + threadIdx.x) * S; i < p.zero_to; i += step) {
+    for (int64_t i = p.zero_from + ((int64_t)(blockIdx.x - p.tiles) * blockDim.x + threadIdx.x) * S; i < p.zero_to; i += step) {
         if (i + S <= p.zero_to) store_span<OUT, S>(p.dweight, i, zeros);
         else store_first<OUT, S>(p.dweight, i, zeros, (int)(p.zero_to - i));
     }
+}
+
+// The lanes whose digit is this lane's, of those that have one.
+__device__ __forceinline__ uint64_t same_digit(uint32_t digit, bool has) {
+    uint64_t same = __ballot(has);
+#pragma unroll
+    for (int b = 0; b < 8; ++b) {
+        const uint64_t set = __ballot((digit >> b) & 1);
+        same &= (digit >> b) & 1 ? set : ~set;
+    }
+    return same;
 }
 
 // Digits of the workgroup's places, counted.
@@ -178,16 +190,11 @@ __global__ __launch_bounds__(kThreads) void scatter(BwdParams p) {
     };
     count_step();
     uint32_t total = 0, before = 0;
-    if (p.tiles == 1) {                                 // one workgroup and one step: its own counts are all there are
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) total += at[w][d];
-    } else {
 #pragma unroll 16
-        for (int g = 0; g < p.tiles; ++g) {
-            const uint32_t c = p.counts[g * kBins + d];
-            total += c;
-            before += g < (int)blockIdx.x ? c : 0u;
-        }
+    for (int g = 0; g < p.tiles; ++g) {
+        const uint32_t c = p.counts[g * kBins + d];
+        total += c;
+        before += g < (int)blockIdx.x ? c : 0u;
     }
     // the digits below: within the wave, then the waves before
     uint32_t below = total;
@@ -220,13 +227,7 @@ __global__ __launch_bounds__(kThreads) void scatter(BwdParams p) {
         for (int k = 0; k < kPlaces; ++k) {
             const int64_t key = keys.at[k];
             const uint32_t digit = (uint32_t)(key >> p.shift) & (kBins - 1);
-            // the lanes of the same digit
-            uint64_t same = __ballot(key != kNone);
-#pragma unroll
-            for (int b = 0; b < 8; ++b) {
-                const uint64_t set = __ballot((digit >> b) & 1);
-                same &= (digit >> b) & 1 ? set : ~set;
-            }
+            const uint64_t same = same_digit(digit, key != kNone);
             if (key != kNone) {
                 const int first = __ffsll((unsigned long long)same) - 1;
                 uint32_t base = 0;
@@ -236,6 +237,99 @@ __global__ __launch_bounds__(kThreads) void scatter(BwdParams p) {
                 p.to[base + __popcll(same & ((1ull << lane) - 1))] = Pair{(uint32_t)key, FIRST ? (uint32_t)i : p.from[i].pos};
             }
         }
+    }
+}
+
+// The whole sort by one workgroup, for up to kSmallTokens: places in registers, moved through LDS between the passes.
+// The other workgroups set the table to zero meanwhile.  4,096 tokens take 7 us of bytes and 10.7 of 30,000 values, 1,000
+// bytes 5; the launches above take about 9 and 21, and two or four times the host's time.  16 places per thread took
+// 21.5 us for 16,384 bytes: one CU's issue rate, where the launches above spread over many.
+constexpr int kSmallThreads = 1024;
+constexpr int kSmallWaves = kSmallThreads / 64;
+constexpr int kSmallPlaces = 4;
+constexpr int kSmallTokens = kSmallThreads * kSmallPlaces;
+
+template <int TOK, int OUT>
+__global__ __launch_bounds__(kSmallThreads) void sort_small(BwdParams p) {
+    constexpr int PER = kSmallPlaces;
+    if (blockIdx.x >= 1) return zero_share<OUT>(p);
+    __shared__ uint32_t keys[kSmallTokens];
+    __shared__ uint16_t places[kSmallTokens];
+    __shared__ uint32_t at[kSmallWaves][kBins], waves[kBins / 64];
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const int mine = wave * (64 * PER) + lane;                  // the wave's places, 64 side by side
+    int n = (int)p.ntokens;
+    constexpr uint32_t kNoKey = ~0u;                            // keys are below 2^31
+    uint32_t key[PER], pos[PER], rank[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        pos[k] = mine + 64 * k;
+        key[k] = (int)pos[k] < n ? (uint32_t)key_at<TOK, true>(p, pos[k]) : kNoKey;
+    }
+    for (int pass = 0; pass < p.passes; ++pass) {
+        const int shift = 8 * pass;
+        for (int i = lane; i < kBins; i += 64) at[wave][i] = 0;
+        __builtin_amdgcn_wave_barrier();                        // a wave's own counts, in its own order
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const uint32_t digit = (key[k] >> shift) & (kBins - 1);
+            const uint64_t same = same_digit(digit, key[k] != kNoKey);
+            const int first = same ? __ffsll((unsigned long long)same) - 1 : lane;
+            uint32_t base = 0;
+            if (key[k] != kNoKey && lane == first) base = atomicAdd(&at[wave][digit], (uint32_t)__popcll(same));
+            rank[k] = __shfl(base, first, 64) + __popcll(same & ((1ull << lane) - 1));
+        }
+        __syncthreads();
+        // thread d: where digit d of each wave goes
+        uint32_t total = 0, below = 0;
+        if (tid < kBins) {
+#pragma unroll
+            for (int w = 0; w < kSmallWaves; ++w) total += at[w][tid];
+            below = total;
+#pragma unroll
+            for (int off = 1; off < 64; off *= 2) {
+                const uint32_t v = __shfl_up(below, off, 64);
+                below += lane >= off ? v : 0u;
+            }
+            if (lane == 63) waves[wave] = below;
+        }
+        __syncthreads();
+        if (tid < kBins) {
+#pragma unroll
+            for (int w = 0; w < kBins / 64; ++w) below += w < wave ? waves[w] : 0u;
+            if (pass == 0 && tid == kBins - 1) *p.valid = below;
+            below -= total;
+#pragma unroll
+            for (int w = 0; w < kSmallWaves; ++w) {
+                const uint32_t c = at[w][tid];
+                at[w][tid] = below;
+                below += c;
+            }
+        }
+        __syncthreads();
+        if (pass + 1 == p.passes) {
+#pragma unroll
+            for (int k = 0; k < PER; ++k)
+                if (key[k] != kNoKey)
+                    p.to[at[wave][(key[k] >> shift) & (kBins - 1)] + rank[k]] = Pair{key[k], pos[k]};
+            return;
+        }
+        if (pass == 0) n = (int)(waves[0] + waves[1] + waves[2] + waves[3]);
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+            if (key[k] != kNoKey) {
+                const uint32_t dest = at[wave][(key[k] >> shift) & (kBins - 1)] + rank[k];
+                keys[dest] = key[k];
+                places[dest] = (uint16_t)pos[k];
+            }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const int i = mine + 64 * k;
+            key[k] = i < n ? keys[i] : kNoKey;
+            pos[k] = i < n ? places[i] : 0u;
+        }
+        __syncthreads();
     }
 }
 

@@ -87,6 +87,7 @@ struct EmbedPlan {
         // tokens per workgroup: 1,024, or what keeps the workgroups at kBins (each reads the counts of all)
         tile = std::max<int64_t>(1024, ((ntokens + E::kBins - 1) / E::kBins + 1023) / 1024 * 1024);
         tiles = (ntokens + tile - 1) / tile;
+        if (ntokens > 0 && ntokens <= E::kSmallTokens) tiles = 1;       // sorted by one workgroup at once
         passes = 1;
         while (passes < 4 && (vocab - 1) >> (8 * passes)) ++passes;
         // sorted positions per wave: 64, or fewer where that leaves the SIMDs with less than two waves
@@ -108,7 +109,7 @@ template <int TOK, int OUT> hipError_t embed_sort(mbs::embed::BwdParams &p, cons
     namespace E = mbs::embed;
     E::Pair *const ab[2] = {reinterpret_cast<E::Pair *>(ws + f.a), reinterpret_cast<E::Pair *>(ws + f.b)};
     // the table is set to zero in equal shares beside the launches of the sort; 16-byte shares keep the stores aligned
-    const int64_t elems = p.vocab * p.dim, launches = f.tiles == 0 ? 1 : f.tiles == 1 ? f.passes : 2 * f.passes;
+    const int64_t elems = p.vocab * p.dim, launches = f.tiles > 1 ? 2 * f.passes : 1;
     const int64_t share = ((elems + launches - 1) / launches + 63) / 64 * 64;
     const int64_t zeroing = std::min<int64_t>((share + 4095) / 4096, 2048);     // workgroups of at least 4,096 elements
     const dim3 grid((unsigned)(f.tiles + zeroing)), block(E::kThreads);
@@ -118,18 +119,23 @@ template <int TOK, int OUT> hipError_t embed_sort(mbs::embed::BwdParams &p, cons
         p.zero_to = std::min(p.zero_from + share, elems);
     };
     void *args[] = {&p};
+    if (f.tiles <= 1) {
+        // its workgroups are four times as large, so a fourth as many zero the table
+        next_share();
+        p.to = ab[0];
+        const dim3 small(1 + (unsigned)((zeroing + 3) / 4));
+        p.tiles = 1;
+        return hipLaunchKernel(reinterpret_cast<const void *>(&E::sort_small<TOK, OUT>), small, dim3(E::kSmallThreads), args, 0, st);
+    }
     for (int k = 0; k < f.passes; ++k) {
         p.shift = 8 * k;
         p.from = k == 0 ? nullptr : ab[(k - 1) & 1];
         p.to = ab[k & 1];
-        hipError_t e = hipSuccess;
-        if (f.tiles != 1) {
-            next_share();
-            e = hipLaunchKernel(k == 0 ? reinterpret_cast<const void *>(&E::count_digits<TOK, OUT, true>)
-                                       : reinterpret_cast<const void *>(&E::count_digits<TOK, OUT, false>),
-                                grid, block, args, 0, st);
-            if (e != hipSuccess || f.tiles == 0) return e;
-        }
+        next_share();
+        hipError_t e = hipLaunchKernel(k == 0 ? reinterpret_cast<const void *>(&E::count_digits<TOK, OUT, true>)
+                                              : reinterpret_cast<const void *>(&E::count_digits<TOK, OUT, false>),
+                                       grid, block, args, 0, st);
+        if (e != hipSuccess) return e;
         next_share();
         e = hipLaunchKernel(k == 0 ? reinterpret_cast<const void *>(&E::scatter<TOK, OUT, true>)
                                    : reinterpret_cast<const void *>(&E::scatter<TOK, OUT, false>),
@@ -439,6 +445,7 @@ int mb_embedding_bwd(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_
     mbs::embed::BwdParams p{};
     p.ntokens = ntokens; p.vocab = vocab; p.dim = dim;
     p.tokens = tokens; p.dy = dy; p.dweight = dweight; p.scale = scale;
+    p.passes = f.passes;
     p.tile = (int32_t)f.tile; p.tiles = (int32_t)f.tiles; p.chunk = (int32_t)f.chunk;
     p.counts = reinterpret_cast<uint32_t *>(ws.at + f.counts);
     p.valid = reinterpret_cast<uint32_t *>(ws.at + f.valid);
