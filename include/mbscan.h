@@ -352,7 +352,7 @@ typedef enum {
  * that the host cannot see: its row is NaN.
  *
  *   tokens  token_type (ntokens)      any leading shape, flattened
- *   weight  weight_dtype (vocab, dim) vocab below 2^31, and not 0 where there are tokens
+ *   weight  weight_dtype (vocab, dim) vocab below 2^31, and not 0 where there are tokens; dim below 2^30
  *   out     out_dtype (ntokens, dim)  must not overlap an input
  * One fp32 product per element, rounded once to out_dtype.
  */
@@ -370,7 +370,7 @@ int mb_embedding_fwd(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_
  *
  *   tokens  token_type (ntokens)       ntokens below 2^31
  *   dy      dy_dtype (ntokens, dim)
- *   dweight out_dtype (vocab, dim)     must not overlap an input
+ *   dweight out_dtype (vocab, dim)     must not overlap an input; ntokens * dim below 2^37
  *   workspace  device memory of mb_embedding_bwd_workspace(ntokens, vocab, dim) bytes (of a
  *              negative mb_status where the sizes are refused), 16-byte aligned, that nothing else
  *              uses until the call's work is done; NULL: the call allocates it on the stream

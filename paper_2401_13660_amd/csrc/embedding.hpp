@@ -11,6 +11,13 @@
 // of columns, each row read once, and writes a token's sum where all of its rows lie in the chunk;
 // the sums of a token that goes on into other chunks are joined afterwards in the order of the
 // chunks.  No atomic adds floats: a result depends on the tokens and dy alone.
+//
+// 32,768 bytes of a text, width 1792 in bf16: 34 us, of which the sums take 22.4 (5.2 TB/s, the rate of
+// a device copy), the sort's two launches 9 and the joining 4.4, a chain of loads each.  16,384 tokens
+// of a table of 32,000 rows of 768 fp32: 45 us, four launches of the sort at 6 to 7.5 (a quarter of
+// the table's 98 MB zeroed beside each), the sums 14.5 and the joining 4.  With the next pass's digits
+// counted by atomics in the launch before, three launches of the sort took 33 us instead of 28: equal
+// tokens meet in one counter.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -68,36 +75,37 @@ template <int TOK> __device__ __forceinline__ int64_t token_at(const void *p, in
 // row, so that none is cut (what two spans share they both hold the same of).  Rows shorter than a span take spans of one.
 template <int S> __device__ __forceinline__ int64_t span_at(int64_t col, int64_t dim) { return min(col, dim - S); }
 
-// A workgroup takes p.rows rows, as spans side by side.
+// A workgroup takes p.rows rows at a time, as spans side by side.  Bound by the writes: 32,768 rows of 1,792 bf16 take
+// 20.5 us, 5.8 TB/s with what the Infinity Cache takes of them; 32 rows 3 us, the chain of a token, its row and a store.
 template <int TOK, int W, int OUT, int S>
 __global__ __launch_bounds__(kThreads) void embed_fwd(FwdParams p) {
     constexpr int PER = 4;
-    const int64_t row0 = (int64_t)blockIdx.x * p.rows;
     const uint32_t spans = (uint32_t)((p.dim + S - 1) / S);
-    const uint32_t items = (uint32_t)min((int64_t)p.rows, p.ntokens - row0) * spans;
-    for (uint32_t i0 = threadIdx.x; i0 < items; i0 += PER * kThreads) {
-        int64_t row[PER], t[PER];
-        int64_t col[PER];
-        Span<W, S> s[PER];
+    for (int64_t row0 = (int64_t)blockIdx.x * p.rows; row0 < p.ntokens; row0 += (int64_t)gridDim.x * p.rows) {
+        const uint32_t items = (uint32_t)min((int64_t)p.rows, p.ntokens - row0) * spans;
+        for (uint32_t i0 = threadIdx.x; i0 < items; i0 += PER * kThreads) {
+            int64_t row[PER], t[PER], col[PER];
+            Span<W, S> s[PER];
 #pragma unroll
-        for (int k = 0; k < PER; ++k) {
-            const uint32_t i = min(i0 + k * kThreads, items - 1);       // past the end: the last one again, not stored
-            const uint32_t r = i / spans;
-            row[k] = row0 + r;
-            col[k] = span_at<S>((int64_t)(i - r * spans) * S, p.dim);
-            t[k] = token_at<TOK>(p.tokens, row[k]);
-        }
+            for (int k = 0; k < PER; ++k) {
+                const uint32_t i = min(i0 + k * kThreads, items - 1);   // past the end: the last one again, not stored
+                const uint32_t r = i / spans;
+                row[k] = row0 + r;
+                col[k] = span_at<S>((int64_t)(i - r * spans) * S, p.dim);
+                t[k] = token_at<TOK>(p.tokens, row[k]);
+            }
 #pragma unroll
-        for (int k = 0; k < PER; ++k) {
-            s[k].load(p.weight, (t[k] >= 0 && t[k] < p.vocab ? t[k] : 0) * p.dim + col[k]);
-        }
+            for (int k = 0; k < PER; ++k)
+                s[k].load(p.weight, (t[k] >= 0 && t[k] < p.vocab ? t[k] : 0) * p.dim + col[k]);
 #pragma unroll
-        for (int k = 0; k < PER; ++k) {
-            if (i0 + k * kThreads >= items) break;
-            float v[S];
+            for (int k = 0; k < PER; ++k) {
+                if (i0 + k * kThreads >= items) break;
+                float v[S];
 #pragma unroll
-            for (int j = 0; j < S; ++j) v[j] = t[k] < 0 ? 0.0f : t[k] < p.vocab ? p.scale * s[k].get(j) : __builtin_nanf("");
-            store_span<OUT, S>(p.out, row[k] * p.dim + col[k], v);
+                for (int j = 0; j < S; ++j)
+                    v[j] = t[k] < 0 ? 0.0f : t[k] < p.vocab ? p.scale * s[k].get(j) : __builtin_nanf("");
+                store_span<OUT, S>(p.out, row[k] * p.dim + col[k], v);
+            }
         }
     }
 }

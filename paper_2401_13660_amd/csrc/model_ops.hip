@@ -417,8 +417,8 @@ int mb_embedding_fwd(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_
     // spans of a row, and rows per workgroup: 1,024 spans where that leaves 2,048 workgroups
     const int64_t spans = (dim + span - 1) / span;
     const int64_t rows = std::max<int64_t>(1, std::min(1024 / spans, ntokens / 2048));
-    const int64_t blocks = (ntokens + rows - 1) / rows;
-    if (spans >= (int64_t(1) << 31) || blocks >= (int64_t(1) << 24)) return MB_ERR_SHAPE;
+    const int64_t blocks = std::min<int64_t>((ntokens + rows - 1) / rows, 1 << 20);
+    if (spans >= (int64_t(1) << 30)) return MB_ERR_SHAPE;
     mbs::embed::FwdParams p{ntokens, vocab, dim, tokens, weight, out, scale, (int32_t)rows};
     return status(launch(fn, dim3((unsigned)blocks), dim3(mbs::embed::kThreads), &p, stream));
 }
