@@ -59,7 +59,50 @@ __device__ __forceinline__ float silu_slope(float pre) {
     return s * __builtin_fmaf(pre, 1.0f - s, 1.0f);
 }
 
-// CUT: L is no multiple of the span, so a row's last span is cut.
+// A span with the row's end in it or before it: zeros past the end.  It was read where the row's last whole span lies (L
+// at least S), `past` elements early, and moves to its place; without CUT that is by all of S or not at all.
+template <int S, bool CUT> __device__ __forceinline__ void end_span(float *v, int64_t past) {
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+        float r = 0.0f;
+#pragma unroll
+        for (int k = i; k < (CUT ? S : i + 1); ++k) r = past == k - i ? v[k] : r;
+        v[i] = r;
+    }
+}
+
+// g from dy, in place; xin: the H inputs before the span and the span's.
+template <int S, int K> __device__ __forceinline__ void through_swish(float *g, const float *xin, const float *w, float bias) {
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+        float pre = bias;
+#pragma unroll
+        for (int j = 0; j < K; ++j) pre = __builtin_fmaf(w[j], xin[i + j], pre);
+        g[i] *= silu_slope(pre);
+    }
+}
+
+template <int S, int K> __device__ __forceinline__ void add_products(float *acc, const float *g, const float *xin) {
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+#pragma unroll
+        for (int j = 0; j < K; ++j) acc[j] = __builtin_fmaf(g[i], xin[i + j], acc[j]);
+        acc[K] += g[i];
+    }
+}
+
+// dx of a span from its g and the H values after it.
+template <int S, int K> __device__ __forceinline__ void back_through_taps(float (&dx)[S], const float *g, const float *w) {
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+        dx[i] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < K; ++j) dx[i] = __builtin_fmaf(w[j], g[i + K - 1 - j], dx[i]);
+    }
+}
+
+// CUT: L is no multiple of the span, so a row's last span is cut.  The instantiations without need 91 to 97 registers, 5
+// waves per SIMD; with it up to 119, and 4.
 template <int IN, int OUT, int K, bool CUT>
 __global__ __launch_bounds__(kThreads) void conv1d_bwd(Params p) {
     constexpr int H = K - 1, HH = H > 0 ? H : 1, S = kSpan<IN, OUT>, T = 64 * S;
@@ -126,55 +169,27 @@ __global__ __launch_bounds__(kThreads) void conv1d_bwd(Params p) {
             g[i] = ys.get(i);
         }
         if (!whole && L >= S) {
-            // zeros past the end; a cut span, read where the row's last whole one lies, moves to its place
             const int64_t past = max(t0 + S - L, (int64_t)0);
-#pragma unroll
-            for (int i = 0; i < S; ++i) {
-                float xi = 0.0f, gi = 0.0f;
-#pragma unroll
-                for (int k = i; k < (CUT ? S : i + 1); ++k) {
-                    xi = past == k - i ? xin[H + k] : xi;
-                    gi = past == k - i ? g[k] : gi;
-                }
-                xin[H + i] = xi;
-                g[i] = gi;
-            }
+            end_span<S, CUT>(xin + H, past);
+            end_span<S, CUT>(g, past);
         }
 #pragma unroll
         for (int j = 0; j < H; ++j) xin[j] = from_lane_before(xin[S + j], lane_value(halo, j));
         if (tile > first) load(tile - 1);
 
-        if (p.apply_silu) {
-#pragma unroll
-            for (int i = 0; i < S; ++i) {
-                float pre = bias;
-#pragma unroll
-                for (int j = 0; j < K; ++j) pre = __builtin_fmaf(w[j], xin[i + j], pre);
-                g[i] *= silu_slope(pre);
-            }
-        }
+        if (p.apply_silu) through_swish<S, K>(g, xin, w, bias);
         if (!whole) {                                   // nor does an infinity beside the end reach past it
 #pragma unroll
             for (int i = 0; i < S; ++i) g[i] = t0 + i < L ? g[i] : 0.0f;
         }
-#pragma unroll
-        for (int i = 0; i < S; ++i) {
-#pragma unroll
-            for (int j = 0; j < K; ++j) acc[j] = __builtin_fmaf(g[i], xin[i + j], acc[j]);
-            acc[K] += g[i];
-        }
+        add_products<S, K>(acc, g, xin);
 #pragma unroll
         for (int j = 0; j < H; ++j) {
             g[S + j] = from_lane_after(g[j], carry[j]);
             carry[j] = lane_value(g[j], 0);
         }
         float dx[S];
-#pragma unroll
-        for (int i = 0; i < S; ++i) {
-            dx[i] = 0.0f;
-#pragma unroll
-            for (int j = 0; j < K; ++j) dx[i] = __builtin_fmaf(w[j], g[i + H - j], dx[i]);
-        }
+        back_through_taps<S, K>(dx, g, w);
         if (H > 0 && p.dstate_out && (int64_t)(tile + 1) * T > L - H) {
 #pragma unroll
             for (int i = 0; i < S; ++i)
@@ -197,6 +212,89 @@ __global__ __launch_bounds__(kThreads) void conv1d_bwd(Params p) {
     for (int j = 0; j <= K; ++j) {
         const float s = wave_sum(acc[j]);
         if (lane == j) p.part[item * (K + 1) + j] = s;
+    }
+}
+
+// Rows of at most G spans: 64 / G of them side by side in a wave, each whole in its lanes.  (4, 4608, 64) bf16 takes 11
+// us with the finish, a row in each wave took 19; (64, 3584, 16) 41 and 161; (4, 4608, 257), a row in each wave either
+// way, 18 and 25 in the walk above, which has the edges of its stretches to look after.
+template <int IN, int OUT, int K, int G>
+__global__ __launch_bounds__(kThreads) void conv1d_bwd_short(Params p) {
+    constexpr int H = K - 1, HH = H > 0 ? H : 1, S = kSpan<IN, OUT>;
+    const int64_t L = p.seqlen, rows = p.batch * p.dim;
+    const int lane = threadIdx.x & 63, l = lane & (G - 1);
+    const int64_t asked = ((int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6)) * (64 / G) + lane / G;
+    const bool active = asked < rows;                   // lanes without a row do the last one's work and write nothing
+    const int64_t row = active ? asked : rows - 1, d = row % p.dim, base = row * L, t0 = (int64_t)l * S;
+    Span<IN, S> xs;
+    Span<OUT, S> ys;
+    if (L >= S) {
+        xs.load(p.x, base + min(t0, L - S));
+        ys.load(p.dy, base + min(t0, L - S));
+    } else {
+        const int n = (int)max((int64_t)0, L - t0);
+        xs.load_first(p.x, base + (n > 0 ? t0 : 0), n);
+        ys.load_first(p.dy, base + (n > 0 ? t0 : 0), n);
+    }
+    float w[K], first[HH] = {};
+#pragma unroll
+    for (int j = 0; j < K; ++j) w[j] = p.w[d * K + j];
+    const float bias = p.bias ? p.bias[d] : 0.0f;
+    if (p.state_in) {
+#pragma unroll
+        for (int j = 0; j < H; ++j) first[j] = p.state_in[row * H + j];
+    }
+    float xin[H + S], g[S + HH], acc[K + 1] = {}, dx[S];
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+        xin[H + i] = xs.get(i);
+        g[i] = ys.get(i);
+    }
+    if (L >= S) {
+        const int64_t past = max(t0 + S - L, (int64_t)0);
+        end_span<S, true>(xin + H, past);
+        end_span<S, true>(g, past);
+    }
+#pragma unroll
+    for (int j = 0; j < H; ++j) {
+        const float v = from_lane_before(xin[S + j], 0.0f);
+        xin[j] = l == 0 ? first[j] : v;
+    }
+    if (p.apply_silu) through_swish<S, K>(g, xin, w, bias);
+#pragma unroll
+    for (int i = 0; i < S; ++i) g[i] = t0 + i < L ? g[i] : 0.0f;
+    add_products<S, K>(acc, g, xin);
+#pragma unroll
+    for (int j = 0; j < H; ++j) {
+        const float v = from_lane_after(g[j], 0.0f);
+        g[S + j] = l == G - 1 ? 0.0f : v;
+    }
+    back_through_taps<S, K>(dx, g, w);
+    if (H > 0 && p.dstate_out) {
+#pragma unroll
+        for (int i = 0; i < S; ++i)
+            if (t0 + i >= L - H && t0 + i < L) dx[i] += p.dstate_out[row * H + t0 + i + H - L];
+    }
+    if (active && t0 < L) {
+        if (t0 + S <= L) store_span<OUT, S>(p.dx, base + t0, dx);
+        else store_first<OUT, S>(p.dx, base + t0, dx, (int)(L - t0));
+    }
+    if (H > 0 && p.dstate_in) {
+        float v = p.dstate_out && l >= L && l < H ? p.dstate_out[row * H + l - L] : 0.0f;
+#pragma unroll
+        for (int k = 0; k < H; ++k) {
+            const float gk = __shfl(g[k], lane & ~(G - 1), 64);
+#pragma unroll
+            for (int m = k; m < H; ++m) v = l == m ? __builtin_fmaf(w[m - k], gk, v) : v;
+        }
+        if (active && l < H) p.dstate_in[row * H + l] = v;
+    }
+#pragma unroll
+    for (int j = 0; j <= K; ++j) {
+        float s = acc[j];
+#pragma unroll
+        for (int off = 1; off < G; off *= 2) s += __shfl_xor(s, off, 64);
+        if (active && l == j) p.part[row * (K + 1) + j] = s;
     }
 }
 

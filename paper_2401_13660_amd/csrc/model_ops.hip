@@ -236,11 +236,18 @@ template <int IN, int OUT, int K> hipError_t conv_bwd_k(mbs::convbwd::Params &p,
     namespace C = mbs::convbwd;
     void *args[] = {&p};
     hipError_t e = hipSuccess;
-    const int64_t waves = p.batch * p.dim * p.nseg;
+    constexpr int S = C::kSpan<IN, OUT>;
+    const int64_t rows = p.batch * p.dim, spans = (p.seqlen + S - 1) / S;
+    // rows of one tile need no walk, and up to 32 (16) spans two (four) of them share a wave
+    const int64_t lanes = spans == 0 || spans > 32 ? 64 : spans > 16 ? 32 : 16, waves = (rows * p.nseg * lanes + 63) / 64;
+    const void *walk = p.seqlen % S ? reinterpret_cast<const void *>(&C::conv1d_bwd<IN, OUT, K, true>)
+                                    : reinterpret_cast<const void *>(&C::conv1d_bwd<IN, OUT, K, false>);
+    const void *fn = spans == 0 || spans > 64 ? walk
+                     : lanes == 64            ? reinterpret_cast<const void *>(&C::conv1d_bwd_short<IN, OUT, K, 64>)
+                     : lanes == 32            ? reinterpret_cast<const void *>(&C::conv1d_bwd_short<IN, OUT, K, 32>)
+                                              : reinterpret_cast<const void *>(&C::conv1d_bwd_short<IN, OUT, K, 16>);
     if (waves > 0)
-        e = hipLaunchKernel(p.seqlen % C::kSpan<IN, OUT> ? reinterpret_cast<const void *>(&C::conv1d_bwd<IN, OUT, K, true>)
-                                                         : reinterpret_cast<const void *>(&C::conv1d_bwd<IN, OUT, K, false>),
-                            dim3((unsigned)((waves + C::kWaves - 1) / C::kWaves)), dim3(C::kThreads), args, 0, st);
+        e = hipLaunchKernel(fn, dim3((unsigned)((waves + C::kWaves - 1) / C::kWaves)), dim3(C::kThreads), args, 0, st);
     if (e != hipSuccess) return e;
     return hipLaunchKernel(reinterpret_cast<const void *>(&C::conv1d_bwd_finish<K>),
                            dim3((unsigned)((p.dim * (K + 1) + C::kThreads - 1) / C::kThreads)), dim3(C::kThreads), args, 0, st);
