@@ -23,6 +23,10 @@
 // rows are cut into pieces of kPiece tokens whose maxima and sums one launch finds; a second one
 // joins them, decides, and races within each piece of the row that stops the sequence; a third one
 // joins the pieces' winners.
+//
+// Bound by latency: 16 drafts of 32 prompts over 256 bytes take 6.1 us for 1.1 MB (58 with one wave per
+// sequence), one byte of one prompt 2.7; 4 drafts of 16 prompts over 32,000 tokens in bf16 6.6, 7.9 and
+// 2.8 us for 11 MB, with races of 8,192 tokens per workgroup instead of 2,048 the second launch took 16.
 #pragma once
 
 #include <hip/hip_runtime.h>
