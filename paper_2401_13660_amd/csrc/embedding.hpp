@@ -14,10 +14,10 @@
 //
 // 32,768 bytes of a text, width 1792 in bf16: 34 us, of which the sums take 22.4 (5.2 TB/s, the rate of
 // a device copy), the sort's two launches 9 and the joining 4.4, a chain of loads each.  16,384 tokens
-// of a table of 32,000 rows of 768 fp32: 45 us, four launches of the sort at 6 to 7.5 (a quarter of
-// the table's 98 MB zeroed beside each), the sums 14.5 and the joining 4.  With the next pass's digits
-// counted by atomics in the launch before, three launches of the sort took 33 us instead of 28: equal
-// tokens meet in one counter.
+// of a table of 32,000 rows of 768 fp32: 43 us, three launches of the sort at 7.6 to 10 (a third of
+// the table's 98 MB zeroed beside each), the sums 14.4 and the joining 4.5.  With a launch of its own
+// for each pass's counts the sort took four, 45 us in all; with the next pass's counts added in memory
+// token by token instead of in LDS 49: equal tokens meet in one counter.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -57,6 +57,8 @@ struct BwdParams {
     int32_t passes;                // 8 bits each
     int32_t shift;                 // bits below this pass's digit
     uint32_t *counts;              // (tiles, kBins)
+    uint32_t *next_counts;         // the next pass's, counted by this one, or null
+    int32_t ahead;                 // passes after the first whose counts the first launch sets to zero
     uint32_t *valid;               // tokens within the vocabulary
     const Pair *from;              // the pass's input after the first pass
     Pair *to;                      // the pass's output; the sorted list
@@ -164,6 +166,7 @@ __global__ __launch_bounds__(kThreads) void count_digits(BwdParams p) {
     const int64_t n = FIRST ? p.ntokens : (int64_t)*p.valid;
     const int64_t from = (int64_t)blockIdx.x * p.tile, to = min(from + p.tile, n);
     count[threadIdx.x] = 0;
+    for (int k = 0; FIRST && k < p.ahead; ++k) p.next_counts[(k * p.tiles + blockIdx.x) * kBins + threadIdx.x] = 0;
     for (int64_t i = from; i < to || i == from; i += kStep) {
         Keys<TOK, FIRST> keys;
         keys.load(p, i, to);
@@ -178,15 +181,23 @@ __global__ __launch_bounds__(kThreads) void count_digits(BwdParams p) {
 
 // Each place's key and position to the place that its digit gives it.  Every workgroup adds up the counts for itself:
 // the digits below (over all workgroups), then the workgroups, steps and waves before, then the places before.
-template <int TOK, int OUT, bool FIRST>
+//
+// NEXT (up to kNextTiles workgroups): it counts the next pass's digits too, by the workgroup that will find them, in LDS
+// and then in memory: whole numbers, so the order of the atomics changes nothing, and a pass takes one launch.
+constexpr int kNextTiles = 32;
+
+template <int TOK, int OUT, bool FIRST, bool NEXT>
 __global__ __launch_bounds__(kThreads) void scatter(BwdParams p) {
     if ((int)blockIdx.x >= p.tiles) return zero_share<OUT>(p);
+    __shared__ uint32_t next[NEXT ? kNextTiles : 1][kBins];
     __shared__ uint32_t at[kWaves][kBins], waves[kWaves];
     const int d = threadIdx.x, wave = d >> 6, lane = d & 63;
     const int64_t n = FIRST ? p.ntokens : (int64_t)*p.valid;
     const int64_t from = (int64_t)blockIdx.x * p.tile, to = min(from + p.tile, n);
     Keys<TOK, FIRST> keys;
     keys.load(p, from, to);
+    if constexpr (NEXT)
+        for (int g = 0; g < p.tiles; ++g) next[g][d] = 0;
     auto count_step = [&] {
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) at[w][d] = 0;
@@ -242,9 +253,16 @@ __global__ __launch_bounds__(kThreads) void scatter(BwdParams p) {
                 if (lane == first) base = atomicAdd(&at[wave][digit], (uint32_t)__popcll(same));
                 base = __shfl(base, first, 64);
                 const int64_t i = i0 + wave * (64 * kPlaces) + 64 * k + lane;
-                p.to[base + __popcll(same & ((1ull << lane) - 1))] = Pair{(uint32_t)key, FIRST ? (uint32_t)i : p.from[i].pos};
+                const uint32_t dest = base + __popcll(same & ((1ull << lane) - 1));
+                p.to[dest] = Pair{(uint32_t)key, FIRST ? (uint32_t)i : p.from[i].pos};
+                if constexpr (NEXT) atomicAdd(&next[dest / kStep][(key >> (p.shift + 8)) & (kBins - 1)], 1u);
             }
         }
+    }
+    if constexpr (NEXT) {
+        __syncthreads();
+        for (int g = 0; g < p.tiles; ++g)
+            if (next[g][d] != 0) atomicAdd(&p.next_counts[g * kBins + d], next[g][d]);
     }
 }
 

@@ -81,6 +81,7 @@ struct Areas {
 struct EmbedPlan {
     int64_t tile, tiles, chunk, groups;
     int passes;
+    bool merged;                                        // each pass counts the next one's digits
     size_t counts, valid, a, b, head, tail, bytes;
     EmbedPlan(int64_t ntokens, int64_t vocab, int64_t dim) {
         namespace E = mbs::embed;
@@ -95,7 +96,8 @@ struct EmbedPlan {
         while (chunk > 16 && ntokens / chunk * ((dim + 255) / 256) < 2048) chunk /= 2;
         groups = (ntokens + chunk * E::kWaves - 1) / (chunk * E::kWaves);
         Areas w;
-        counts = w.add((size_t)tiles * E::kBins * 4);
+        merged = tiles <= E::kNextTiles;                // tile is kStep then
+        counts = w.add((size_t)(merged ? passes : 1) * (size_t)tiles * E::kBins * 4);
         valid = w.add(4);
         a = w.add((size_t)ntokens * sizeof(E::Pair));
         b = w.add(passes > 1 ? (size_t)ntokens * sizeof(E::Pair) : 0);
@@ -109,7 +111,7 @@ template <int TOK, int OUT> hipError_t embed_sort(mbs::embed::BwdParams &p, cons
     namespace E = mbs::embed;
     E::Pair *const ab[2] = {reinterpret_cast<E::Pair *>(ws + f.a), reinterpret_cast<E::Pair *>(ws + f.b)};
     // the table is set to zero in equal shares beside the launches of the sort; 16-byte shares keep the stores aligned
-    const int64_t elems = p.vocab * p.dim, launches = f.tiles > 1 ? 2 * f.passes : 1;
+    const int64_t elems = p.vocab * p.dim, launches = f.tiles <= 1 ? 1 : f.merged ? f.passes + 1 : 2 * f.passes;
     const int64_t share = ((elems + launches - 1) / launches + 63) / 64 * 64;
     const int64_t zeroing = std::min<int64_t>((share + 4095) / 4096, 2048);     // workgroups of at least 4,096 elements
     const dim3 grid((unsigned)(f.tiles + zeroing)), block(E::kThreads);
@@ -128,18 +130,29 @@ template <int TOK, int OUT> hipError_t embed_sort(mbs::embed::BwdParams &p, cons
         return hipLaunchKernel(reinterpret_cast<const void *>(&E::sort_small<TOK, OUT>), small, dim3(E::kSmallThreads), args, 0, st);
     }
     for (int k = 0; k < f.passes; ++k) {
+        const bool first = k == 0, next = f.merged && k + 1 < f.passes;
+        uint32_t *const all = reinterpret_cast<uint32_t *>(ws + f.counts);
         p.shift = 8 * k;
-        p.from = k == 0 ? nullptr : ab[(k - 1) & 1];
+        p.from = first ? nullptr : ab[(k - 1) & 1];
         p.to = ab[k & 1];
+        p.counts = all + (f.merged ? (int64_t)k * f.tiles * E::kBins : 0);
+        p.next_counts = next ? p.counts + f.tiles * E::kBins : nullptr;
+        p.ahead = first && f.merged ? f.passes - 1 : 0;
+        hipError_t e = hipSuccess;
+        if (first || !f.merged) {
+            next_share();
+            // keys of later passes are no tokens: one instantiation for all token types
+            e = hipLaunchKernel(first ? reinterpret_cast<const void *>(&E::count_digits<TOK, OUT, true>)
+                                      : reinterpret_cast<const void *>(&E::count_digits<0, OUT, false>),
+                                grid, block, args, 0, st);
+            if (e != hipSuccess) return e;
+        }
         next_share();
-        hipError_t e = hipLaunchKernel(k == 0 ? reinterpret_cast<const void *>(&E::count_digits<TOK, OUT, true>)
-                                              : reinterpret_cast<const void *>(&E::count_digits<TOK, OUT, false>),
-                                       grid, block, args, 0, st);
-        if (e != hipSuccess) return e;
-        next_share();
-        e = hipLaunchKernel(k == 0 ? reinterpret_cast<const void *>(&E::scatter<TOK, OUT, true>)
-                                   : reinterpret_cast<const void *>(&E::scatter<TOK, OUT, false>),
-                            grid, block, args, 0, st);
+        const void *fn = first ? next ? reinterpret_cast<const void *>(&E::scatter<TOK, OUT, true, true>)
+                                      : reinterpret_cast<const void *>(&E::scatter<TOK, OUT, true, false>)
+                         : next ? reinterpret_cast<const void *>(&E::scatter<0, OUT, false, true>)
+                                : reinterpret_cast<const void *>(&E::scatter<0, OUT, false, false>);
+        e = hipLaunchKernel(fn, grid, block, args, 0, st);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
@@ -454,7 +467,6 @@ int mb_embedding_bwd(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_
     p.tokens = tokens; p.dy = dy; p.dweight = dweight; p.scale = scale;
     p.passes = f.passes;
     p.tile = (int32_t)f.tile; p.tiles = (int32_t)f.tiles; p.chunk = (int32_t)f.chunk;
-    p.counts = reinterpret_cast<uint32_t *>(ws.at + f.counts);
     p.valid = reinterpret_cast<uint32_t *>(ws.at + f.valid);
     p.head = reinterpret_cast<float *>(ws.at + f.head);
     p.tail = reinterpret_cast<float *>(ws.at + f.tail);

@@ -187,3 +187,23 @@ def test_refusals():
                  lambda: mb.embedding_fwd(torch.zeros(5, dtype=torch.int32, device="cuda:0"), W, out=W)):
         with pytest.raises(mb.MBScanError):
             call()
+
+
+@pytest.mark.parametrize("n,V", [(6000, 70001), (20000, 20000000), (32768, 3000), (33000, 3000), (40000, 70000), (300001, 400),
+                                 (262145, 256), (4096, 300), (4097, 300)])
+def test_gradient_of_many_tokens(n, V):
+    """The sort in one, two, three and four passes, by one workgroup and by many, that count ahead and that do not."""
+    import paper_2401_13660_amd as mb
+    d = 3 if V < 10 ** 6 else 1
+    announce(f"embedding_bwd n={n} V={V} d={d}")
+    r = np.random.default_rng(n + V)
+    t = torch.from_numpy(np.where(r.random(n) < 0.3, r.integers(0, 5, n), r.integers(-1, V + 1, n))).to("cuda:0")
+    dy = randn((n, d), n, "f32")
+    g = mb.embedding_bwd(t, dy, V)
+    again = mb.embedding_bwd(t, dy, V)
+    ok = (t >= 0) & (t < V)
+    ref = torch.zeros(V, d, dtype=torch.float64, device="cuda:0").index_add_(0, t[ok], dy[ok].double())
+    mag = torch.zeros(V, d, dtype=torch.float64, device="cuda:0").index_add_(0, t[ok], dy[ok].double().abs())
+    count = torch.bincount(t[ok], minlength=V)[:, None]
+    assert torch.equal(g, again)
+    assert ((g.double() - ref).abs() <= (count + 2) * U * mag).all()
