@@ -652,8 +652,8 @@ def grad_norm(grads):
 
 
 def clip_grad_norm(grads, max_norm, *, eps=1e-6, out=None):
-    """Scales a list of fp32 and bf16 tensors by max_norm / (norm + eps) where that is below 1, in place or
-    into ``out`` (tensors of the same shapes and types).  Returns the norm before clipping, a 0-dimensional
+    """Scales a list of fp32 and bf16 tensors (the gradients, not the parameters) by max_norm / (norm + eps)
+    where that is below 1, in place or into ``out`` (tensors of the same shapes and types).  Returns the norm before clipping, a 0-dimensional
     fp32 tensor on the GPU."""
     lib = load_library()
     if _fast is not None:
@@ -669,6 +669,8 @@ def clip_grad_norm(grads, max_norm, *, eps=1e-6, out=None):
         for i, (o, t) in enumerate(zip(out, grads)):
             _need(o, f"out {i}", t.shape, t.dtype, dev)
         optrs = (_VP * len(out))(*(o.data_ptr() for o in out))
+    if any(t.requires_grad for t in (grads if out is None else out)):
+        raise MBScanError("gradients are clipped, not the parameters: a tensor that would be written requires grad")
     norm = torch.empty((), dtype=torch.float32, device=dev)
     ws = _workspace(lib.mb_grad_norm_workspace(len(grads)), "mb_clip_grad_norm", dev)
     with _on_device(dev):

@@ -504,6 +504,12 @@ PyObject *clip_grad_norm(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
         const TensorList g(c, a[0]);
         const float max_norm = real(a[1], c.ok), eps = real(a[2], c.ok);
         PLAIN_OR_NONE(c);
+        // what is written are gradients, not the parameters that torch's function of this name takes
+        PyObject *written = a[3] == Py_None ? a[0] : a[3];
+        for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(written); ++i) {
+            const at::Tensor *t = plain(PySequence_Fast_ITEMS(written)[i]);
+            if (!t || t->requires_grad()) Py_RETURN_NONE;
+        }
         std::vector<void *> out;
         if (a[3] != Py_None) {
             const TensorList o(c, a[3], a[0]);

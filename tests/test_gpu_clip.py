@@ -145,3 +145,23 @@ def test_refusals():
         with pytest.raises(mb.MBScanError):
             call()
     assert (g == 1).all() and (h == 1).all()
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_parameters_are_not_clipped(native, monkeypatch):
+    """A list of parameters, which torch's function of a like name takes, is refused instead of scaled."""
+    import paper_2401_13660_amd as mb
+    from paper_2401_13660_amd import _binding
+    announce(f"clip_grad_norm of parameters, native {native}")
+    if not native:
+        monkeypatch.setattr(_binding, "_fast", None)
+    w = torch.nn.Parameter(torch.ones(5, device="cuda:0"))
+    g = torch.ones(5, device="cuda:0")
+    for call in (lambda: mb.clip_grad_norm([w], 0.1), lambda: mb.clip_grad_norm([g, w], 0.1),
+                 lambda: mb.clip_grad_norm([g], 0.1, out=[w])):
+        with pytest.raises(mb.MBScanError, match="requires grad"):
+            call()
+    assert (w == 1).all() and (g == 1).all()
+    out = torch.empty(5, device="cuda:0")
+    mb.clip_grad_norm([w], 0.1, out=[out])                  # read only
+    assert abs(float(out.norm()) - 0.1) < 1e-6
