@@ -474,7 +474,7 @@ int mb_clip_grad_norm(int64_t count, const void *const *grads, void *const *out,
  *   workspace     as for mb_embedding_bwd, of mb_verify_sample_workspace(batch, ndraft, vocab) bytes
  *                 (none up to a vocabulary of 1,024)
  * Outputs must not overlap each other or the inputs.  vocab >= 1, below
- * 2^31 - 8192; batch below 2^22; batch * (2 ndraft + 1) * (vocab / 8192 + 1) below 2^23 where vocab
+ * 2^31 - 4096; batch below 2^22; batch * (2 ndraft + 1) * (vocab / 4096 + 1) below 2^23 where vocab
  * is above 1,024.  Probabilities are fp32.
  */
 int mb_verify_sample(int64_t batch, int64_t ndraft, int64_t vocab, int32_t logit_dtype, float temperature,

@@ -25,8 +25,9 @@
 // joins the pieces' winners.
 //
 // Bound by latency: 16 drafts of 32 prompts over 256 bytes take 6.1 us for 1.1 MB (58 with one wave per
-// sequence), one byte of one prompt 2.7; 4 drafts of 16 prompts over 32,000 tokens in bf16 6.6, 7.9 and
-// 2.8 us for 11 MB, with races of 8,192 tokens per workgroup instead of 2,048 the second launch took 16.
+// sequence), one byte of one prompt 2.7; 4 drafts of 16 prompts over 32,000 tokens in bf16 14.4 us a call
+// for 11 MB, three launches of 6, 7.9 and 2.8: with races of 8,192 tokens per workgroup instead of 2,048
+// the second launch took 16, and maxima and sums by 8,192 instead of 4,096 took 0.6 us longer.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -40,7 +41,7 @@ namespace sample {
 constexpr int kSmallVocab = 1024;
 constexpr int kMaxWaves = 16;
 constexpr int kThreads = 256;      // of a piece
-constexpr int kPieceSpans = 8;     // spans of 4 per thread where maxima and sums are found
+constexpr int kPieceSpans = 4;     // spans of 4 per thread where maxima and sums are found
 constexpr int kRaceSpans = 2;      // and where the race is run, two exponentials and a division per token
 constexpr int kPiece = kThreads * kPieceSpans * 4;
 constexpr int kRacePiece = kThreads * kRaceSpans * 4;
