@@ -20,7 +20,7 @@ P = {k: 0x100000000 * (i + 1) for i, k in enumerate(
 @no_gpu_only
 @pytest.mark.parametrize("name", ["mb_embedding_fwd", "mb_embedding_bwd"])
 @pytest.mark.parametrize("over,code", [
-    (dict(n=-1), -2), (dict(V=-1), -2), (dict(V=1 << 31), -2), (dict(n=1 << 31), -2), (dict(n=1 << 50, d=1 << 20), -2),
+    (dict(n=-1), -2), (dict(V=-1), -2), (dict(V=1 << 31), -2), (dict(n=1 << 50, d=1 << 20), -2),
     (dict(tok=3), -3), (dict(it=2), -3), (dict(ot=-1), -3),
     (dict(a=None), -1), (dict(b=None), -1), (dict(c=None), -1),
     (dict(a=P["tokens"] + 2), -4), (dict(b=P["weight"] + 1), -4), (dict(c=P["out"] + 2), -4),
@@ -122,6 +122,7 @@ def test_workspaces():
     lib = mb.load_library()
     assert lib.mb_grad_norm_workspace(-1) == -2 and lib.mb_embedding_bwd_workspace(-1, 1, 1) == -2
     assert lib.mb_embedding_bwd_workspace(1 << 31, 256, 64) == -2
+    assert lib.mb_embedding_bwd(1 << 31, 5, 8, 1, 0, 0, 1.0, P["tokens"], P["dy"], P["out"], None, None) == -2
     assert lib.mb_conv1d_bwd_workspace(None) == -1
     d = B.ConvDesc(4, 3584, 8192, 4, 1, 1, 1, 0, 0)
     assert lib.mb_conv1d_bwd_workspace(ctypes.byref(d)) >= 4 * 3584 * 5 * 4
