@@ -268,20 +268,19 @@ __global__ __launch_bounds__(kThreads) void scatter(BwdParams p) {
 
 // The whole sort by one workgroup, for up to kSmallTokens: places in registers, moved through LDS between the passes.
 // The other workgroups set the table to zero meanwhile.  4,096 tokens take 7 us of bytes and 10.7 of 30,000 values, 1,000
-// bytes 5; the launches above take about 9 and 21, and two or four times the host's time.  16 places per thread took
-// 21.5 us for 16,384 bytes: one CU's issue rate, where the launches above spread over many.
+// bytes 3.6 with 256 threads (5 with 1,024); the launches above take about 9 and 21, and two or four times the host's
+// time.  16 places per thread took 21.5 us for 16,384 bytes: one CU's issue rate, where the launches above spread over many.
 constexpr int kSmallThreads = 1024;
-constexpr int kSmallWaves = kSmallThreads / 64;
 constexpr int kSmallPlaces = 4;
 constexpr int kSmallTokens = kSmallThreads * kSmallPlaces;
 
-template <int TOK, int OUT>
-__global__ __launch_bounds__(kSmallThreads) void sort_small(BwdParams p) {
-    constexpr int PER = kSmallPlaces;
+template <int TOK, int OUT, int THREADS>
+__global__ __launch_bounds__(THREADS) void sort_small(BwdParams p) {
+    constexpr int PER = kSmallPlaces, WAVES = THREADS / 64;
     if (blockIdx.x >= 1) return zero_share<OUT>(p);
-    __shared__ uint32_t keys[kSmallTokens];
-    __shared__ uint16_t places[kSmallTokens];
-    __shared__ uint32_t at[kSmallWaves][kBins], waves[kBins / 64];
+    __shared__ uint32_t keys[THREADS * PER];
+    __shared__ uint16_t places[THREADS * PER];
+    __shared__ uint32_t at[WAVES][kBins], waves[kBins / 64];
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int mine = wave * (64 * PER) + lane;                  // the wave's places, 64 side by side
     int n = (int)p.ntokens;
@@ -310,7 +309,7 @@ __global__ __launch_bounds__(kSmallThreads) void sort_small(BwdParams p) {
         uint32_t total = 0, below = 0;
         if (tid < kBins) {
 #pragma unroll
-            for (int w = 0; w < kSmallWaves; ++w) total += at[w][tid];
+            for (int w = 0; w < WAVES; ++w) total += at[w][tid];
             below = total;
 #pragma unroll
             for (int off = 1; off < 64; off *= 2) {
@@ -326,7 +325,7 @@ __global__ __launch_bounds__(kSmallThreads) void sort_small(BwdParams p) {
             if (pass == 0 && tid == kBins - 1) *p.valid = below;
             below -= total;
 #pragma unroll
-            for (int w = 0; w < kSmallWaves; ++w) {
+            for (int w = 0; w < WAVES; ++w) {
                 const uint32_t c = at[w][tid];
                 at[w][tid] = below;
                 below += c;
@@ -371,10 +370,14 @@ __global__ __launch_bounds__(kThreads) void sum_chunks(BwdParams p, uint32_t col
     __shared__ uint32_t piece_key[kWaves][2];
     __shared__ int piece_is[kWaves];
     constexpr int kHead = 1, kThrough = 2, kTail = 4;   // the first run came from before; it goes on after; the last one does
-    const int64_t group = blockIdx.x / col_tiles, n = *p.valid;
-    if (group * kWaves * p.chunk >= n) return;
+    const int64_t group = blockIdx.x / col_tiles, most = p.ntokens - 1;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t from = (group * kWaves + wave) * p.chunk;
+    // All that the wave reads of the list, asked for at once; places past the valid ones hold nothing that counts.
+    const Pair mine = p.to[min(from + lane, most)];
+    const uint32_t key_before = p.to[min(max(from - 1, (int64_t)0), most)].key, key_after = p.to[min(from + p.chunk, most)].key;
+    const int64_t n = *p.valid;
+    if (group * kWaves * p.chunk >= n) return;
     const int64_t col = span_at<S>((int64_t)(blockIdx.x % col_tiles) * (64 * S) + lane * S, p.dim);
     const int m = (int)max((int64_t)0, min((int64_t)p.chunk, n - from));
     // The sum of a run that is whole, in dW's type.
@@ -386,9 +389,8 @@ __global__ __launch_bounds__(kThreads) void sum_chunks(BwdParams p, uint32_t col
     };
     int is = 0;
     if (m > 0) {
-        const Pair mine = p.to[from + min(lane, m - 1)];
-        const int64_t before = from > 0 ? (int64_t)p.to[from - 1].key : kNone;
-        const int64_t after = from + m < n ? (int64_t)p.to[from + m].key : kNone;
+        const int64_t before = from > 0 ? (int64_t)key_before : kNone;
+        const int64_t after = from + m < n ? (int64_t)key_after : kNone;
         float acc[S] = {};
         uint32_t key = __builtin_amdgcn_readlane(mine.key, 0);
         bool came = before == (int64_t)key;             // the run at hand began before the chunk

@@ -122,12 +122,15 @@ template <int TOK, int OUT> hipError_t embed_sort(mbs::embed::BwdParams &p, cons
     };
     void *args[] = {&p};
     if (f.tiles <= 1) {
-        // its workgroups are four times as large, so a fourth as many zero the table
         next_share();
         p.to = ab[0];
-        const dim3 small(1 + (unsigned)((zeroing + 3) / 4));
         p.tiles = 1;
-        return hipLaunchKernel(reinterpret_cast<const void *>(&E::sort_small<TOK, OUT>), small, dim3(E::kSmallThreads), args, 0, st);
+        // 256 threads where they do: fewer waves' counts to add up.  The larger workgroups zero four times as much each
+        const bool quarter = p.ntokens <= E::kThreads * E::kSmallPlaces;
+        const unsigned blocks = 1 + (unsigned)(quarter ? zeroing : (zeroing + 3) / 4);
+        return hipLaunchKernel(quarter ? reinterpret_cast<const void *>(&E::sort_small<TOK, OUT, E::kThreads>)
+                                       : reinterpret_cast<const void *>(&E::sort_small<TOK, OUT, E::kSmallThreads>),
+                               dim3(blocks), dim3(quarter ? E::kThreads : E::kSmallThreads), args, 0, st);
     }
     for (int k = 0; k < f.passes; ++k) {
         const bool first = k == 0, next = f.merged && k + 1 < f.passes;
