@@ -101,8 +101,8 @@ template <int S, int K> __device__ __forceinline__ void back_through_taps(float 
     }
 }
 
-// CUT: L is no multiple of the span, so a row's last span is cut.  The instantiations without need 91 to 97 registers, 5
-// waves per SIMD; with it up to 119, and 4.
+// Rows of no timestep, or of more than 64 spans.  CUT: L is no multiple of the span, so a row's last span is cut.  The
+// instantiations without need 91 to 97 registers, 5 waves per SIMD; with it up to 119, and 4.
 template <int IN, int OUT, int K, bool CUT>
 __global__ __launch_bounds__(kThreads) void conv1d_bwd(Params p) {
     constexpr int H = K - 1, HH = H > 0 ? H : 1, S = kSpan<IN, OUT>, T = 64 * S;
@@ -145,15 +145,9 @@ __global__ __launch_bounds__(kThreads) void conv1d_bwd(Params p) {
     Span<OUT, S> ys;
     float halo = 0.0f;                                          // lane j < H: the input H - j before the tile
     auto load = [&](int tile) {
-        const int64_t t = (int64_t)tile * T + lane * S;
-        if (L >= S) {                                   // a span past the row's end: the last whole one, shifted below
-            xs.template load<true>(p.x, base + min(t, L - S));
-            ys.template load<true>(p.dy, base + min(t, L - S));
-        } else {
-            const int n = (int)max((int64_t)0, min(L - t, (int64_t)S));
-            xs.load_first(p.x, base + t, n);
-            ys.load_first(p.dy, base + t, n);
-        }
+        const int64_t t = min((int64_t)tile * T + lane * S, L - S);    // past the row's end: the last whole span, shifted below
+        xs.template load<true>(p.x, base + t);
+        ys.template load<true>(p.dy, base + t);
         if (H > 0 && lane < H) halo = before((int64_t)tile * T - H + lane);
     };
 
@@ -168,7 +162,7 @@ __global__ __launch_bounds__(kThreads) void conv1d_bwd(Params p) {
             xin[H + i] = xs.get(i);
             g[i] = ys.get(i);
         }
-        if (!whole && L >= S) {
+        if (!whole) {
             const int64_t past = max(t0 + S - L, (int64_t)0);
             end_span<S, CUT>(xin + H, past);
             end_span<S, CUT>(g, past);
