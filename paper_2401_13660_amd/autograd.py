@@ -13,6 +13,7 @@ multiple of 16 (the library raises otherwise).  The convolution's backward is
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import _binding as _b
 
@@ -55,6 +56,7 @@ class _CausalConv1d(torch.autograd.Function):
         return y, state_out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy, dstate_out):
         x, w, bias, state = ctx.saved_tensors
         dy = torch.zeros_like(x, dtype=ctx.ytype) if dy is None else dy
@@ -65,7 +67,7 @@ class _CausalConv1d(torch.autograd.Function):
 
 def causal_conv1d(x, w, bias=None, state=None, *, apply_silu=True):
     """Differentiable convolution (+ Swish): returns (y, state_out), y in x's dtype.  Shapes and dtypes as for
-    ``conv1d``; gradients flow to every tensor argument."""
+    ``conv1d``; gradients flow to every tensor argument, once: a second derivative raises."""
     return _CausalConv1d.apply(x, w, bias, state, apply_silu)
 
 
@@ -77,6 +79,7 @@ class _Embedding(torch.autograd.Function):
         return _b.embedding_fwd(tokens, weight, scale=scale, out_dtype=out_dtype)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         tokens, = ctx.saved_tensors
         dw = _b.embedding_bwd(tokens, dy.contiguous(), ctx.vocab, scale=ctx.scale, out_dtype=ctx.wtype)
