@@ -372,8 +372,8 @@ int mb_embedding_fwd(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_
  *   dy      dy_dtype (ntokens, dim)
  *   dweight out_dtype (vocab, dim)     must not overlap an input; ntokens * dim below 2^37
  *   workspace  device memory of mb_embedding_bwd_workspace(ntokens, vocab, dim) bytes (of a
- *              negative mb_status where the sizes are refused), 16-byte aligned, that nothing else
- *              uses until the call's work is done; NULL: the call allocates it on the stream
+ *              negative mb_status where the sizes are refused; 0: none is used), 16-byte aligned,
+ *              that nothing else uses until the call's work is done; NULL: the call allocates it on the stream
  *              (hipMallocAsync) and frees it there, which costs the host about 8 us
  */
 int mb_embedding_bwd(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_type, int32_t dy_dtype, int32_t out_dtype,

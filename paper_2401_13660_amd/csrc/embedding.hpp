@@ -6,11 +6,12 @@
 //
 // Tokens are bytes, int32 or int64.  Sums are fp32, rounded once to dW's type.
 //
-// The gradient sorts the positions by token (a stable counting sort, 8 bits a pass: one pass for
-// bytes) and cuts the sorted list into chunks of 64.  A wave adds up the rows of a chunk for a tile
-// of columns, each row read once, and writes a token's sum where all of its rows lie in the chunk;
-// the sums of a token that goes on into other chunks are joined afterwards in the order of the
-// chunks.  No atomic adds floats: a result depends on the tokens and dy alone.
+// Few tokens of few rows (sum_direct): a workgroup per row looks for its tokens.  Otherwise the gradient
+// sorts the positions by token (a stable counting sort, 8 bits a pass: one pass for bytes) and cuts the
+// sorted list into chunks of 64.  A wave adds up the rows of a chunk for a tile of columns, each row read
+// once, and writes a token's sum where all of its rows lie in the chunk; the sums of a token that goes on
+// into other chunks are joined afterwards in the order of the chunks.  No atomic adds floats: a result
+// depends on the tokens and dy alone.
 //
 // 32,768 bytes of a text, width 1792 in bf16: 34 us, of which the sums take 22.4 (5.2 TB/s, the rate of
 // a device copy), the sort's two launches 9 and the joining 4.4, a chain of loads each.  16,384 tokens
@@ -356,6 +357,73 @@ __global__ __launch_bounds__(THREADS) void sort_small(BwdParams p) {
         }
         __syncthreads();
     }
+}
+
+// Few tokens and few rows: a workgroup per row of the table and tile of 256 columns.  Each wave looks through its share of
+// the tokens, lists the places of its row's, and adds those up; the waves' sums are joined in LDS.  One launch, no sort, no
+// workspace, no row set to zero first.
+//
+// Bound by latency: a token, a list, rows of dy, a store.  256 rows of 512, 500 tokens of a text: 4.1 us, the sort and the
+// sums 12; 2,000 tokens 8 and 14.  A row's tokens are one compute unit's work, about 60 GB/s, so the worst is one value
+// throughout: 13 (1,000 tokens) and 30 us (2,000) where sort and sums, which cut evenly, take 11 and 14; 4,000 tokens of a
+// text take as long either way, hence the limit.  Every workgroup reads all tokens, so many rows are no gain: 1,000 rows of
+// 1,792 13 to 16 us, 4,000 of them 42 to 50.  16 waves, 16 rows ahead (registers) and tiles of 512 columns: all no faster.
+constexpr int kDirectWaves = 8;
+constexpr int kDirectTokens = 2048;
+constexpr int kDirectBlocks = 4096;
+constexpr int kDirectSteps = kDirectTokens / (64 * kDirectWaves);
+
+template <int TOK, int DY, int OUT, int S>
+__global__ __launch_bounds__(64 * kDirectWaves) void sum_direct(BwdParams p, uint32_t col_tiles) {
+    constexpr int AHEAD = 8;
+    __shared__ uint16_t list[kDirectWaves][64 * kDirectSteps];
+    __shared__ float sums[kDirectWaves][64 * S];
+    __shared__ int found[kDirectWaves];
+    const int64_t v = blockIdx.x / col_tiles;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n = (int)p.ntokens, share = (n + kDirectWaves - 1) / kDirectWaves, from = wave * share, to = min(from + share, n);
+    const int64_t tile0 = (int64_t)(blockIdx.x % col_tiles) * (64 * S), col = span_at<S>(tile0 + lane * S, p.dim);
+    int64_t t[kDirectSteps];
+#pragma unroll
+    for (int k = 0; k < kDirectSteps; ++k) t[k] = from + 64 * k + lane < to ? token_at<TOK>(p.tokens, from + 64 * k + lane) : kNone;
+    int m = 0;
+#pragma unroll
+    for (int k = 0; k < kDirectSteps; ++k) {
+        const uint64_t same = __ballot(t[k] == v);
+        if (t[k] == v) list[wave][m + __popcll(same & ((1ull << lane) - 1))] = (uint16_t)(from + 64 * k + lane);
+        m += __popcll(same);
+    }
+    __builtin_amdgcn_wave_barrier();                    // a wave's own list, in its own order
+    if (m > 0) {
+        float acc[S] = {};
+        for (int i = 0; i < m; i += AHEAD) {
+            Span<DY, S> row[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) row[k].template load<true>(p.dy, (int64_t)list[wave][min(i + k, m - 1)] * p.dim + col);
+            float part[S] = {};
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+#pragma unroll
+                for (int j = 0; j < S; ++j) part[j] += i + k < m ? row[k].get(j) : 0.0f;
+#pragma unroll
+            for (int j = 0; j < S; ++j) acc[j] += part[j];
+        }
+#pragma unroll
+        for (int j = 0; j < S; ++j) sums[wave][j * 64 + lane] = acc[j];
+    }
+    if (lane == 0) found[wave] = m;
+    __syncthreads();
+    if (wave != 0) return;
+    float acc[S] = {};
+#pragma unroll
+    for (int w = 0; w < kDirectWaves; ++w)
+        if (found[w] > 0) {
+#pragma unroll
+            for (int j = 0; j < S; ++j) acc[j] += sums[w][j * 64 + lane];
+        }
+#pragma unroll
+    for (int j = 0; j < S; ++j) acc[j] *= p.scale;
+    store_span<OUT, S>(p.dweight, v * p.dim + col, acc);
 }
 
 // Everything asked of memory has arrived (vmcnt 0).  Loads and stores share that counter and a wait is for the oldest of

@@ -82,9 +82,11 @@ struct EmbedPlan {
     int64_t tile, tiles, chunk, groups;
     int passes;
     bool merged;                                        // each pass counts the next one's digits
+    bool direct;                                        // no sort: sum_direct, without a workspace
     size_t counts, valid, a, b, head, tail, bytes;
     EmbedPlan(int64_t ntokens, int64_t vocab, int64_t dim) {
         namespace E = mbs::embed;
+        direct = ntokens <= E::kDirectTokens && vocab * ((dim + 255) / 256) <= E::kDirectBlocks;
         // tokens per workgroup: 1,024, or what keeps the workgroups at kBins (each reads the counts of all)
         tile = std::max<int64_t>(1024, ((ntokens + E::kBins - 1) / E::kBins + 1023) / 1024 * 1024);
         tiles = (ntokens + tile - 1) / tile;
@@ -103,7 +105,7 @@ struct EmbedPlan {
         b = w.add(passes > 1 ? (size_t)ntokens * sizeof(E::Pair) : 0);
         head = w.add((size_t)groups * (size_t)dim * 4);
         tail = w.add((size_t)groups * (size_t)dim * 4);
-        bytes = w.bytes;
+        bytes = direct ? 0 : w.bytes;
     }
 };
 
@@ -176,6 +178,24 @@ template <int DY, int OUT, int S> hipError_t embed_sum(mbs::embed::BwdParams &p,
 template <int DY, int OUT> hipError_t embed_sum(mbs::embed::BwdParams &p, const EmbedPlan &f, hipStream_t st) {
     constexpr int S = DY == 1 ? 8 : 4;
     return p.dim < S ? embed_sum<DY, OUT, 1>(p, f, st) : embed_sum<DY, OUT, S>(p, f, st);
+}
+
+template <int TOK, int DY, int OUT> hipError_t embed_direct(mbs::embed::BwdParams &p, hipStream_t st) {
+    namespace E = mbs::embed;
+    uint32_t cols = p.dim < 4 ? 1 : (uint32_t)((p.dim + 255) / 256);
+    void *args[] = {&p, &cols};
+    return hipLaunchKernel(p.dim < 4 ? reinterpret_cast<const void *>(&E::sum_direct<TOK, DY, OUT, 1>)
+                                     : reinterpret_cast<const void *>(&E::sum_direct<TOK, DY, OUT, 4>),
+                           dim3((unsigned)(p.vocab * cols)), dim3(64 * E::kDirectWaves), args, 0, st);
+}
+template <int DY, int OUT> hipError_t embed_direct(mbs::embed::BwdParams &p, int32_t token_type, hipStream_t st) {
+    return token_type == MB_TOKEN_U8    ? embed_direct<0, DY, OUT>(p, st)
+           : token_type == MB_TOKEN_I32 ? embed_direct<1, DY, OUT>(p, st)
+                                        : embed_direct<2, DY, OUT>(p, st);
+}
+hipError_t embed_direct(mbs::embed::BwdParams &p, int32_t token_type, int32_t dy_dtype, int32_t out_dtype, hipStream_t st) {
+    if (dy_dtype == MB_F32) return out_dtype == MB_F32 ? embed_direct<0, 0>(p, token_type, st) : embed_direct<0, 1>(p, token_type, st);
+    return out_dtype == MB_F32 ? embed_direct<1, 0>(p, token_type, st) : embed_direct<1, 1>(p, token_type, st);
 }
 
 template <int OUT> hipError_t embed_bwd(mbs::embed::BwdParams &p, const EmbedPlan &f, int32_t token_type, int32_t dy_dtype,
@@ -457,17 +477,18 @@ int mb_embedding_bwd(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_
     const size_t tsz = token_size(token_type), ysz = dtype_size(dy_dtype), osz = dtype_size(out_dtype);
     if (!aligned(tokens, tsz) || !aligned(dy, ysz) || !aligned(dweight, osz)) return MB_ERR_ALIGN;
     if (!aligned(workspace, 16)) return MB_ERR_ALIGN;
+    const EmbedPlan f(ntokens, vocab, dim);
     const Range outs[] = {{dweight, (size_t)table_elems * osz},
-                          {workspace, workspace ? EmbedPlan(ntokens, vocab, dim).bytes : 0}};
+                          {workspace, workspace ? std::max<size_t>(f.bytes, 16) : 0}};
     const Range ins[] = {{tokens, (size_t)ntokens * tsz}, {dy, (size_t)row_elems * ysz}};
     if (any_overlap(outs, ins)) return MB_ERR_ALIAS;
-    const EmbedPlan f(ntokens, vocab, dim);
     if (f.groups * ((dim + 255) / 256) >= (int64_t(1) << 22)) return MB_ERR_SHAPE;
-    Workspace ws(workspace, f.bytes, st_of(stream));
-    if (!ws.at) return MB_ERR_HIP;
     mbs::embed::BwdParams p{};
     p.ntokens = ntokens; p.vocab = vocab; p.dim = dim;
     p.tokens = tokens; p.dy = dy; p.dweight = dweight; p.scale = scale;
+    if (f.direct) return status(embed_direct(p, token_type, dy_dtype, out_dtype, st_of(stream)));
+    Workspace ws(workspace, f.bytes, st_of(stream));
+    if (!ws.at) return MB_ERR_HIP;
     p.passes = f.passes;
     p.tile = (int32_t)f.tile; p.tiles = (int32_t)f.tiles; p.chunk = (int32_t)f.chunk;
     p.valid = reinterpret_cast<uint32_t *>(ws.at + f.valid);
