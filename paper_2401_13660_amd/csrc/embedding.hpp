@@ -6,12 +6,12 @@
 //
 // Tokens are bytes, int32 or int64.  Sums are fp32, rounded once to dW's type.
 //
-// Few tokens of few rows (sum_direct): a workgroup per row looks for its tokens.  Otherwise the gradient
-// sorts the positions by token (a stable counting sort, 8 bits a pass: one pass for bytes) and cuts the
-// sorted list into chunks of 64.  A wave adds up the rows of a chunk for a tile of columns, each row read
-// once, and writes a token's sum where all of its rows lie in the chunk; the sums of a token that goes on
-// into other chunks are joined afterwards in the order of the chunks.  No atomic adds floats: a result
-// depends on the tokens and dy alone.
+// Few tokens (sum_direct): a workgroup per row or per token looks for the row's tokens.  Otherwise the
+// gradient sorts the positions by token (a stable counting sort, 8 bits a pass: one pass for bytes) and
+// cuts the sorted list into chunks of 64.  A wave adds up the rows of a chunk for a tile of columns, each
+// row read once, and writes a token's sum where all of its rows lie in the chunk; the sums of a token that
+// goes on into other chunks are joined afterwards in the order of the chunks.  No atomic adds floats: a
+// result depends on the tokens and dy alone.
 //
 // 32,768 bytes of a text, width 1792 in bf16: 34 us, of which the sums take 22.4 (5.2 TB/s, the rate of
 // a device copy), the sort's two launches 9 and the joining 4.4, a chain of loads each.  16,384 tokens
@@ -359,29 +359,61 @@ __global__ __launch_bounds__(THREADS) void sort_small(BwdParams p) {
     }
 }
 
-// Few tokens and few rows: a workgroup per row of the table and tile of 256 columns.  Each wave looks through its share of
-// the tokens, lists the places of its row's, and adds those up; the waves' sums are joined in LDS.  One launch, no sort, no
-// workspace, no row set to zero first.
+// Few tokens: a workgroup per row of the table (BY_ROW) or per token, the first of its value, and tile of 256 columns.  Each
+// wave looks through its share of the tokens, lists the places of its row's, and adds those up; the waves' sums are joined
+// in LDS.  One launch, no sort, no workspace; by token, workgroups of their own set the other rows to zero.
 //
-// Bound by latency: a token, a list, rows of dy, a store.  256 rows of 512, 500 tokens of a text: 4.1 us, the sort and the
-// sums 12; 2,000 tokens 8 and 14.  A row's tokens are one compute unit's work, about 60 GB/s, so the worst is one value
-// throughout: 13 (1,000 tokens) and 30 us (2,000) where sort and sums, which cut evenly, take 11 and 14; 4,000 tokens of a
-// text take as long either way, hence the limit.  Every workgroup reads all tokens, so many rows are no gain: 1,000 rows of
-// 1,792 13 to 16 us, 4,000 of them 42 to 50.  16 waves, 16 rows ahead (registers) and tiles of 512 columns: all no faster.
+// Bound by latency: a token, a list, rows of dy, a store.  256 rows of 512 in bf16, 500 tokens of a text: 4.1 us, the sort
+// and the sums 12; 2,000 tokens 8 and 14.  5,000 rows of 512, by token: 500 6.6 and 14.6, 32,000 rows 10.9 and 17.7.  A row's
+// tokens are one compute unit's work, about 60 GB/s, so the worst is one value throughout: 13 (1,000 tokens) and 30 us
+// (2,000) where sort and sums, which cut evenly, take 11 and 14; 4,000 tokens of a text take as long either way, hence
+// kDirectTokens.  Every workgroup reads all tokens: 1,000 rows of 1,792 take 13 to 16 us, 4,000 of them 42 to 50, 1,000 tokens
+// of 32,000 rows of 1,024 24 and sorted 20, hence the limits on workgroups.  16 waves, 16 rows ahead (registers) and tiles
+// of 512 columns: all no faster.
 constexpr int kDirectWaves = 8;
 constexpr int kDirectTokens = 2048;
-constexpr int kDirectBlocks = 4096;
+constexpr int kDirectRows = 4096;      // workgroups at most, by row
+constexpr int kDirectPlaces = 2048;    // by token
 constexpr int kDirectSteps = kDirectTokens / (64 * kDirectWaves);
+constexpr int kZeroBlocks = 1024;
+constexpr int kZeroRows = 128;         // per workgroup at most
 
-template <int TOK, int DY, int OUT, int S>
+// Rows of the table that no token names, set to zero by `blocks` workgroups.
+template <int TOK, int OUT, int S> __device__ __forceinline__ void zero_unnamed(const BwdParams &p, int block, int blocks) {
+    __shared__ uint32_t named[kZeroRows];
+    const int64_t per = (p.vocab + blocks - 1) / blocks, lo = block * per;
+    const int rows = (int)max((int64_t)0, min(per, p.vocab - lo));
+    for (int i = threadIdx.x; i < rows; i += blockDim.x) named[i] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < (int)p.ntokens; i += blockDim.x) {
+        const int64_t t = token_at<TOK>(p.tokens, i);
+        if (t >= lo && t < lo + rows) named[t - lo] = 1;
+    }
+    __syncthreads();
+    const uint32_t spans = (uint32_t)((p.dim + S - 1) / S);
+    const float zeros[S] = {};
+    for (uint32_t i = threadIdx.x; i < rows * spans; i += blockDim.x) {
+        const uint32_t r = i / spans;
+        if (!named[r]) store_span<OUT, S>(p.dweight, (lo + r) * p.dim + span_at<S>((int64_t)(i - r * spans) * S, p.dim), zeros);
+    }
+}
+
+template <int TOK, int DY, int OUT, int S, bool BY_ROW>
 __global__ __launch_bounds__(64 * kDirectWaves) void sum_direct(BwdParams p, uint32_t col_tiles) {
     constexpr int AHEAD = 8;
+    const int n = (int)p.ntokens;
+    int64_t v = blockIdx.x / col_tiles;
+    const int own = BY_ROW ? 0 : (int)v;                // the place whose token's row it is
+    if constexpr (!BY_ROW) {
+        if (own >= n) return zero_unnamed<TOK, OUT, S>(p, (int)(blockIdx.x - n * col_tiles), (int)(gridDim.x - n * col_tiles));
+        v = token_at<TOK>(p.tokens, own);
+        if (v < 0 || v >= p.vocab) return;
+    }
     __shared__ uint16_t list[kDirectWaves][64 * kDirectSteps];
     __shared__ float sums[kDirectWaves][64 * S];
     __shared__ int found[kDirectWaves];
-    const int64_t v = blockIdx.x / col_tiles;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n = (int)p.ntokens, share = (n + kDirectWaves - 1) / kDirectWaves, from = wave * share, to = min(from + share, n);
+    const int share = (n + kDirectWaves - 1) / kDirectWaves, from = wave * share, to = min(from + share, n);
     const int64_t tile0 = (int64_t)(blockIdx.x % col_tiles) * (64 * S), col = span_at<S>(tile0 + lane * S, p.dim);
     int64_t t[kDirectSteps];
 #pragma unroll
@@ -394,6 +426,9 @@ __global__ __launch_bounds__(64 * kDirectWaves) void sum_direct(BwdParams p, uin
         m += __popcll(same);
     }
     __builtin_amdgcn_wave_barrier();                    // a wave's own list, in its own order
+    if constexpr (!BY_ROW) {                            // an earlier place has the token: that one's workgroup adds up
+        if (__syncthreads_or(m > 0 && list[wave][0] < own)) return;
+    }
     if (m > 0) {
         float acc[S] = {};
         for (int i = 0; i < m; i += AHEAD) {

@@ -82,11 +82,19 @@ struct EmbedPlan {
     int64_t tile, tiles, chunk, groups;
     int passes;
     bool merged;                                        // each pass counts the next one's digits
-    bool direct;                                        // no sort: sum_direct, without a workspace
+    bool direct, by_row;                                // no sort: sum_direct, without a workspace
+    int64_t direct_blocks;
     size_t counts, valid, a, b, head, tail, bytes;
     EmbedPlan(int64_t ntokens, int64_t vocab, int64_t dim) {
         namespace E = mbs::embed;
-        direct = ntokens <= E::kDirectTokens && vocab * ((dim + 255) / 256) <= E::kDirectBlocks;
+        // few tokens: a workgroup per row of the table or per token, whichever are fewer, where either are few enough
+        const int64_t cols = (dim + 255) / 256, rows = vocab * cols, places = ntokens * cols;
+        const bool few = ntokens <= E::kDirectTokens, row_ok = few && rows <= E::kDirectRows;
+        const bool place_ok = few && places <= E::kDirectPlaces && vocab <= E::kZeroRows * E::kZeroBlocks;
+        const int64_t place_blocks = places + std::min<int64_t>(vocab, E::kZeroBlocks);
+        direct = row_ok || place_ok;
+        by_row = row_ok && (!place_ok || rows <= place_blocks);
+        direct_blocks = by_row ? rows : place_blocks;
         // tokens per workgroup: 1,024, or what keeps the workgroups at kBins (each reads the counts of all)
         tile = std::max<int64_t>(1024, ((ntokens + E::kBins - 1) / E::kBins + 1023) / 1024 * 1024);
         tiles = (ntokens + tile - 1) / tile;
@@ -180,26 +188,25 @@ template <int DY, int OUT> hipError_t embed_sum(mbs::embed::BwdParams &p, const 
     return p.dim < S ? embed_sum<DY, OUT, 1>(p, f, st) : embed_sum<DY, OUT, S>(p, f, st);
 }
 
-template <int TOK, int DY, int OUT> hipError_t embed_direct(mbs::embed::BwdParams &p, hipStream_t st) {
+template <int TOK, int DY, int OUT> hipError_t embed_direct(mbs::embed::BwdParams &p, const EmbedPlan &f, hipStream_t st) {
     namespace E = mbs::embed;
-    uint32_t cols = p.dim < 4 ? 1 : (uint32_t)((p.dim + 255) / 256);
+    uint32_t cols = (uint32_t)((p.dim + 255) / 256);
+    const void *fn = p.dim < 4  ? f.by_row ? reinterpret_cast<const void *>(&E::sum_direct<TOK, DY, OUT, 1, true>)
+                                           : reinterpret_cast<const void *>(&E::sum_direct<TOK, DY, OUT, 1, false>)
+                     : f.by_row ? reinterpret_cast<const void *>(&E::sum_direct<TOK, DY, OUT, 4, true>)
+                                : reinterpret_cast<const void *>(&E::sum_direct<TOK, DY, OUT, 4, false>);
     void *args[] = {&p, &cols};
-    return hipLaunchKernel(p.dim < 4 ? reinterpret_cast<const void *>(&E::sum_direct<TOK, DY, OUT, 1>)
-                                     : reinterpret_cast<const void *>(&E::sum_direct<TOK, DY, OUT, 4>),
-                           dim3((unsigned)(p.vocab * cols)), dim3(64 * E::kDirectWaves), args, 0, st);
+    return hipLaunchKernel(fn, dim3((unsigned)f.direct_blocks), dim3(64 * E::kDirectWaves), args, 0, st);
 }
-template <int DY, int OUT> hipError_t embed_direct(mbs::embed::BwdParams &p, int32_t token_type, hipStream_t st) {
-    return token_type == MB_TOKEN_U8    ? embed_direct<0, DY, OUT>(p, st)
-           : token_type == MB_TOKEN_I32 ? embed_direct<1, DY, OUT>(p, st)
-                                        : embed_direct<2, DY, OUT>(p, st);
-}
-hipError_t embed_direct(mbs::embed::BwdParams &p, int32_t token_type, int32_t dy_dtype, int32_t out_dtype, hipStream_t st) {
-    if (dy_dtype == MB_F32) return out_dtype == MB_F32 ? embed_direct<0, 0>(p, token_type, st) : embed_direct<0, 1>(p, token_type, st);
-    return out_dtype == MB_F32 ? embed_direct<1, 0>(p, token_type, st) : embed_direct<1, 1>(p, token_type, st);
+template <int DY, int OUT> hipError_t embed_direct(mbs::embed::BwdParams &p, const EmbedPlan &f, int32_t token_type, hipStream_t st) {
+    return token_type == MB_TOKEN_U8    ? embed_direct<0, DY, OUT>(p, f, st)
+           : token_type == MB_TOKEN_I32 ? embed_direct<1, DY, OUT>(p, f, st)
+                                        : embed_direct<2, DY, OUT>(p, f, st);
 }
 
 template <int OUT> hipError_t embed_bwd(mbs::embed::BwdParams &p, const EmbedPlan &f, int32_t token_type, int32_t dy_dtype,
                                         char *ws, hipStream_t st) {
+    if (f.direct) return dy_dtype == MB_F32 ? embed_direct<0, OUT>(p, f, token_type, st) : embed_direct<1, OUT>(p, f, token_type, st);
     const hipError_t e = token_type == MB_TOKEN_U8    ? embed_sort<0, OUT>(p, f, ws, st)
                          : token_type == MB_TOKEN_I32 ? embed_sort<1, OUT>(p, f, ws, st)
                                                       : embed_sort<2, OUT>(p, f, ws, st);
@@ -486,7 +493,9 @@ int mb_embedding_bwd(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_
     mbs::embed::BwdParams p{};
     p.ntokens = ntokens; p.vocab = vocab; p.dim = dim;
     p.tokens = tokens; p.dy = dy; p.dweight = dweight; p.scale = scale;
-    if (f.direct) return status(embed_direct(p, token_type, dy_dtype, out_dtype, st_of(stream)));
+    if (f.direct)
+        return status(out_dtype == MB_F32 ? embed_bwd<0>(p, f, token_type, dy_dtype, nullptr, st_of(stream))
+                                          : embed_bwd<1>(p, f, token_type, dy_dtype, nullptr, st_of(stream)));
     Workspace ws(workspace, f.bytes, st_of(stream));
     if (!ws.at) return MB_ERR_HIP;
     p.passes = f.passes;

@@ -1,4 +1,4 @@
-"""The embedding's gradient at the edges between its ways of adding up: a workgroup per row (few tokens of few rows), the
+"""The embedding's gradient at the edges between its ways of adding up: a workgroup per row or per token (few tokens), the
 sort by one workgroup, the sort by many.  Tolerances as in test_gpu_embedding."""
 import numpy as np
 import pytest
@@ -8,7 +8,7 @@ from gpu_util import announce, has_gpu
 from test_gpu_embedding import DT, TOK, check_bwd, randn, shifted
 
 pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not has_gpu(), reason="needs a GPU")]
-FEW, MANY = 200, 9000              # rows of a table: a workgroup each, and too many for that
+FEW, MANY, TOO_MANY = 200, 9000, 131073        # rows of a table: a workgroup each; a workgroup per token; sorted
 
 
 def text(n, V, seed, padding=True):
@@ -22,7 +22,7 @@ def text(n, V, seed, padding=True):
     return torch.from_numpy(t).to("cuda:0")
 
 
-@pytest.mark.parametrize("V", [FEW, MANY])
+@pytest.mark.parametrize("V", [FEW, MANY, TOO_MANY])
 @pytest.mark.parametrize("n", [0, 1, 2, 7, 8, 9, 63, 64, 65, 511, 512, 513, 520, 1023, 1024, 1025, 2047, 2048, 2049, 4095, 4096, 4097])
 def test_tokens(n, V):
     announce(f"embedding_bwd n={n} V={V}")
@@ -33,27 +33,29 @@ def test_tokens(n, V):
 @pytest.mark.parametrize("d", [1, 2, 3, 4, 5, 8, 9, 255, 256, 257, 260, 511, 513, 1792])
 def test_widths(d, dd, od):
     announce(f"embedding_bwd dim={d} {dd}->{od}")
-    for V in (FEW, MANY):
+    for V in (FEW, MANY) if d > 257 else (FEW, MANY, TOO_MANY):
         check_bwd(text(700, V, d), randn((700, d), d + 1, dd), V, -0.5, od)
 
 
-@pytest.mark.parametrize("V,d", [(4096, 256), (4097, 256), (4096, 257), (2048, 512), (2048, 513), (1, 5), (4096, 3)])
-def test_rows_at_the_limit(V, d):
-    announce(f"embedding_bwd V={V} dim={d}")
-    check_bwd(text(1500, V, V + d), randn((1500, d), 3, "f32"), V, 1.0, "f32")
+@pytest.mark.parametrize("n,V,d", [(2048, 4096, 256), (2048, 4096, 257), (1024, 5000, 512), (1025, 5000, 512), (1024, 5000, 513),
+                                   (700, 1723, 4), (700, 1724, 4), (700, 1725, 4), (1500, 4097, 257), (1500, 2048, 513),
+                                   (40, 131072, 5), (2048, 131072, 3), (3, 1, 5), (100, 1025, 700), (100, 2049, 600)])
+def test_limits(n, V, d):
+    announce(f"embedding_bwd n={n} V={V} dim={d}")
+    check_bwd(text(n, V, V + d), randn((n, d), 3, "f32"), V, 1.0, "f32")
 
 
-@pytest.mark.parametrize("V", [FEW, MANY])
+@pytest.mark.parametrize("V", [FEW, MANY, TOO_MANY])
 @pytest.mark.parametrize("tok", ["u8", "i32", "i64"])
 def test_one_value_and_runs(tok, V):
-    """One row takes every token; each wave's share has a token of its own; only the last token counts."""
+    """One row takes every token; each wave's share has a token of its own; the last token is another."""
     announce(f"embedding_bwd one value, runs: {tok} V={V}")
-    dy = randn((2048, 300), 4, "bf16")
+    dy = randn((2048, 200), 4, "bf16")
     for t in (torch.full((2048,), 7), torch.arange(2048) // 256, torch.cat([torch.full((2047,), 255), torch.tensor([3])])):
         check_bwd(t.to("cuda:0").to(TOK[tok]), dy, V, 1.0, "f32")
 
 
-@pytest.mark.parametrize("V", [FEW, MANY])
+@pytest.mark.parametrize("V", [FEW, MANY, TOO_MANY])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_padding_infinities_and_addresses(dtype, V):
     import paper_2401_13660_amd as mb
@@ -73,7 +75,7 @@ def test_padding_infinities_and_addresses(dtype, V):
     check_bwd(t, dy.masked_fill(out[:, None], 0.0), V, 1.0, "f32")
 
 
-@pytest.mark.parametrize("V", [FEW, MANY])
+@pytest.mark.parametrize("V", [FEW, MANY, TOO_MANY])
 def test_in_a_graph(V):
     """Replays, with other work and other tokens between them."""
     import paper_2401_13660_amd as mb
