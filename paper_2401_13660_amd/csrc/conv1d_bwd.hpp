@@ -44,7 +44,7 @@ struct Params {
     void *dx;                     // (batch, dim, L) out
     float *dw, *dbias;            // (dim, K), (dim) or null
     float *dstate_in;             // (batch, dim, K-1) or null
-    float *part;                  // (nseg, batch, dim, K + 1): each stretch's share of dw and dbias
+    float *part;                  // (nseg, batch, dim, K + 1): each stretch's share of dw and dbias; null: nseg and batch are 1
     int64_t nseg;                 // stretches per row
     int32_t seg_tiles;            // tiles per stretch
     int apply_silu;
@@ -99,6 +99,13 @@ template <int S, int K> __device__ __forceinline__ void back_through_taps(float 
 #pragma unroll
         for (int j = 0; j < K; ++j) dx[i] = __builtin_fmaf(w[j], g[i + K - 1 - j], dx[i]);
     }
+}
+
+// A stretch's sum j: of dw's tap j, or (K) of dbias.  One sequence in one stretch per row: the result itself.
+template <int K> __device__ __forceinline__ void put_sum(const Params &p, int64_t item, int j, float s) {
+    if (p.part) p.part[item * (K + 1) + j] = s;
+    else if (j < K) p.dw[item * K + j] = s;
+    else if (p.dbias) p.dbias[item] = s;
 }
 
 // Rows of no timestep, or of more than 64 spans.  CUT: L is no multiple of the span, so a row's last span is cut.  The
@@ -205,7 +212,7 @@ __global__ __launch_bounds__(kThreads) void conv1d_bwd(Params p) {
 #pragma unroll
     for (int j = 0; j <= K; ++j) {
         const float s = wave_sum(acc[j]);
-        if (lane == j) p.part[item * (K + 1) + j] = s;
+        if (lane == j) put_sum<K>(p, item, j, s);
     }
 }
 
@@ -288,7 +295,7 @@ __global__ __launch_bounds__(kThreads) void conv1d_bwd_short(Params p) {
         float s = acc[j];
 #pragma unroll
         for (int off = 1; off < G; off *= 2) s += __shfl_xor(s, off, 64);
-        if (active && l == j) p.part[row * (K + 1) + j] = s;
+        if (active && l == j) put_sum<K>(p, row, j, s);
     }
 }
 

@@ -291,21 +291,29 @@ template <int IN, int OUT, int K> hipError_t conv_bwd_k(mbs::convbwd::Params &p,
                                               : reinterpret_cast<const void *>(&C::conv1d_bwd_short<IN, OUT, K, 16>);
     if (waves > 0)
         e = hipLaunchKernel(fn, dim3((unsigned)((waves + C::kWaves - 1) / C::kWaves)), dim3(C::kThreads), args, 0, st);
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || (waves > 0 && !p.part)) return e;
     return hipLaunchKernel(reinterpret_cast<const void *>(&C::conv1d_bwd_finish<K>),
                            dim3((unsigned)((p.dim * (K + 1) + C::kThreads - 1) / C::kThreads)), dim3(C::kThreads), args, 0, st);
 }
 
 // Stretches per row: enough for 4 waves per SIMD.  (2, 1536, 1021) fp32 in one, two and four stretches per row took 13.6,
 // 11.7 and 13.6 us, (1, 2048, 2047) in two, four and eight 14.7, 16.6 and 18.1 (with the finish): more waves hide more
-// latency, but each computes its edge again and leaves partial sums.
+// latency, but each computes its edge again and leaves partial sums.  One sequence in one stretch needs no finish (up to 4
+// tiles, or one wave per SIMD for each 4 of them): (1, 3584, 1021) fp32 10.1 us instead of 12.4 in two stretches, (1, 512, 1021)
+// 5.6 and 6.6, (1, 2048, 2048) 11.8 and 12.5; beyond, (1, 64, 2048) 7.6 and 5.3, (1, 1024, 4096) 19.2 and 13.8.
 void conv_bwd_segments(mbs::convbwd::Params &p, int32_t in_dtype, int32_t out_dtype) {
     const int64_t span = in_dtype == MB_F32 && out_dtype == MB_F32 ? 4 : 8;
     const int64_t rows = p.batch * p.dim, tiles = std::max<int64_t>((p.seqlen + 64 * span - 1) / (64 * span), 1);
     const int64_t want = 4 * 256 * 4;
-    const int64_t n = std::min(tiles, (want + rows - 1) / std::max<int64_t>(rows, 1));
+    const bool whole = p.batch == 1 && (tiles <= 4 || tiles * 256 <= rows);
+    const int64_t n = whole ? 1 : std::min(tiles, (want + rows - 1) / std::max<int64_t>(rows, 1));
     p.seg_tiles = (int32_t)((tiles + n - 1) / std::max<int64_t>(n, 1));
     p.nseg = (tiles + p.seg_tiles - 1) / p.seg_tiles;
+}
+
+// The workspace: the stretches' sums, none where a row's one stretch has the channel's sums.
+int64_t conv_bwd_bytes(const mbs::convbwd::Params &p, int64_t K) {
+    return p.batch * p.nseg == 1 ? 0 : p.batch * p.dim * (K + 1) * p.nseg * 4;
 }
 
 template <int IN, int OUT> hipError_t conv_bwd_dispatch(mbs::convbwd::Params &p, int K, hipStream_t st) {
@@ -315,6 +323,12 @@ template <int IN, int OUT> hipError_t conv_bwd_dispatch(mbs::convbwd::Params &p,
         case 3: return conv_bwd_k<IN, OUT, 3>(p, st);
         default: return conv_bwd_k<IN, OUT, 4>(p, st);
     }
+}
+
+hipError_t conv_bwd_launch(mbs::convbwd::Params &p, const mb_conv_desc *desc, hipStream_t st) {
+    if (desc->in_dtype == MB_F32)
+        return desc->out_dtype == MB_F32 ? conv_bwd_dispatch<0, 0>(p, desc->width, st) : conv_bwd_dispatch<0, 1>(p, desc->width, st);
+    return desc->out_dtype == MB_F32 ? conv_bwd_dispatch<1, 0>(p, desc->width, st) : conv_bwd_dispatch<1, 1>(p, desc->width, st);
 }
 
 // Partial sums, and the list where it does not fit the kernels' arguments.
@@ -543,25 +557,20 @@ int mb_conv1d_bwd(const mb_conv_desc *desc, const void *x, const float *w, const
     conv_bwd_segments(p, desc->in_dtype, desc->out_dtype);
     // a wave per row and stretch, and at most 2^32 threads in a launch
     if (rows * p.nseg >= (int64_t(1) << 26)) return MB_ERR_SHAPE;
-    const size_t part_b = (size_t)(padded * p.nseg) * 4;
+    const size_t part_b = (size_t)conv_bwd_bytes(p, K);
     if (!aligned(workspace, 16)) return MB_ERR_ALIGN;
     const Range outs[] = {{dx, (size_t)elems * out_sz}, {dw, w_b}, {dbias, bias ? b_b : 0}, {dstate_in, st_b},
-                          {workspace, part_b}};
+                          {workspace, workspace ? std::max<size_t>(part_b, 16) : 0}};
     if (any_overlap(outs, ins)) return MB_ERR_ALIAS;
 
     p.x = x; p.w = w; p.bias = bias; p.state_in = state_in; p.dy = dy; p.dstate_out = dstate_out;
     p.dx = dx; p.dw = dw; p.dbias = bias ? dbias : nullptr; p.dstate_in = dstate_in;
     p.apply_silu = desc->apply_silu ? 1 : 0;
+    if (part_b == 0) return status(conv_bwd_launch(p, desc, st_of(stream)));
     Workspace ws(workspace, part_b, st_of(stream));
     if (!ws.at) return MB_ERR_HIP;
     p.part = reinterpret_cast<float *>(ws.at);
-    hipStream_t st = ws.st;
-    hipError_t e;
-    if (desc->in_dtype == MB_F32)
-        e = desc->out_dtype == MB_F32 ? conv_bwd_dispatch<0, 0>(p, (int)K, st) : conv_bwd_dispatch<0, 1>(p, (int)K, st);
-    else
-        e = desc->out_dtype == MB_F32 ? conv_bwd_dispatch<1, 0>(p, (int)K, st) : conv_bwd_dispatch<1, 1>(p, (int)K, st);
-    return status(ws.done(e));
+    return status(ws.done(conv_bwd_launch(p, desc, ws.st)));
 }
 
 int64_t mb_conv1d_bwd_workspace(const mb_conv_desc *desc) {
@@ -576,7 +585,7 @@ int64_t mb_conv1d_bwd_workspace(const mb_conv_desc *desc) {
     mbs::convbwd::Params p{};
     p.batch = B; p.dim = D; p.seqlen = desc->seqlen;
     conv_bwd_segments(p, desc->in_dtype, desc->out_dtype);
-    return padded * p.nseg * 4;
+    return conv_bwd_bytes(p, K);
 }
 
 int mb_grad_norm(int64_t count, const void *const *grads, const int64_t *sizes, const int32_t *dtypes, float *norm,
