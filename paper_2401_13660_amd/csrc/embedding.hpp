@@ -13,12 +13,12 @@
 // goes on into other chunks are joined afterwards in the order of the chunks.  No atomic adds floats: a
 // result depends on the tokens and dy alone.
 //
-// 32,768 bytes of a text, width 1792 in bf16: 34 us, of which the sums take 22.4 (5.2 TB/s, the rate of
+// 32,768 bytes of a text, width 1792 in bf16: 34 us, of which the sums take 22.2 (5.2 TB/s, the rate of
 // a device copy), the sort's two launches 9 and the joining 4.4, a chain of loads each.  16,384 tokens
-// of a table of 32,000 rows of 768 fp32: 43 us, three launches of the sort at 7.6 to 10 (a third of
-// the table's 98 MB zeroed beside each), the sums 14.4 and the joining 4.5.  With a launch of its own
-// for each pass's counts the sort took four, 45 us in all; with the next pass's counts added in memory
-// token by token instead of in LDS 49: equal tokens meet in one counter.
+// of a table of 32,000 rows of 768 fp32: 41 us, three launches of the sort at 5 to 10 (a share of the
+// table's 98 MB zeroed beside each), the sums 14.4 and the joining 4.  With a launch of its own for each
+// pass's counts the sort took four, 45 us in all; with the next pass's counts added in memory token by
+// token instead of in LDS 49: equal tokens meet in one counter.
 #pragma once
 
 #include <hip/hip_runtime.h>

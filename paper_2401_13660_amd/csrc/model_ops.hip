@@ -120,19 +120,26 @@ struct EmbedPlan {
 template <int TOK, int OUT> hipError_t embed_sort(mbs::embed::BwdParams &p, const EmbedPlan &f, char *ws, hipStream_t st) {
     namespace E = mbs::embed;
     E::Pair *const ab[2] = {reinterpret_cast<E::Pair *>(ws + f.a), reinterpret_cast<E::Pair *>(ws + f.b)};
-    // the table is set to zero in equal shares beside the launches of the sort; 16-byte shares keep the stores aligned
-    const int64_t elems = p.vocab * p.dim, launches = f.tiles <= 1 ? 1 : f.merged ? f.passes + 1 : 2 * f.passes;
-    const int64_t share = ((elems + launches - 1) / launches + 63) / 64 * 64;
-    const int64_t zeroing = std::min<int64_t>((share + 4095) / 4096, 2048);     // workgroups of at least 4,096 elements
-    const dim3 grid((unsigned)(f.tiles + zeroing)), block(E::kThreads);
+    // the table is set to zero in shares beside the launches of the sort.  A scatter takes twice a count's time, and hides more:
+    // 98 MB in shares of 1, 3 and 3 41 to 45 us in all, in equal ones 42 to 47; larger tables keep every launch busy, 268 MB
+    // in equal shares 64 to 70, else 66 to 71
+    const int64_t elems = p.vocab * p.dim;
+    const int beside = elems * (OUT == 1 ? 2 : 4) <= int64_t(128) << 20 ? 3 : 1;
+    const int64_t parts = f.tiles <= 1 ? beside : f.passes * beside + (f.merged ? 1 : f.passes);
+    const dim3 block(E::kThreads);
+    int64_t part = 0, zeroing = 0;                      // workgroups of at least 4,096 elements
+    dim3 grid;
     p.zero_from = p.zero_to = 0;
-    auto next_share = [&] {
+    auto next_share = [&](int weight) {
+        part += weight;
         p.zero_from = p.zero_to;
-        p.zero_to = std::min(p.zero_from + share, elems);
+        p.zero_to = part == parts ? elems : std::min(elems, elems / parts * part / 64 * 64);    // the stores stay aligned
+        zeroing = std::min<int64_t>((p.zero_to - p.zero_from + 4095) / 4096, 2048);
+        grid = dim3((unsigned)(f.tiles + zeroing));
     };
     void *args[] = {&p};
     if (f.tiles <= 1) {
-        next_share();
+        next_share(beside);
         p.to = ab[0];
         p.tiles = 1;
         // 256 threads where they do: fewer waves' counts to add up.  The larger workgroups zero four times as much each
@@ -153,14 +160,14 @@ template <int TOK, int OUT> hipError_t embed_sort(mbs::embed::BwdParams &p, cons
         p.ahead = first && f.merged ? f.passes - 1 : 0;
         hipError_t e = hipSuccess;
         if (first || !f.merged) {
-            next_share();
+            next_share(1);
             // keys of later passes are no tokens: one instantiation for all token types
             e = hipLaunchKernel(first ? reinterpret_cast<const void *>(&E::count_digits<TOK, OUT, true>)
                                       : reinterpret_cast<const void *>(&E::count_digits<0, OUT, false>),
                                 grid, block, args, 0, st);
             if (e != hipSuccess) return e;
         }
-        next_share();
+        next_share(beside);
         const void *fn = first ? next ? reinterpret_cast<const void *>(&E::scatter<TOK, OUT, true, true>)
                                       : reinterpret_cast<const void *>(&E::scatter<TOK, OUT, true, false>)
                          : next ? reinterpret_cast<const void *>(&E::scatter<0, OUT, false, true>)
