@@ -32,6 +32,8 @@ namespace embed {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kBins = 256;         // digits of one pass of the sort
+constexpr int kWideBits = 10;      // of the one pass for tables a little larger
+constexpr int kWideTiles = 64;     // workgroups of it at most
 constexpr int kChunk = 64;         // sorted positions per wave at most: one per lane
 constexpr int kJoinWaves = 8;
 constexpr int kNone = -1;
@@ -57,7 +59,7 @@ struct BwdParams {
     int64_t zero_from, zero_to;    // elements of dweight that the launch sets to zero on the side
     int32_t passes;                // 8 bits each
     int32_t shift;                 // bits below this pass's digit
-    uint32_t *counts;              // (tiles, kBins)
+    uint32_t *counts;              // (tiles, digits)
     uint32_t *next_counts;         // the next pass's, counted by this one, or null
     int32_t ahead;                 // passes after the first whose counts the first launch sets to zero
     uint32_t *valid;               // tokens within the vocabulary
@@ -149,10 +151,10 @@ template <int OUT> __device__ __forceinline__ void zero_share(const BwdParams &p
 }
 
 // The lanes whose digit is this lane's, of those that have one.
-__device__ __forceinline__ uint64_t same_digit(uint32_t digit, bool has) {
+template <int BITS = 8> __device__ __forceinline__ uint64_t same_digit(uint32_t digit, bool has) {
     uint64_t same = __ballot(has);
 #pragma unroll
-    for (int b = 0; b < 8; ++b) {
+    for (int b = 0; b < BITS; ++b) {
         const uint64_t set = __ballot((digit >> b) & 1);
         same &= (digit >> b) & 1 ? set : ~set;
     }
@@ -160,13 +162,15 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t digit, bool has) {
 }
 
 // Digits of the workgroup's places, counted.
-template <int TOK, int OUT, bool FIRST>
+template <int TOK, int OUT, bool FIRST, int BITS>
 __global__ __launch_bounds__(kThreads) void count_digits(BwdParams p) {
+    constexpr int BINS = 1 << BITS;
     if ((int)blockIdx.x >= p.tiles) return zero_share<OUT>(p);
-    __shared__ uint32_t count[kBins];
+    __shared__ uint32_t count[BINS];
     const int64_t n = FIRST ? p.ntokens : (int64_t)*p.valid;
     const int64_t from = (int64_t)blockIdx.x * p.tile, to = min(from + p.tile, n);
-    count[threadIdx.x] = 0;
+#pragma unroll
+    for (int d = threadIdx.x; d < BINS; d += kThreads) count[d] = 0;
     for (int k = 0; FIRST && k < p.ahead; ++k) p.next_counts[(k * p.tiles + blockIdx.x) * kBins + threadIdx.x] = 0;
     for (int64_t i = from; i < to || i == from; i += kStep) {
         Keys<TOK, FIRST> keys;
@@ -174,10 +178,11 @@ __global__ __launch_bounds__(kThreads) void count_digits(BwdParams p) {
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < kPlaces; ++k)
-            if (keys.at[k] != kNone) atomicAdd(&count[(keys.at[k] >> p.shift) & (kBins - 1)], 1u);
+            if (keys.at[k] != kNone) atomicAdd(&count[(keys.at[k] >> p.shift) & (BINS - 1)], 1u);
     }
     __syncthreads();
-    p.counts[blockIdx.x * kBins + threadIdx.x] = count[threadIdx.x];
+#pragma unroll
+    for (int d = threadIdx.x; d < BINS; d += kThreads) p.counts[blockIdx.x * BINS + d] = count[d];
 }
 
 // Each place's key and position to the place that its digit gives it.  Every workgroup adds up the counts for itself:
@@ -185,13 +190,18 @@ __global__ __launch_bounds__(kThreads) void count_digits(BwdParams p) {
 //
 // NEXT (up to kNextTiles workgroups): it counts the next pass's digits too, by the workgroup that will find them, in LDS
 // and then in memory: whole numbers, so the order of the atomics changes nothing, and a pass takes one launch.
+//
+// Tables of 257 to 1,024 rows (bytes and a few more) take one pass of 10 bits: 300 rows of 1,024 in bf16, 8,000 tokens 18 us in
+// all, in two passes 25; 50,000 tokens 38 and 42; 131,000 77 and 75, since every workgroup adds up four times the counts,
+// hence kWideTiles.  3,000 tokens 16 us, in two passes by one workgroup 17.6.
 constexpr int kNextTiles = 32;
 
-template <int TOK, int OUT, bool FIRST, bool NEXT>
+template <int TOK, int OUT, bool FIRST, bool NEXT, int BITS>
 __global__ __launch_bounds__(kThreads) void scatter(BwdParams p) {
+    constexpr int BINS = 1 << BITS, PER = BINS / kThreads;      // a thread's digits, side by side
     if ((int)blockIdx.x >= p.tiles) return zero_share<OUT>(p);
     __shared__ uint32_t next[NEXT ? kNextTiles : 1][kBins];
-    __shared__ uint32_t at[kWaves][kBins], waves[kWaves];
+    __shared__ uint32_t at[kWaves][BINS], waves[kWaves];
     const int d = threadIdx.x, wave = d >> 6, lane = d & 63;
     const int64_t n = FIRST ? p.ntokens : (int64_t)*p.valid;
     const int64_t from = (int64_t)blockIdx.x * p.tile, to = min(from + p.tile, n);
@@ -201,23 +211,30 @@ __global__ __launch_bounds__(kThreads) void scatter(BwdParams p) {
         for (int g = 0; g < p.tiles; ++g) next[g][d] = 0;
     auto count_step = [&] {
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) at[w][d] = 0;
+        for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+            for (int j = 0; j < PER; ++j) at[w][d * PER + j] = 0;
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < kPlaces; ++k)
-            if (keys.at[k] != kNone) atomicAdd(&at[wave][(keys.at[k] >> p.shift) & (kBins - 1)], 1u);
+            if (keys.at[k] != kNone) atomicAdd(&at[wave][(keys.at[k] >> p.shift) & (BINS - 1)], 1u);
         __syncthreads();
     };
     count_step();
-    uint32_t total = 0, before = 0;
+    uint32_t total[PER] = {}, before[PER] = {}, mine = 0;
 #pragma unroll 16
     for (int g = 0; g < p.tiles; ++g) {
-        const uint32_t c = p.counts[g * kBins + d];
-        total += c;
-        before += g < (int)blockIdx.x ? c : 0u;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const uint32_t c = p.counts[g * BINS + d * PER + j];
+            total[j] += c;
+            before[j] += g < (int)blockIdx.x ? c : 0u;
+        }
     }
+#pragma unroll
+    for (int j = 0; j < PER; ++j) mine += total[j];
     // the digits below: within the wave, then the waves before
-    uint32_t below = total;
+    uint32_t below = mine;
 #pragma unroll
     for (int off = 1; off < 64; off *= 2) {
         const uint32_t v = __shfl_up(below, off, 64);
@@ -227,8 +244,13 @@ __global__ __launch_bounds__(kThreads) void scatter(BwdParams p) {
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) below += w < wave ? waves[w] : 0u;
-    if (FIRST && blockIdx.x == 0 && d == kBins - 1) *p.valid = below;
-    before += below - total;
+    if (FIRST && blockIdx.x == 0 && d == kThreads - 1) *p.valid = below;
+    below -= mine;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        before[j] += below;
+        below += total[j];
+    }
 
     for (int64_t i0 = from; i0 < to; i0 += kStep) {
         if (i0 > from) {
@@ -237,17 +259,19 @@ __global__ __launch_bounds__(kThreads) void scatter(BwdParams p) {
             count_step();
         }
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const uint32_t c = at[w][d];
-            at[w][d] = before;
-            before += c;
-        }
+        for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                const uint32_t c = at[w][d * PER + j];
+                at[w][d * PER + j] = before[j];
+                before[j] += c;
+            }
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < kPlaces; ++k) {
             const int64_t key = keys.at[k];
-            const uint32_t digit = (uint32_t)(key >> p.shift) & (kBins - 1);
-            const uint64_t same = same_digit(digit, key != kNone);
+            const uint32_t digit = (uint32_t)(key >> p.shift) & (BINS - 1);
+            const uint64_t same = same_digit<BITS>(digit, key != kNone);
             if (key != kNone) {
                 const int first = __ffsll((unsigned long long)same) - 1;
                 uint32_t base = 0;

@@ -82,6 +82,7 @@ struct EmbedPlan {
     int64_t tile, tiles, chunk, groups;
     int passes;
     bool merged;                                        // each pass counts the next one's digits
+    bool wide;                                          // one pass of kWideBits
     bool direct, by_row;                                // no sort: sum_direct, without a workspace
     int64_t direct_blocks;
     size_t counts, valid, a, b, head, tail, bytes;
@@ -95,19 +96,21 @@ struct EmbedPlan {
         direct = row_ok || place_ok;
         by_row = row_ok && (!place_ok || rows <= place_blocks);
         direct_blocks = by_row ? rows : place_blocks;
+        passes = 1;
+        while (passes < 4 && (vocab - 1) >> (8 * passes)) ++passes;
         // tokens per workgroup: 1,024, or what keeps the workgroups at kBins (each reads the counts of all)
         tile = std::max<int64_t>(1024, ((ntokens + E::kBins - 1) / E::kBins + 1023) / 1024 * 1024);
         tiles = (ntokens + tile - 1) / tile;
-        if (ntokens > 0 && ntokens <= E::kSmallTokens) tiles = 1;       // sorted by one workgroup at once
-        passes = 1;
-        while (passes < 4 && (vocab - 1) >> (8 * passes)) ++passes;
+        wide = passes == 2 && vocab <= 1 << E::kWideBits && ntokens > E::kDirectTokens && tiles <= E::kWideTiles;
+        if (wide) passes = 1;
+        if (!wide && ntokens > 0 && ntokens <= E::kSmallTokens) tiles = 1;  // sorted by one workgroup at once
         // sorted positions per wave: 64, or fewer where that leaves the SIMDs with less than two waves
         chunk = E::kChunk;
         while (chunk > 16 && ntokens / chunk * ((dim + 255) / 256) < 2048) chunk /= 2;
         groups = (ntokens + chunk * E::kWaves - 1) / (chunk * E::kWaves);
         Areas w;
         merged = tiles <= E::kNextTiles;                // tile is kStep then
-        counts = w.add((size_t)(merged ? passes : 1) * (size_t)tiles * E::kBins * 4);
+        counts = w.add((size_t)(merged ? passes : 1) * (size_t)tiles * (wide ? 1 << E::kWideBits : E::kBins) * 4);
         valid = w.add(4);
         a = w.add((size_t)ntokens * sizeof(E::Pair));
         b = w.add(passes > 1 ? (size_t)ntokens * sizeof(E::Pair) : 0);
@@ -162,16 +165,18 @@ template <int TOK, int OUT> hipError_t embed_sort(mbs::embed::BwdParams &p, cons
         if (first || !f.merged) {
             next_share(1);
             // keys of later passes are no tokens: one instantiation for all token types
-            e = hipLaunchKernel(first ? reinterpret_cast<const void *>(&E::count_digits<TOK, OUT, true>)
-                                      : reinterpret_cast<const void *>(&E::count_digits<0, OUT, false>),
+            e = hipLaunchKernel(f.wide  ? reinterpret_cast<const void *>(&E::count_digits<TOK, OUT, true, E::kWideBits>)
+                                : first ? reinterpret_cast<const void *>(&E::count_digits<TOK, OUT, true, 8>)
+                                        : reinterpret_cast<const void *>(&E::count_digits<0, OUT, false, 8>),
                                 grid, block, args, 0, st);
             if (e != hipSuccess) return e;
         }
         next_share(beside);
-        const void *fn = first ? next ? reinterpret_cast<const void *>(&E::scatter<TOK, OUT, true, true>)
-                                      : reinterpret_cast<const void *>(&E::scatter<TOK, OUT, true, false>)
-                         : next ? reinterpret_cast<const void *>(&E::scatter<0, OUT, false, true>)
-                                : reinterpret_cast<const void *>(&E::scatter<0, OUT, false, false>);
+        const void *fn = f.wide  ? reinterpret_cast<const void *>(&E::scatter<TOK, OUT, true, false, E::kWideBits>)
+                         : first ? next ? reinterpret_cast<const void *>(&E::scatter<TOK, OUT, true, true, 8>)
+                                        : reinterpret_cast<const void *>(&E::scatter<TOK, OUT, true, false, 8>)
+                         : next  ? reinterpret_cast<const void *>(&E::scatter<0, OUT, false, true, 8>)
+                                 : reinterpret_cast<const void *>(&E::scatter<0, OUT, false, false, 8>);
         e = hipLaunchKernel(fn, grid, block, args, 0, st);
         if (e != hipSuccess) return e;
     }

@@ -45,6 +45,16 @@ def test_limits(n, V, d):
     check_bwd(text(n, V, V + d), randn((n, d), 3, "f32"), V, 1.0, "f32")
 
 
+@pytest.mark.parametrize("tok,n", [("i32", 2049), ("i64", 3000), ("u8", 4096), ("i32", 4097), ("i64", 5000), ("i32", 32768),
+                                   ("u8", 32769), ("i64", 65536), ("i32", 65537)])
+@pytest.mark.parametrize("V", [256, 257, 511, 700, 1023, 1024, 1025])
+def test_a_few_more_rows_than_bytes(tok, n, V):
+    announce(f"embedding_bwd n={n} V={V} {tok}")
+    t = text(n, V, n + V, tok != "u8").to(TOK[tok])
+    check_bwd(t, randn((n, 12), 5, "bf16"), V, 1.0, "f32")
+    check_bwd(t.clamp(max=0), randn((n, 12), 6, "bf16"), V, 1.0, "bf16")
+
+
 @pytest.mark.parametrize("V", [FEW, MANY, TOO_MANY])
 @pytest.mark.parametrize("tok", ["u8", "i32", "i64"])
 def test_one_value_and_runs(tok, V):
