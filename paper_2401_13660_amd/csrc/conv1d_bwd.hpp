@@ -183,7 +183,10 @@ __global__ __launch_bounds__(kThreads) void conv1d_bwd(Params p) {
 #pragma unroll
             for (int i = 0; i < S; ++i) g[i] = t0 + i < L ? g[i] : 0.0f;
         }
-        add_products<S, K>(acc, g, xin);
+        float part[K + 1] = {};                         // a tile's sums of their own: a row's one running sum would round L / 64 times
+        add_products<S, K>(part, g, xin);
+#pragma unroll
+        for (int j = 0; j <= K; ++j) acc[j] += part[j];
 #pragma unroll
         for (int j = 0; j < H; ++j) {
             g[S + j] = from_lane_after(g[j], carry[j]);
