@@ -485,10 +485,6 @@ __global__ __launch_bounds__(64 * kDirectWaves) void sum_direct(BwdParams p, uin
     store_span<OUT, S>(p.dweight, v * p.dim + col, acc);
 }
 
-// Everything asked of memory has arrived (vmcnt 0).  Loads and stores share that counter and a wait is for the oldest of
-// both, so a wave that waited row by row would wait for each sum that it stored in between as well.
-__device__ __forceinline__ void wait_for_memory() { __builtin_amdgcn_s_waitcnt(0x0f70); }
-
 // Sums of the rows of a group of kWaves chunks, one chunk per wave, for one tile of columns.
 template <int DY, int OUT, int S>
 __global__ __launch_bounds__(kThreads) void sum_chunks(BwdParams p, uint32_t col_tiles) {

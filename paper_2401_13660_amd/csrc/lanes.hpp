@@ -118,6 +118,10 @@ template <int DT, int S> __device__ __forceinline__ void store_first(void *p, in
         if (i < n) st_out<DT>(p, at + i, v[i]);
 }
 
+// Everything asked of memory has arrived (vmcnt 0).  Loads and stores share that counter and a wait is for the oldest of
+// both, so a wave that waited row by row would wait for each sum that it stored in between as well.
+__device__ __forceinline__ void wait_for_memory() { __builtin_amdgcn_s_waitcnt(0x0f70); }
+
 // Each lane's neighbour's value; the wave's first (last) lane takes `edge`.
 __device__ __forceinline__ float from_lane_before(float v, float edge) {
     return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(edge), __float_as_int(v), 0x138, 0xf, 0xf, false));

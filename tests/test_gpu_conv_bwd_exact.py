@@ -1,0 +1,100 @@
+"""The convolution's gradient in whole numbers: inputs within 3, taps in halves, no Swish, so that every product and every
+partial sum of any order is exact in fp32 (9 batch L below 2^24) and the results have to be equal to the last bit.
+
+The definition has a term per existing pair of a timestep and an input: an infinity or a NaN spoils the terms that it is
+in, and no others."""
+import pytest
+import torch
+
+from gpu_util import announce, has_gpu
+from test_gpu_embedding import DT
+
+pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not has_gpu(), reason="needs a GPU")]
+INF, NAN = float("inf"), float("nan")
+
+
+def whole(shape, g, most=3):
+    return torch.randint(-most, most + 1, shape, generator=g, device="cuda:0")
+
+
+def inputs(B, D, L, K, dtype, out, seed):
+    g = torch.Generator(device="cuda:0").manual_seed(seed)
+    return dict(x=whole((B, D, L), g).to(DT[dtype]), dy=whole((B, D, L), g).to(DT[out]), w=whole((D, K), g, 2) * 0.5,
+                bias=whole((D,), g).float(), state=whole((B, D, K - 1), g).float(),
+                dstate_out=whole((B, D, K - 1), g).float())
+
+
+def plain(a):
+    """Every existing term, in 64 bits."""
+    x, dy, w = a["x"].double(), a["dy"].double(), a["w"].double()
+    L, K = x.shape[2], w.shape[1]
+    ext = torch.cat([a["state"].double(), x], 2)
+    dext = torch.zeros_like(ext)
+    dext[:, :, L:] += a["dstate_out"].double()
+    for j in range(K):
+        dext[:, :, j:j + L] += dy * w[:, j:j + 1]
+    dw = torch.stack([(dy * ext[:, :, j:j + L]).sum((0, 2)) for j in range(K)], 1)
+    return dict(dx=dext[:, :, K - 1:], dw=dw, dbias=dy.sum((0, 2)), dstate=dext[:, :, :K - 1])
+
+
+def check(a):
+    import paper_2401_13660_amd as mb
+    g = mb.conv1d_bwd(a["x"], a["w"], a["dy"], a["bias"], a["state"], a["dstate_out"], apply_silu=False)
+    ref = plain(a)
+    for k in ref:
+        assert torch.equal(torch.nan_to_num(g[k].double(), 1e30, 2e30, -2e30), torch.nan_to_num(ref[k], 1e30, 2e30, -2e30)), k
+
+
+# rows of one span and less, of 16, 32 and 64 spans, of whole tiles and cut ones, in one stretch and in several
+LENGTHS = [1, 2, 3, 7, 39, 40, 64, 128, 130, 255, 256, 257, 511, 512, 513, 516, 1023, 1024, 1027, 2050, 4096]
+
+
+@pytest.mark.parametrize("K", [1, 2, 3, 4])
+@pytest.mark.parametrize("dtype,out", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16")])
+def test_lengths(dtype, out, K):
+    announce(f"conv1d_bwd exact, K={K} {dtype} {out}")
+    for L in LENGTHS:
+        for B in (1, 3):
+            check(inputs(B, 5, L, K, dtype, out, L + B))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,D,L", [(1, 3, 20480), (2, 2, 9000), (5, 7, 4099), (1, 4100, 2600), (40, 3, 5001), (1, 1, 300001),
+                                   (300, 20, 33)])
+def test_stretches_and_batches(dtype, B, D, L):
+    announce(f"conv1d_bwd exact ({B}, {D}, {L}) {dtype}")
+    check(inputs(B, D, L, 4, dtype, dtype, B + D + L))
+
+
+@pytest.mark.parametrize("K", [2, 4])
+@pytest.mark.parametrize("dtype,out", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16")])
+@pytest.mark.parametrize("bad", [INF, -INF, NAN])
+def test_what_stands_at_a_rows_end(dtype, out, K, bad):
+    """An infinity or NaN among a row's last inputs reaches the taps that see it, one among its last gradients the inputs
+    that it flows to, one among the taps the inputs that it multiplies."""
+    announce(f"conv1d_bwd: {bad} at the rows' ends, K={K} {dtype} {out}")
+    for L in LENGTHS:
+        for back in range(1, min(K, L) + 1):
+            a = inputs(2, 7, L, K, dtype, out, L + back)
+            a["x"][1, 2, L - back] = bad
+            a["dy"][0, 4, L - back] = bad
+            a["w"][6, back - 1] = bad
+            check(a)
+
+
+@pytest.mark.parametrize("L", [16, 40, 130, 260, 512, 1100])
+def test_other_rows_keep_their_bits(L):
+    """Whatever a row's end holds, the rows beside it come out as without it."""
+    import paper_2401_13660_amd as mb
+    announce(f"conv1d_bwd: rows beside one with infinities, L={L}")
+    a = inputs(1, 12, L, 4, "f32", "bf16", L)
+    a = dict(a, x=a["x"] + 0.3, w=a["w"] + 0.1)             # sums that round
+    args = a["dy"], a["bias"], a["state"], a["dstate_out"]
+    clean = mb.conv1d_bwd(a["x"], a["w"], *args, apply_silu=False)
+    a["x"][0, 5, L - 1], a["w"][9, 1] = INF, NAN
+    g = mb.conv1d_bwd(a["x"], a["w"], *args, apply_silu=False)
+    others = [i for i in range(12) if i not in (5, 9)]
+    for k in ("dw", "dbias"):
+        assert torch.equal(g[k][others], clean[k][others]), k
+    for k in ("dx", "dstate"):
+        assert torch.equal(g[k][:, others], clean[k][:, others]), k
