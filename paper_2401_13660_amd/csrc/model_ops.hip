@@ -89,10 +89,11 @@ struct EmbedPlan {
     EmbedPlan(int64_t ntokens, int64_t vocab, int64_t dim) {
         namespace E = mbs::embed;
         // few tokens: a workgroup per row of the table or per token, whichever are fewer, where either are few enough
-        const int64_t cols = (dim + 255) / 256, rows = vocab * cols, places = ntokens * cols;
+        // (without tokens the rows are as wide: one workgroup counts a row's spans in 32 bits)
+        const int64_t cols = (dim + 255) / 256, rows = vocab * cols, places = std::max<int64_t>(ntokens, 1) * cols;
         const bool few = ntokens <= E::kDirectTokens, row_ok = few && rows <= E::kDirectRows;
         const bool place_ok = few && places <= E::kDirectPlaces && vocab <= E::kZeroRows * E::kZeroBlocks;
-        const int64_t place_blocks = places + std::min<int64_t>(vocab, E::kZeroBlocks);
+        const int64_t place_blocks = ntokens * cols + std::min<int64_t>(vocab, E::kZeroBlocks);
         direct = row_ok || place_ok;
         by_row = row_ok && (!place_ok || rows <= place_blocks);
         direct_blocks = by_row ? rows : place_blocks;
