@@ -515,6 +515,12 @@ def _workspace(size, what, dev):
     return torch.empty(size, dtype=torch.uint8, device=dev)
 
 
+def _was_written(tensors):
+    """A caller's tensors were written through their addresses: counted, so that autograd refuses a gradient for which it
+    had saved one."""
+    torch.autograd.graph.increment_version([t for t in tensors if not t.is_inference()])
+
+
 _TOKEN_TYPES = {torch.uint8: 0, torch.int32: 1, torch.int64: 2}
 
 
@@ -541,7 +547,7 @@ def embedding_fwd(tokens, weight, *, scale=1.0, out_dtype=None, out=None):
     dev = weight.device
     _need(weight, "weight", (V, d))
     code = _tokens(tokens, dev)
-    shape = tuple(tokens.shape) + (d,)
+    shape, given = tuple(tokens.shape) + (d,), out is not None
     if out is None:
         out = torch.empty(shape, dtype=out_dtype or weight.dtype, device=dev)
     else:
@@ -550,6 +556,8 @@ def embedding_fwd(tokens, weight, *, scale=1.0, out_dtype=None, out=None):
         st = lib.mb_embedding_fwd(tokens.numel(), V, d, code, _dt(weight.dtype), _dt(out.dtype), float(scale),
                                   _ptr(tokens), _ptr(weight), _ptr(out), _stream(dev))
     _check(st, "mb_embedding_fwd")
+    if given:
+        _was_written([out])
     return out
 
 
@@ -569,6 +577,7 @@ def embedding_bwd(tokens, dy, vocab, *, scale=1.0, out_dtype=torch.float32, out=
     vocab = int(vocab)
     if vocab < 0:
         raise MBScanError("vocab must not be negative")
+    given = out is not None
     if out is None:
         out = torch.empty((vocab, d), dtype=out_dtype, device=dev)
     else:
@@ -578,6 +587,8 @@ def embedding_bwd(tokens, dy, vocab, *, scale=1.0, out_dtype=torch.float32, out=
         st = lib.mb_embedding_bwd(tokens.numel(), vocab, d, code, _dt(dy.dtype), _dt(out.dtype), float(scale),
                                   _ptr(tokens), _ptr(dy), _ptr(out), _ptr(ws), _stream(dev))
     _check(st, "mb_embedding_bwd")
+    if given:
+        _was_written([out])
     return out
 
 
@@ -677,6 +688,7 @@ def clip_grad_norm(grads, max_norm, *, eps=1e-6, out=None):
         st = lib.mb_clip_grad_norm(len(grads), ptrs, optrs, sizes, types, float(max_norm), float(eps), _ptr(norm),
                                    _ptr(ws), _stream(dev))
     _check(st, "mb_clip_grad_norm")
+    _was_written(grads if out is None else out)
     return norm
 
 

@@ -20,6 +20,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <initializer_list>
+#include <optional>
 #include <vector>
 
 #include "mbscan.h"
@@ -339,6 +340,12 @@ PyObject *verify_rank(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
 
 void *data(const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
 
+// A caller's tensor was written through its address: counted, so that autograd refuses a gradient for which it had saved it.
+void was_written(PyObject *o) {
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 // A real number as a float; ok becomes false where it is none.
 float real(PyObject *o, bool &ok) {
     const double v = PyFloat_CheckExact(o) ? PyFloat_AS_DOUBLE(o) : PyLong_CheckExact(o) ? PyLong_AsDouble(o) : (ok = false, 0.0);
@@ -374,6 +381,7 @@ PyObject *embedding_fwd(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
                                     wp, op, c.stream);
         });
         if (st != MB_OK) return PyLong_FromLong(st);
+        if (a[4] != Py_None) was_written(a[4]);
         return a[4] == Py_None ? wrap(std::move(out)) : same(a[4]);
     });
 }
@@ -408,6 +416,7 @@ PyObject *embedding_bwd(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
                                     yp, op, data(ws), c.stream);
         });
         if (st != MB_OK) return PyLong_FromLong(st);
+        if (a[5] != Py_None) was_written(a[5]);
         return a[5] == Py_None ? wrap(std::move(out)) : same(a[5]);
     });
 }
@@ -447,8 +456,10 @@ PyObject *conv1d_bwd(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
     });
 }
 
-// A list or tuple of dense fp32 and bf16 tensors on one device, as the library takes it.
+// A list or tuple of dense fp32 and bf16 tensors on one device, as the library takes it.  It holds them: another thread may
+// change the list while the library is called without the interpreter lock.
 struct TensorList {
+    std::vector<PyObject *> held;
     std::vector<const void *> at;
     std::vector<int64_t> sizes;
     std::vector<int32_t> types;
@@ -458,6 +469,7 @@ struct TensorList {
         const Py_ssize_t n = PySequence_Fast_GET_SIZE(o);
         PyObject **item = PySequence_Fast_ITEMS(o), **other = like ? PySequence_Fast_ITEMS(like) : nullptr;
         if (like && PySequence_Fast_GET_SIZE(like) != n) c.ok = false;
+        held.reserve(n);
         at.reserve(n);
         if (!like) { sizes.reserve(n); types.reserve(n); }
         for (Py_ssize_t i = 0; c.ok && i < n; ++i) {
@@ -471,8 +483,13 @@ struct TensorList {
                 sizes.push_back(t->numel());
                 types.push_back(code(t->scalar_type()));
             }
+            held.push_back(same(item[i]));
             at.push_back(t->data_ptr());
         }
+    }
+    TensorList(const TensorList &) = delete;
+    ~TensorList() {
+        for (PyObject *o : held) Py_DECREF(o);
     }
 };
 
@@ -505,24 +522,23 @@ PyObject *clip_grad_norm(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
         const float max_norm = real(a[1], c.ok), eps = real(a[2], c.ok);
         PLAIN_OR_NONE(c);
         // what is written are gradients, not the parameters that torch's function of this name takes
-        PyObject *written = a[3] == Py_None ? a[0] : a[3];
-        for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(written); ++i) {
-            const at::Tensor *t = plain(PySequence_Fast_ITEMS(written)[i]);
-            if (!t || t->requires_grad()) Py_RETURN_NONE;
-        }
+        std::optional<TensorList> given;
+        if (a[3] != Py_None) given.emplace(c, a[3], a[0]);
+        PLAIN_OR_NONE(c);
+        const TensorList &written = given ? *given : g;
         std::vector<void *> out;
-        if (a[3] != Py_None) {
-            const TensorList o(c, a[3], a[0]);
-            PLAIN_OR_NONE(c);
-            for (const void *p : o.at) out.push_back(const_cast<void *>(p));
-        }
+        for (PyObject *o : written.held)
+            if (THPVariable_Unpack(o).requires_grad()) Py_RETURN_NONE;
+        for (size_t i = 0; given && i < written.at.size(); ++i) out.push_back(const_cast<void *>(written.at[i]));
         const int64_t n = (int64_t)g.at.size();
         at::Tensor norm = c.fresh({}, at::kFloat), ws = c.workspace(grad_norm_workspace_fn(n));
         const int st = unlocked([&] {
-            return clip_grad_norm_fn(n, g.at.data(), a[3] != Py_None ? out.data() : nullptr, g.sizes.data(), g.types.data(),
+            return clip_grad_norm_fn(n, g.at.data(), given ? out.data() : nullptr, g.sizes.data(), g.types.data(),
                                      max_norm, eps, static_cast<float *>(norm.data_ptr()), data(ws), c.stream);
         });
-        return st != MB_OK ? PyLong_FromLong(st) : wrap(std::move(norm));
+        if (st != MB_OK) return PyLong_FromLong(st);
+        for (PyObject *o : written.held) was_written(o);
+        return wrap(std::move(norm));
     });
 }
 
