@@ -370,7 +370,7 @@ int mb_embedding_fwd(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_
  *
  *   tokens  token_type (ntokens)       ntokens below 2^31
  *   dy      dy_dtype (ntokens, dim)
- *   dweight out_dtype (vocab, dim)     must not overlap an input; ntokens * dim below 2^37
+ *   dweight out_dtype (vocab, dim)     must not overlap an input; with tokens, dim below 2^30 and ntokens * dim below 2^37
  *   workspace  device memory of mb_embedding_bwd_workspace(ntokens, vocab, dim) bytes (of a
  *              negative mb_status where the sizes are refused; 0: none is used), 16-byte aligned,
  *              that nothing else uses until the call's work is done; NULL: the call allocates it on the stream
@@ -393,7 +393,7 @@ int64_t mb_embedding_bwd_workspace(int64_t ntokens, int64_t vocab, int64_t dim);
  *   dstate_in   float (B, D, k-1)     NULL means not written
  * Outputs are overwritten (not accumulated) and must not overlap any other
  * argument; with no row or no timestep dw and dbias are zeros.  B * D below
- * 2^26, D and L below 2^31.  Arithmetic is fp32; results are deterministic.
+ * 2^26, D * (k + 1) below 255 * 2^24, L below 2^31.  Arithmetic is fp32; results are deterministic.
  *   workspace   as for mb_embedding_bwd, of mb_conv1d_bwd_workspace(desc) bytes
  */
 int mb_conv1d_bwd(const mb_conv_desc *desc, const void *x, const float *w, const float *bias, const float *state_in,

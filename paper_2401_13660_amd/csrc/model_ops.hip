@@ -119,6 +119,11 @@ struct EmbedPlan {
         tail = w.add((size_t)groups * (size_t)dim * 4);
         bytes = direct ? 0 : w.bytes;
     }
+    // Do the sums' launches, of 256 and 512 threads per group and tile of columns, have less than 2^32 threads?
+    bool launches(int64_t dim) const {
+        const int64_t cols = (dim + 255) / 256;
+        return direct || (groups * cols < int64_t(1) << 24 && (groups - 1) * cols < int64_t(1) << 23);
+    }
 };
 
 template <int TOK, int OUT> hipError_t embed_sort(mbs::embed::BwdParams &p, const EmbedPlan &f, char *ws, hipStream_t st) {
@@ -227,14 +232,6 @@ template <int OUT> hipError_t embed_bwd(mbs::embed::BwdParams &p, const EmbedPla
     return dy_dtype == MB_F32 ? embed_sum<0, OUT>(p, f, st) : embed_sum<1, OUT>(p, f, st);
 }
 
-// Row and token numbers, and a last piece's tokens past the vocabulary, stay below 2^31.
-bool sample_sizes(int64_t batch, int64_t ndraft, int64_t vocab) {
-    constexpr int64_t most = int64_t(1) << 31;
-    // and a launch has less than 2^32 threads
-    if (vocab <= mbs::sample::kSmallVocab && batch >= most / (32 * mbs::sample::kMaxWaves)) return false;
-    return batch < most && ndraft < most - mbs::sample::kMaxWaves && vocab < most - mbs::sample::kPiece;
-}
-
 // The pieces of a large vocabulary's rows; none for a small one's.
 struct SamplePlan {
     int64_t pieces = 0, race_pieces = 0, blocks = 0;
@@ -251,6 +248,19 @@ struct SamplePlan {
         bytes = w.bytes;
     }
 };
+
+// The checks of its sizes, for the call and for its workspace.  Row and token numbers, and a last piece's tokens past the
+// vocabulary, stay below 2^31, and a launch has less than 2^32 threads.
+bool sample_sizes(int64_t batch, int64_t ndraft, int64_t vocab) {
+    constexpr int64_t most = int64_t(1) << 31;
+    if (batch < 0 || ndraft < 0 || vocab < 1) return false;
+    if (batch >= most || ndraft >= most - mbs::sample::kMaxWaves || vocab >= most - mbs::sample::kPiece) return false;
+    int64_t rows, elems;
+    if (!mul_ok(batch, ndraft + 1, &rows) || !mul_ok(rows, vocab, &elems)) return false;
+    if (vocab <= mbs::sample::kSmallVocab) return batch < most / (32 * mbs::sample::kMaxWaves);
+    const SamplePlan f(batch, ndraft, vocab);
+    return f.blocks < (int64_t(1) << 23) && batch * f.race_pieces < (int64_t(1) << 23);
+}
 
 template <int DT> hipError_t sample_launch(mbs::sample::Params &p, const SamplePlan &f, void *workspace, hipStream_t st) {
     namespace S = mbs::sample;
@@ -286,6 +296,15 @@ int embed_checks(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_type
     if (!valid_token_type(token_type) || !valid_dtype(in_dtype) || !valid_dtype(out_dtype)) return MB_ERR_DTYPE;
     if (ntokens >= kMaxElems || !mul_ok(ntokens, dim, row_elems) || !mul_ok(vocab, dim, table_elems)) return MB_ERR_SHAPE;
     return MB_OK;
+}
+
+// Those of the gradient alone, before its plan is made.
+int embed_bwd_checks(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_type, int32_t dy_dtype, int32_t out_dtype,
+                     int64_t *row_elems, int64_t *table_elems) {
+    const int st = embed_checks(ntokens, vocab, dim, token_type, dy_dtype, out_dtype, row_elems, table_elems);
+    if (st != MB_OK) return st;
+    if (ntokens >= (int64_t(1) << 31)) return MB_ERR_SHAPE;
+    return *table_elems == 0 || EmbedPlan(ntokens, vocab, dim).launches(dim) ? MB_OK : MB_ERR_SHAPE;
 }
 
 template <int IN, int OUT, int K> hipError_t conv_bwd_k(mbs::convbwd::Params &p, hipStream_t st) {
@@ -327,6 +346,22 @@ void conv_bwd_segments(mbs::convbwd::Params &p, int32_t in_dtype, int32_t out_dt
 // The workspace: the stretches' sums, none where a row's one stretch has the channel's sums.
 int64_t conv_bwd_bytes(const mbs::convbwd::Params &p, int64_t K) {
     return p.batch * p.nseg == 1 ? 0 : p.batch * p.dim * (K + 1) * p.nseg * 4;
+}
+
+// The checks of its sizes and types, for the call and for its workspace.  p: the sizes and stretches.
+int conv_bwd_checks(const mb_conv_desc *desc, mbs::convbwd::Params &p, int64_t *elems) {
+    if (!desc) return MB_ERR_NULL;
+    const int64_t B = desc->batch, D = desc->dim, L = desc->seqlen, K = desc->width;
+    if (B < 0 || D < 0 || L < 0) return MB_ERR_SHAPE;
+    if (!valid_dtype(desc->in_dtype) || !valid_dtype(desc->out_dtype)) return MB_ERR_DTYPE;
+    if (K < 1 || K > 4 || desc->reserved != 0 || desc->reserved2 != 0) return MB_ERR_UNSUPPORTED;
+    int64_t rows, padded;
+    if (!mul_ok(B, D, &rows) || !mul_ok(rows, L, elems) || !mul_ok(rows, K + 1, &padded)) return MB_ERR_SHAPE;
+    if (D >= (int64_t(1) << 31) || rows >= (int64_t(1) << 31) || L >= (int64_t(1) << 31)) return MB_ERR_SHAPE;
+    p.batch = B; p.dim = D; p.seqlen = L;
+    conv_bwd_segments(p, desc->in_dtype, desc->out_dtype);
+    // a wave per row and stretch, a thread per sum, and less than 2^32 threads in a launch
+    return rows * p.nseg >= (int64_t(1) << 26) || D * (K + 1) >= int64_t(255) << 24 ? MB_ERR_SHAPE : MB_OK;
 }
 
 template <int IN, int OUT> hipError_t conv_bwd_dispatch(mbs::convbwd::Params &p, int K, hipStream_t st) {
@@ -503,9 +538,8 @@ int mb_embedding_fwd(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_
 int mb_embedding_bwd(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_type, int32_t dy_dtype, int32_t out_dtype,
                      float scale, const void *tokens, const void *dy, void *dweight, void *workspace, void *stream) {
     int64_t row_elems, table_elems;
-    const int st = embed_checks(ntokens, vocab, dim, token_type, dy_dtype, out_dtype, &row_elems, &table_elems);
+    const int st = embed_bwd_checks(ntokens, vocab, dim, token_type, dy_dtype, out_dtype, &row_elems, &table_elems);
     if (st != MB_OK) return st;
-    if (ntokens >= (int64_t(1) << 31)) return MB_ERR_SHAPE;
     if (table_elems == 0) return MB_OK;
     if (!dweight || (ntokens > 0 && (!tokens || !dy))) return MB_ERR_NULL;
     const size_t tsz = token_size(token_type), ysz = dtype_size(dy_dtype), osz = dtype_size(out_dtype);
@@ -516,7 +550,6 @@ int mb_embedding_bwd(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_
                           {workspace, workspace ? std::max<size_t>(f.bytes, 16) : 0}};
     const Range ins[] = {{tokens, (size_t)ntokens * tsz}, {dy, (size_t)row_elems * ysz}};
     if (any_overlap(outs, ins)) return MB_ERR_ALIAS;
-    if (f.groups * ((dim + 255) / 256) >= (int64_t(1) << 22)) return MB_ERR_SHAPE;
     mbs::embed::BwdParams p{};
     p.ntokens = ntokens; p.vocab = vocab; p.dim = dim;
     p.tokens = tokens; p.dy = dy; p.dweight = dweight; p.scale = scale;
@@ -537,23 +570,19 @@ int mb_embedding_bwd(int64_t ntokens, int64_t vocab, int64_t dim, int32_t token_
 
 int64_t mb_embedding_bwd_workspace(int64_t ntokens, int64_t vocab, int64_t dim) {
     int64_t row_elems, table_elems;
-    const int st = embed_checks(ntokens, vocab, dim, MB_TOKEN_U8, MB_F32, MB_F32, &row_elems, &table_elems);
+    const int st = embed_bwd_checks(ntokens, vocab, dim, MB_TOKEN_U8, MB_F32, MB_F32, &row_elems, &table_elems);
     if (st != MB_OK) return st;
-    if (ntokens >= (int64_t(1) << 31)) return MB_ERR_SHAPE;
-    return (int64_t)EmbedPlan(ntokens, vocab, dim).bytes;
+    return table_elems == 0 ? 0 : (int64_t)EmbedPlan(ntokens, vocab, dim).bytes;
 }
 
 int mb_conv1d_bwd(const mb_conv_desc *desc, const void *x, const float *w, const float *bias, const float *state_in,
                   const void *dy, const float *dstate_out, void *dx, float *dw, float *dbias, float *dstate_in,
                   void *workspace, void *stream) {
-    if (!desc) return MB_ERR_NULL;
-    const int64_t B = desc->batch, D = desc->dim, L = desc->seqlen, K = desc->width;
-    if (B < 0 || D < 0 || L < 0) return MB_ERR_SHAPE;
-    if (!valid_dtype(desc->in_dtype) || !valid_dtype(desc->out_dtype)) return MB_ERR_DTYPE;
-    if (K < 1 || K > 4 || desc->reserved != 0 || desc->reserved2 != 0) return MB_ERR_UNSUPPORTED;
-    int64_t rows, elems, padded;
-    if (!mul_ok(B, D, &rows) || !mul_ok(rows, L, &elems) || !mul_ok(rows, K + 1, &padded)) return MB_ERR_SHAPE;
-    if (D >= (int64_t(1) << 31) || rows >= (int64_t(1) << 31) || L >= (int64_t(1) << 31)) return MB_ERR_SHAPE;
+    mbs::convbwd::Params p{};
+    int64_t elems;
+    const int bad = conv_bwd_checks(desc, p, &elems);
+    if (bad != MB_OK) return bad;
+    const int64_t D = p.dim, K = desc->width, rows = p.batch * D;
     if (D == 0) return MB_OK;
     if (!w || !dw || (bias && !dbias)) return MB_ERR_NULL;
     if (elems > 0 && (!x || !dy || !dx)) return MB_ERR_NULL;
@@ -565,11 +594,6 @@ int mb_conv1d_bwd(const mb_conv_desc *desc, const void *x, const float *w, const
     const size_t w_b = (size_t)(D * K) * 4, b_b = (size_t)D * 4, st_b = (size_t)(rows * (K - 1)) * 4;
     const Range ins[] = {{x, (size_t)elems * in_sz}, {w, w_b}, {bias, b_b}, {state_in, st_b}, {dy, (size_t)elems * out_sz},
                          {dstate_out, st_b}};
-    mbs::convbwd::Params p{};
-    p.batch = B; p.dim = D; p.seqlen = L;
-    conv_bwd_segments(p, desc->in_dtype, desc->out_dtype);
-    // a wave per row and stretch, and at most 2^32 threads in a launch
-    if (rows * p.nseg >= (int64_t(1) << 26)) return MB_ERR_SHAPE;
     const size_t part_b = (size_t)conv_bwd_bytes(p, K);
     if (!aligned(workspace, 16)) return MB_ERR_ALIGN;
     const Range outs[] = {{dx, (size_t)elems * out_sz}, {dw, w_b}, {dbias, bias ? b_b : 0}, {dstate_in, st_b},
@@ -587,18 +611,10 @@ int mb_conv1d_bwd(const mb_conv_desc *desc, const void *x, const float *w, const
 }
 
 int64_t mb_conv1d_bwd_workspace(const mb_conv_desc *desc) {
-    if (!desc) return MB_ERR_NULL;
-    const int64_t B = desc->batch, D = desc->dim, K = desc->width;
-    int64_t rows, padded;
-    if (B < 0 || D < 0 || desc->seqlen < 0 || !mul_ok(B, D, &rows) || rows >= (int64_t(1) << 31) || D >= (int64_t(1) << 31) ||
-        desc->seqlen >= (int64_t(1) << 31) || !mul_ok(rows, K + 1, &padded))
-        return MB_ERR_SHAPE;
-    if (!valid_dtype(desc->in_dtype) || !valid_dtype(desc->out_dtype)) return MB_ERR_DTYPE;
-    if (K < 1 || K > 4) return MB_ERR_UNSUPPORTED;
     mbs::convbwd::Params p{};
-    p.batch = B; p.dim = D; p.seqlen = desc->seqlen;
-    conv_bwd_segments(p, desc->in_dtype, desc->out_dtype);
-    return conv_bwd_bytes(p, K);
+    int64_t elems;
+    const int bad = conv_bwd_checks(desc, p, &elems);
+    return bad != MB_OK ? bad : conv_bwd_bytes(p, desc->width);
 }
 
 int mb_grad_norm(int64_t count, const void *const *grads, const int64_t *sizes, const int32_t *dtypes, float *norm,
@@ -634,15 +650,11 @@ int mb_verify_sample(int64_t batch, int64_t ndraft, int64_t vocab, int32_t logit
                      const void *logits, const void *draft_logits, const int32_t *draft, const int32_t *lengths,
                      const float *uniform, const float *noise, int32_t *accepted, int32_t *last_pos,
                      int32_t *next_token, float *probs, void *workspace, void *stream) {
-    if (batch < 0 || ndraft < 0 || vocab < 1) return MB_ERR_SHAPE;
     if (!sample_sizes(batch, ndraft, vocab)) return MB_ERR_SHAPE;
     if (!valid_dtype(logit_dtype)) return MB_ERR_DTYPE;
     const float inv_temp = 1.0f / temperature;
     if (!(temperature > 0.0f) || std::isinf(temperature) || std::isinf(inv_temp)) return MB_ERR_UNSUPPORTED;
-    int64_t rows, elems, pairs, noises;
-    if (!mul_ok(batch, ndraft + 1, &rows) || !mul_ok(rows, vocab, &elems) || !mul_ok(batch, ndraft, &pairs) ||
-        !mul_ok(batch, vocab, &noises))
-        return MB_ERR_SHAPE;
+    const int64_t elems = batch * (ndraft + 1) * vocab, pairs = batch * ndraft, noises = batch * vocab;
     if (batch == 0) return MB_OK;
     if (!logits || !noise || !accepted || !next_token || (ndraft > 0 && (!draft || !uniform))) return MB_ERR_NULL;
     const size_t lsz = dtype_size(logit_dtype);
@@ -654,7 +666,6 @@ int mb_verify_sample(int64_t batch, int64_t ndraft, int64_t vocab, int32_t logit
     const Range ins[] = {{logits, (size_t)elems * lsz}, {draft_logits, (size_t)(pairs * vocab) * lsz}, {draft, p_b},
                          {lengths, b_b}, {uniform, p_b}, {noise, (size_t)noises * 4}};
     const SamplePlan f(batch, ndraft, vocab);
-    if (f.blocks >= (int64_t(1) << 23) || batch * f.race_pieces >= (int64_t(1) << 23)) return MB_ERR_SHAPE;
     if (!aligned(workspace, 16)) return MB_ERR_ALIGN;
     const Range outs[] = {{accepted, b_b}, {last_pos, b_b}, {next_token, b_b}, {probs, p_b}, {workspace, f.bytes}};
     if (any_overlap(outs, ins)) return MB_ERR_ALIAS;
@@ -669,11 +680,7 @@ int mb_verify_sample(int64_t batch, int64_t ndraft, int64_t vocab, int32_t logit
 }
 
 int64_t mb_verify_sample_workspace(int64_t batch, int64_t ndraft, int64_t vocab) {
-    int64_t rows, elems;
-    if (batch < 0 || ndraft < 0 || vocab < 1 || !sample_sizes(batch, ndraft, vocab) ||
-        !mul_ok(batch, ndraft + 1, &rows) || !mul_ok(rows, vocab, &elems))
-        return MB_ERR_SHAPE;
-    return (int64_t)SamplePlan(batch, ndraft, vocab).bytes;
+    return sample_sizes(batch, ndraft, vocab) ? (int64_t)SamplePlan(batch, ndraft, vocab).bytes : (int64_t)MB_ERR_SHAPE;
 }
 
 }  // extern "C"
