@@ -103,26 +103,19 @@ template <int S, int K> __device__ __forceinline__ void back_through_taps(float 
 
 // The rows' ends.  Past a row's end the kernels below have g = 0, and take its products with the inputs and taps beside it as
 // they take all others.  That adds nothing, unless such an input or tap is infinite or NaN: then the product is NaN, where by
-// the definition there is no term.  A wave that finds a NaN there, or a tap that is not finite, takes these sums, the last H
-// of dx and dstate_in again from memory, timestep by timestep and only of what exists.  Looking costs 0 to 3% ((64, 3584, 16)
-// bf16 39.2 us and 37.9 without, (4, 3584, 8192) 129.4 and 128.7); selecting the terms as they are taken cost 3 to 10%.
+// the definition there is no term.  With the Swish that changes nothing, since g beside the end, and all that it enters, is
+// NaN then.  Without it, a wave that finds a NaN there, or a tap that is not finite, takes these sums, the last H of dx and
+// dstate_in again from memory, timestep by timestep and only of what exists.  (Selecting the terms as they are taken cost 3 to
+// 10% of the time of every call.)
 template <int IN, int OUT, int K> struct Singly {
     static constexpr int H = K - 1;
     const Params &p;
     int64_t row;
-    const float (&w)[K];
-    float bias;
     __device__ __forceinline__ float ext(int64_t m) const {
         if (m >= H) return Act<IN>::ld(p.x, row * p.seqlen + m - H);
         return p.state_in ? p.state_in[row * H + m] : 0.0f;
     }
-    __device__ __forceinline__ float g(int64_t t) const {
-        const float dy = Act<OUT>::ld(p.dy, row * p.seqlen + t);
-        if (!p.apply_silu) return dy;
-        float pre = bias;
-        for (int j = 0; j < K; ++j) pre = __builtin_fmaf(w[j], ext(t + j), pre);
-        return dy * silu_slope(pre);
-    }
+    __device__ __forceinline__ float g(int64_t t) const { return Act<OUT>::ld(p.dy, row * p.seqlen + t); }
     // over every step-th timestep of [from, to)
     __device__ __forceinline__ void sums(float (&acc)[K + 1], int64_t from, int64_t to, int step) const {
 #pragma unroll
@@ -138,13 +131,14 @@ template <int IN, int OUT, int K> struct Singly {
         float v = p.dstate_out && m >= p.seqlen ? p.dstate_out[row * H + m - p.seqlen] : 0.0f;
 #pragma unroll
         for (int j = 0; j < K; ++j)
-            if (m >= j && m - j < p.seqlen) v = __builtin_fmaf(w[j], g(m - j), v);
+            if (m >= j && m - j < p.seqlen) v = __builtin_fmaf(p.w[row % p.dim * K + j], g(m - j), v);
         return v;
     }
-    // of the last H timesteps, those in [from, to); i < H
-    __device__ __forceinline__ void last_dx(int64_t from, int64_t to, int i) const {
+    // the first values were stored by other lanes, and are there before these follow; i < H
+    __device__ __forceinline__ void ends(int64_t from, int64_t to, int i) const {
         const int64_t t = p.seqlen - H + i;
         if (t >= from && t < to) st_out<OUT>(p.dx, row * p.seqlen + t, dext(t + H));
+        if (from == 0 && p.dstate_in) p.dstate_in[row * H + i] = dext(i);
     }
 };
 
@@ -263,7 +257,7 @@ __global__ __launch_bounds__(kThreads) void conv1d_bwd(Params p) {
             for (int m = j; m < H; ++m) v = lane == m ? __builtin_fmaf(w[j], carry[m - j], v) : v;
         p.dstate_in[row * H + lane] = v;
     }
-    if (H > 0 && (int64_t)(end + 1) * T > L - H) {
+    if (H > 0 && !p.apply_silu && (int64_t)(end + 1) * T > L - H) {
         float odd = 0.0f, taps = 0.0f;                  // NaN where there is something
 #pragma unroll
         for (int j = 0; j < K; ++j) {
@@ -271,18 +265,12 @@ __global__ __launch_bounds__(kThreads) void conv1d_bwd(Params p) {
             taps = __builtin_fmaf(w[j], 0.0f, taps);
         }
         const bool beside = (int64_t)end * T + lane * S + S > L && odd != odd;
-        if (__builtin_expect(__ballot(beside || taps != taps) != 0, 0)) {
-            float taps_at[K];
-#pragma unroll
-            for (int j = 0; j < K; ++j) taps_at[j] = p.w[row_at % p.dim * K + j];
-            const Singly<IN, OUT, K> singly{p, row_at, taps_at, p.bias ? p.bias[row_at % p.dim] : 0.0f};
+        if (__ballot(beside || taps != taps) != 0) {
+            const Singly<IN, OUT, K> singly{p, row_at};
             const int64_t from = (int64_t)begin * T, to = min((int64_t)(end + 1) * T, L);
+            wait_for_memory();
             singly.sums(acc, from + lane, to, 64);
-            wait_for_memory();                          // the first values are there before the others follow
-            if (lane < H) {
-                singly.last_dx(from, to, lane);
-                if (begin == 0 && p.dstate_in) p.dstate_in[row_at * H + lane] = singly.dext(lane);
-            }
+            if (lane < H) singly.ends(from, to, lane);
         }
     }
 #pragma unroll
@@ -366,20 +354,17 @@ __global__ __launch_bounds__(kThreads) void conv1d_bwd_short(Params p) {
         }
         if (active && l < H) p.dstate_in[row * H + l] = v;
     }
-    if (H > 0) {
+    if (H > 0 && !p.apply_silu) {
         float odd = 0.0f;                               // NaN where there is something, or an infinite sum
 #pragma unroll
         for (int j = 0; j < K; ++j) odd = __builtin_fmaf(acc[j], 0.0f, __builtin_fmaf(w[j], 0.0f, odd));
         const uint64_t where = __ballot(odd != odd);
-        if (__builtin_expect(where != 0, 0)) {
-            wait_for_memory();                          // the first values are there before the others follow
+        if (where != 0) {
+            wait_for_memory();
             if (where >> (lane & ~(G - 1)) & (~0ull >> (64 - G))) {     // in this row
-                const Singly<IN, OUT, K> singly{p, row, w, bias};
+                const Singly<IN, OUT, K> singly{p, row};
                 singly.sums(acc, l, L, G);
-                if (active && l < H) {
-                    singly.last_dx(0, L, l);
-                    if (p.dstate_in) p.dstate_in[row * H + l] = singly.dext(l);
-                }
+                if (active && l < H) singly.ends(0, L, l);
             }
         }
     }

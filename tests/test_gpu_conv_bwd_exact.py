@@ -3,11 +3,13 @@ partial sum of any order is exact in fp32 (9 batch L below 2^24) and the results
 
 The definition has a term per existing pair of a timestep and an input: an infinity or a NaN spoils the terms that it is
 in, and no others."""
+import numpy as np
 import pytest
 import torch
 
 from gpu_util import announce, has_gpu
-from test_gpu_embedding import DT
+from oracle import model_ops as M
+from test_gpu_embedding import DT, np64
 
 pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not has_gpu(), reason="needs a GPU")]
 INF, NAN = float("inf"), float("nan")
@@ -80,6 +82,24 @@ def test_what_stands_at_a_rows_end(dtype, out, K, bad):
             a["dy"][0, 4, L - back] = bad
             a["w"][6, back - 1] = bad
             check(a)
+
+
+@pytest.mark.parametrize("dtype,out", [("f32", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("bad", [INF, -INF, NAN])
+def test_what_stands_at_a_rows_end_with_the_swish(dtype, out, bad):
+    """There the slope at such an input is NaN, and what it enters."""
+    import paper_2401_13660_amd as mb
+    announce(f"conv1d_bwd with the Swish: {bad} at the rows' ends, {dtype} {out}")
+    for L in LENGTHS:
+        a = inputs(2, 7, L, 4, dtype, out, L)
+        a["x"][1, 2, L - 1 - L % 2] = bad
+        a["w"][6, 1] = bad
+        g = mb.conv1d_bwd(a["x"], a["w"], a["dy"], a["bias"], a["state"], a["dstate_out"])
+        n = {k: np64(v) for k, v in a.items()}
+        with np.errstate(all="ignore"):
+            ref = M.conv_grad(n["x"], n["w"], n["dy"], n["bias"], n["state"], n["dstate_out"])
+        for k in ref:
+            assert np.array_equal(np.isfinite(np64(g[k])), np.isfinite(ref[k])), (k, L)
 
 
 @pytest.mark.parametrize("L", [16, 40, 130, 260, 512, 1100])
