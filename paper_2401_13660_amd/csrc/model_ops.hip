@@ -129,12 +129,12 @@ struct EmbedPlan {
 template <int TOK, int OUT> hipError_t embed_sort(mbs::embed::BwdParams &p, const EmbedPlan &f, char *ws, hipStream_t st) {
     namespace E = mbs::embed;
     E::Pair *const ab[2] = {reinterpret_cast<E::Pair *>(ws + f.a), reinterpret_cast<E::Pair *>(ws + f.b)};
-    // the table is set to zero in shares beside the launches of the sort.  A scatter takes twice a count's time, and hides more:
-    // 98 MB in shares of 1, 3 and 3 41 to 45 us in all, in equal ones 42 to 47; larger tables keep every launch busy, 268 MB
-    // in equal shares 64 to 70, else 66 to 71
+    // the table is set to zero in shares beside the launches of the sort.  A scatter takes twice a count's time and hides more: its
+    // share is three times as large.  Equal ones took 44.4 us in all instead of 42.7 (16,384 tokens, 98 MB), 49.7 and 49.2
+    // (135 MB), 75.9 and 77.4 (268 MB), 177 and 170 (604 MB); 65,536 tokens 84.2 and 84.7, 91.2 and 89.1, 129 and 130
+    constexpr int kBeside = 3;
     const int64_t elems = p.vocab * p.dim;
-    const int beside = elems * (OUT == 1 ? 2 : 4) <= int64_t(128) << 20 ? 3 : 1;
-    const int64_t parts = f.tiles <= 1 ? beside : f.passes * beside + (f.merged ? 1 : f.passes);
+    const int64_t parts = f.tiles <= 1 ? kBeside : f.passes * kBeside + (f.merged ? 1 : f.passes);
     const dim3 block(E::kThreads);
     int64_t part = 0, zeroing = 0;                      // workgroups of at least 4,096 elements
     dim3 grid;
@@ -148,7 +148,7 @@ template <int TOK, int OUT> hipError_t embed_sort(mbs::embed::BwdParams &p, cons
     };
     void *args[] = {&p};
     if (f.tiles <= 1) {
-        next_share(beside);
+        next_share(kBeside);
         p.to = ab[0];
         p.tiles = 1;
         // 256 threads where they do: fewer waves' counts to add up.  The larger workgroups zero four times as much each
@@ -177,7 +177,7 @@ template <int TOK, int OUT> hipError_t embed_sort(mbs::embed::BwdParams &p, cons
                                 grid, block, args, 0, st);
             if (e != hipSuccess) return e;
         }
-        next_share(beside);
+        next_share(kBeside);
         const void *fn = f.wide  ? reinterpret_cast<const void *>(&E::scatter<TOK, OUT, true, false, E::kWideBits>)
                          : first ? next ? reinterpret_cast<const void *>(&E::scatter<TOK, OUT, true, true, 8>)
                                         : reinterpret_cast<const void *>(&E::scatter<TOK, OUT, true, false, 8>)
