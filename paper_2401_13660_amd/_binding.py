@@ -664,8 +664,8 @@ def grad_norm(grads):
 
 def clip_grad_norm(grads, max_norm, *, eps=1e-6, out=None):
     """Scales a list of fp32 and bf16 tensors (the gradients, not the parameters) by max_norm / (norm + eps)
-    where that is below 1, in place or into ``out`` (tensors of the same shapes and types).  Returns the norm before clipping, a 0-dimensional
-    fp32 tensor on the GPU."""
+    where that is below 1, in place or into ``out`` (tensors of the same shapes and types).  Returns the norm before
+    clipping, a 0-dimensional fp32 tensor on the GPU.  The written tensors count as changed for autograd."""
     lib = load_library()
     if _fast is not None:
         res = _fast.clip_grad_norm(grads, max_norm, eps, out)

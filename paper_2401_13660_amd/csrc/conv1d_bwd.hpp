@@ -16,7 +16,9 @@
 // stretch's end, computed there again), so x and dy are read once and dx is written once.  The next
 // tile's loads are on their way while a tile is computed.
 //
-// Bound by HBM: 6 bytes and 32 VALU instructions (two of them transcendental) per bf16 element.
+// A lane sums a tile's products, then the tiles', and so on: dw's rounding grows with the tiles of a row, not its timesteps.
+//
+// Bound by HBM: 6 bytes and 33 VALU instructions (two of them transcendental) per bf16 element.
 // (4, 3584, 8192) bf16 takes 132 us, 5.3 TB/s, a little over the rate of a device copy (5.17); with
 // ordinary instead of streaming loads and stores 147, with streaming stores alone 142, streaming loads
 // alone 149.  One stretch per row there: with 2 (4) per row it took 150 (158), the waves' ends and the

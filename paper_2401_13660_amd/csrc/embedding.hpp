@@ -13,12 +13,13 @@
 // goes on into other chunks are joined afterwards in the order of the chunks.  No atomic adds floats: a
 // result depends on the tokens and dy alone.
 //
-// 32,768 bytes of a text, width 1792 in bf16: 34 us, of which the sums take 22.2 (5.2 TB/s, the rate of
-// a device copy), the sort's two launches 9 and the joining 4.4, a chain of loads each.  16,384 tokens
-// of a table of 32,000 rows of 768 fp32: 41 us, three launches of the sort at 5 to 10 (a share of the
-// table's 98 MB zeroed beside each), the sums 14.4 and the joining 4.  With a launch of its own for each
-// pass's counts the sort took four, 45 us in all; with the next pass's counts added in memory token by
-// token instead of in LDS 49: equal tokens meet in one counter.
+// 32,768 bytes of a text, width 1792 in bf16: 34 us a call.  Kernel by kernel (a trace, where launches do not
+// overlap, so that the parts come to 1.5 to 3 us more than a call): sums 22.9 (5.1 TB/s, the rate of a device
+// copy), the sort 3.5 and 5.6, the joining 4.2, a chain of loads each.  16,384 tokens of a table of 32,000
+// rows of 768 fp32: 41 us a call; in the trace the sort 5.6, 9.9 and 10.2 (a share of the table's 98 MB zeroed
+// beside each), sums 13.8, joining 4.6.  With a launch of its own for each pass's counts the sort took four,
+// 45 us a call; with the next pass's counts added in memory token by token instead of in LDS 49: equal
+// tokens meet in one counter.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -292,9 +293,11 @@ __global__ __launch_bounds__(kThreads) void scatter(BwdParams p) {
 }
 
 // The whole sort by one workgroup, for up to kSmallTokens: places in registers, moved through LDS between the passes.
-// The other workgroups set the table to zero meanwhile.  4,096 tokens take 7 us of bytes and 10.7 of 30,000 values, 1,000
-// bytes 3.6 with 256 threads (5 with 1,024); the launches above take about 9 and 21, and two or four times the host's
-// time.  16 places per thread took 21.5 us for 16,384 bytes: one CU's issue rate, where the launches above spread over many.
+// The other workgroups set the table to zero meanwhile.  In a kernel trace 4,096 bytes take 6.4 us, and as many tokens of
+// 30,000 values 14.3 with the 92 MB of such a table of 768 columns zeroed beside them (10.4 with 24 columns); the launches
+// above take about 9 and 21, and two or four times the host's time.  Up to 1,024 tokens, where sum_direct does not take them:
+// 1,000 bytes of 4,352 columns 13.8 us a call with 256 threads and 15.0 with 1,024, 1,000 tokens of 200,000 rows of 64 19.2
+// and 22.4.  16 places per thread took 21.5 us for 16,384 bytes: one CU's issue rate, where the launches above spread over many.
 constexpr int kSmallThreads = 1024;
 constexpr int kSmallPlaces = 4;
 constexpr int kSmallTokens = kSmallThreads * kSmallPlaces;

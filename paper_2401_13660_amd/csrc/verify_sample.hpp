@@ -24,10 +24,11 @@
 // joins them, decides, and races within each piece of the row that stops the sequence; a third one
 // joins the pieces' winners.
 //
-// Bound by latency: 16 drafts of 32 prompts over 256 bytes take 6.1 us for 1.1 MB (58 with one wave per
-// sequence), one byte of one prompt 2.7; 4 drafts of 16 prompts over 32,000 tokens in bf16 14.4 us a call
-// for 11 MB, three launches of 6, 7.9 and 2.8: with races of 8,192 tokens per workgroup instead of 2,048
-// the second launch took 16, and maxima and sums by 8,192 instead of 4,096 took 0.6 us longer.
+// Bound by latency: in a kernel trace 16 drafts of 32 prompts over 256 bytes take 6.0 us for 1.1 MB (58 with
+// one wave per sequence), one byte of one prompt 2.4; 4 drafts of 16 prompts over 32,000 tokens in bf16, 11 MB,
+// 14.9 us a call and 5.7, 8.0 and 2.5 in the trace, where launches do not overlap.  With races of 8,192 tokens
+// per workgroup instead of 2,048 the second launch took 16, and maxima and sums by 8,192 instead of 4,096
+// took 0.6 us longer.
 #pragma once
 
 #include <hip/hip_runtime.h>
