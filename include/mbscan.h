@@ -55,7 +55,8 @@ extern "C" {
 
 typedef enum {
     MB_F32 = 0,
-    MB_BF16 = 1
+    MB_BF16 = 1,
+    MB_FP8 = 2               /* e4m3 (largest 448, no infinities), where an entry point names it */
 } mb_dtype;
 
 typedef enum {
@@ -482,6 +483,114 @@ int mb_verify_sample(int64_t batch, int64_t ndraft, int64_t vocab, int32_t logit
                      const float *uniform, const float *noise, int32_t *accepted, int32_t *last_pos,
                      int32_t *next_token, float *probs, void *workspace, void *stream);
 int64_t mb_verify_sample_workspace(int64_t batch, int64_t ndraft, int64_t vocab);
+
+/*
+ * The residual's addition and the root-mean-square norm in front of a block:
+ *
+ *   h = x + residual, rounded to the residual's type (x itself without one)
+ *   y = h * rstd * weight,   rstd = 1 / sqrt(mean over the row of h^2 + eps)
+ *
+ *   x            act (rows, dim)             x_dtype
+ *   weight       float (dim)                 NULL means ones
+ *   residual     (rows, dim)                 residual_dtype (fp32 or bf16, whatever x is); NULL: nothing is added,
+ *                                            and residual_out is NULL too
+ *   y            out_dtype (rows, dim)       fp32, bf16 or MB_FP8
+ *   scales       float (rows, ceil(dim/128)) with MB_FP8 (required): those of y's blocks, as mb_quantize_fp8's
+ *   residual_out (rows, dim)                 h, in residual's type; may be residual
+ *   rstd         float (rows)                for the gradient; NULL means not written
+ * Outputs overlap nothing else.  eps finite, >= 0 (MB_ERR_UNSUPPORTED otherwise); dim below 2^25.  Arithmetic is fp32,
+ * squares included: a row of elements above 1e19 has rstd 0.
+ */
+int mb_rms_norm_fwd(int64_t rows, int64_t dim, int32_t x_dtype, int32_t residual_dtype, int32_t out_dtype, float eps,
+                    const void *x, const float *weight, const void *residual, void *y, float *scales, void *residual_out,
+                    float *rstd, void *stream);
+
+/*
+ * The gradients of sum(dy * y) + sum(dh * h):
+ *
+ *   g = dy * weight,  d = rstd * (g - h rstd mean(g h rstd)) + dh
+ *   dx = d,  dresidual = d,  dweight = sum over the rows of dy h rstd
+ *
+ *   dy         dy_dtype (rows, dim)
+ *   h, dh      h_dtype (rows, dim)      h as the forward kept it (x without a residual); dh NULL means 0
+ *   rstd       float (rows)             the forward's
+ *   weight     float (dim)              NULL means ones
+ *   dx         dx_dtype (rows, dim)
+ *   dresidual  h_dtype (rows, dim)      NULL means not written
+ *   dweight    float (dim)              summed over the rows; NULL means not written; zeros without rows
+ *   workspace  as for mb_embedding_bwd, of mb_rms_norm_bwd_workspace(rows, dim) bytes; not used without dweight
+ * Outputs are overwritten and overlap nothing else.  The same bits on every call.
+ */
+int mb_rms_norm_bwd(int64_t rows, int64_t dim, int32_t dy_dtype, int32_t h_dtype, int32_t dx_dtype, const void *dy,
+                    const void *h, const float *rstd, const float *weight, const void *dh, void *dx, void *dresidual,
+                    float *dweight, void *workspace, void *stream);
+int64_t mb_rms_norm_bwd_workspace(int64_t rows, int64_t dim);
+
+/*
+ * Matrices in 8 bits (e4m3) with a scale for each 128 columns of a row, or each tile of 128 x 128:
+ *
+ *   scale = max(largest magnitude of the block / 448, 2^-126),   q = x * (1 / scale), rounded to nearest even
+ *
+ * so that q * scale stands for x.  A NaN stays one, and its block's scale is that of the others; an infinity makes its
+ * block's scale infinite.
+ *
+ *   x       x_dtype (batch, rows, cols)
+ *   q       e4m3 (batch, rows, cols), or with transpose (batch, cols, rows): blocks, rows and columns are then q's
+ *   scales  float (batch, R, ceil(C/128)) for q of R rows and C columns; with tile (batch, ceil(R/128), ceil(C/128))
+ * Outputs overlap nothing else.  batch * ceil(rows/128) * ceil(cols/128) below 2^23.
+ */
+int mb_quantize_fp8(int64_t batch, int64_t rows, int64_t cols, int32_t x_dtype, int32_t tile, int32_t transpose,
+                    const void *x, void *q, float *scales, void *stream);
+
+typedef struct {
+    int64_t batch, m, n, k;
+    int32_t a_batched, b_batched;   /* a (batch, m, k) or (m, k) for every product; b likewise */
+    int32_t a_tile, b_tile;         /* scales per 128 x 128 tile instead of per row */
+    int32_t out_dtype;              /* fp32 or bf16 */
+    int32_t reserved;               /* 0 */
+} mb_matmul_desc;
+
+/*
+ * Products of matrices in 8 bits with scales, as mb_quantize_fp8 and mb_rms_norm_fwd write them:
+ *
+ *   c[m][n] = sum over k of (a[m][k] * its scale) * (b[n][k] * its scale)
+ *
+ *   a         e4m3 (m, k) or (batch, m, k)     a_scales  float ([batch,] m or ceil(m/128), ceil(k/128))
+ *   b         e4m3 (n, k) or (batch, n, k)     b_scales  likewise
+ *   c         out_dtype (batch, m, n), overlaps nothing else
+ * Sums are fp32, rounded once to out_dtype; the same bits on every call.  k = 0 gives zeros.  m, n and k below 2^30,
+ * batch * ceil(m/128) * ceil(n/128) below 2^23.
+ */
+int mb_matmul_fp8(const mb_matmul_desc *desc, const void *a, const float *a_scales, const void *b, const float *b_scales,
+                  void *c, void *stream);
+
+/*
+ * The next token of each sequence, from given random numbers.  In the order of falling logits, the lowest index first
+ * among equals, with e = exp((logit - largest) / temperature):
+ *
+ *   top-k keeps the first top_k tokens (all for top_k <= 0); S = what their e sum to
+ *   top-p keeps those before which less than top_p * S lies (all for top_p >= 1), and always the first
+ *   min-p keeps those with e >= min_p (all for min_p <= 0)
+ *   token = the y with the largest e(y) / noise(y) of the kept, the lowest such y
+ *   prob  = e(token) / the kept tokens' sum: the probability that it was drawn with
+ *
+ * With exponential noise of mean 1 tokens are distributed as the filtered probabilities.  Temperature 0 takes the
+ * largest logit, whatever the noise.  A row of logits that is no distribution (as for mb_verify_sample) gives token -1 and
+ * prob 0; so does a row whose noise lets no token win.  -infinity masks a token.
+ *
+ *   temperature, top_k, top_p, min_p   for every sequence: temperature 0, or > 0 with it and its inverse finite; top_p
+ *                  not NaN; min_p <= 1 (MB_ERR_UNSUPPORTED otherwise)
+ *   temperatures, top_ks, top_ps, min_ps   float (top_ks: int32) (batch) DEVICE memory: one for each sequence instead;
+ *                  a sequence for which they are out of those ranges gives token -1 and prob 0.  NULL: the ones above
+ *   logits         act (batch, vocab)
+ *   noise          float (batch, vocab)
+ *   token          int32 (batch)
+ *   prob           float (batch)      NULL means not written
+ * Outputs overlap nothing else.  vocab >= 1, below 2^30; batch below 2^22.
+ */
+int mb_sample(int64_t batch, int64_t vocab, int32_t logit_dtype, float temperature, int32_t top_k, float top_p, float min_p,
+              const float *temperatures, const int32_t *top_ks, const float *top_ps, const float *min_ps, const void *logits,
+              const float *noise, int32_t *token, float *prob, void *stream);
 
 /* Static, NUL-terminated description of a status code (never NULL). */
 const char *mb_status_string(int status);

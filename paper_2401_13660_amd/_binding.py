@@ -18,7 +18,7 @@ import torch
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libmbscan.so")
 
-MB_F32, MB_BF16 = 0, 1
+MB_F32, MB_BF16, MB_FP8 = 0, 1, 2
 _STATUS_OK = 0
 
 
@@ -36,6 +36,12 @@ class ConvDesc(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int64), ("dim", ctypes.c_int64), ("seqlen", ctypes.c_int64),
                 ("width", ctypes.c_int32), ("in_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
                 ("apply_silu", ctypes.c_int32), ("reserved", ctypes.c_int32), ("reserved2", ctypes.c_int32)]
+
+
+class MatmulDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("m", ctypes.c_int64), ("n", ctypes.c_int64), ("k", ctypes.c_int64),
+                ("a_batched", ctypes.c_int32), ("b_batched", ctypes.c_int32), ("a_tile", ctypes.c_int32),
+                ("b_tile", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 _lib = None
@@ -86,6 +92,18 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         size.restype, size.argtypes = i64, args
     lib.mb_verify_sample.restype = ctypes.c_int
     lib.mb_verify_sample.argtypes = [i64] * 3 + [i32, f32] + [_VP] * 12
+    lib.mb_rms_norm_fwd.restype = ctypes.c_int
+    lib.mb_rms_norm_fwd.argtypes = [i64] * 2 + [i32] * 3 + [f32] + [_VP] * 8
+    lib.mb_rms_norm_bwd.restype = ctypes.c_int
+    lib.mb_rms_norm_bwd.argtypes = [i64] * 2 + [i32] * 3 + [_VP] * 10
+    lib.mb_rms_norm_bwd_workspace.restype = i64
+    lib.mb_rms_norm_bwd_workspace.argtypes = [i64] * 2
+    lib.mb_quantize_fp8.restype = ctypes.c_int
+    lib.mb_quantize_fp8.argtypes = [i64] * 3 + [i32] * 3 + [_VP] * 4
+    lib.mb_matmul_fp8.restype = ctypes.c_int
+    lib.mb_matmul_fp8.argtypes = [ctypes.POINTER(MatmulDesc)] + [_VP] * 6
+    lib.mb_sample.restype = ctypes.c_int
+    lib.mb_sample.argtypes = [i64] * 2 + [i32, f32, i32, f32, f32] + [_VP] * 9
     lib.mb_status_string.restype = ctypes.c_char_p
     lib.mb_status_string.argtypes = [ctypes.c_int]
     lib.mb_abi_version.restype = ctypes.c_int
@@ -729,3 +747,215 @@ def verify_sample(logits, draft, uniform, noise, draft_logits=None, *, lengths=N
                                   _ptr(last_pos), _ptr(next_token), _ptr(probs), _ptr(ws), _stream(dev))
     _check(st, "mb_verify_sample")
     return (accepted, last_pos, next_token, probs) if return_probs else (accepted, last_pos, next_token)
+
+
+FP8 = torch.float8_e4m3fn
+_BLOCK = 128                # values that share a scale
+
+
+def _blocks(n):
+    return -(-n // _BLOCK)
+
+
+def _norm_inputs(x, weight, residual):
+    """The checks that both forms of the norm share: rows and columns."""
+    if not isinstance(x, torch.Tensor) or x.dim() < 1:
+        raise MBScanError("x must be a (..., dim) tensor")
+    dev, d = x.device, x.shape[-1]
+    _need(x, "x", x.shape)
+    if weight is not None:
+        _need(weight, "weight", (d,), torch.float32, dev)
+    if residual is not None:
+        _need(residual, "residual", x.shape, None, dev)
+    return x.numel() // d if d else 0, d, dev
+
+
+def _norm(x, weight, residual, eps, code, y, scales, residual_out, rstd, rows, d, dev):
+    lib = load_library()
+    with _on_device(dev):
+        st = lib.mb_rms_norm_fwd(rows, d, _dt(x.dtype), 0 if residual is None else _dt(residual.dtype), code, float(eps),
+                                 _ptr(x), _ptr(weight), _ptr(residual), _ptr(y), _ptr(scales), _ptr(residual_out), _ptr(rstd),
+                                 _stream(dev))
+    _check(st, "mb_rms_norm_fwd")
+
+
+def _residual_out(residual, given, dev):
+    """The tensor for h, and whether it is the caller's."""
+    if residual is None:
+        if given is not None:
+            raise MBScanError("residual_out given without a residual")
+        return None
+    if given is None:
+        return torch.empty_like(residual)
+    _need(given, "residual_out", residual.shape, residual.dtype, dev)
+    return given
+
+
+def rms_norm_fwd(x, weight=None, residual=None, *, eps=1e-5, out_dtype=None, return_rstd=False, out=None, residual_out=None):
+    """h = x + residual (in residual's type) and y = h / sqrt(mean(h^2) + eps) * weight over the last dimension.
+
+    x: (..., dim) fp32 or bf16; weight: (dim,) fp32 or None; residual: x's shape, fp32 or bf16, or None.
+    ``residual_out`` may be ``residual``: h takes its place.  Returns y in ``out_dtype`` (x's by default), or (y, h)
+    with a residual; ``return_rstd`` appends 1 / sqrt(mean(h^2) + eps), fp32 of x's leading shape, for ``rms_norm_bwd``."""
+    load_library()
+    rows, d, dev = _norm_inputs(x, weight, residual)
+    given = [t for t in (out, residual_out) if t is not None]
+    if out is None:
+        out = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=dev)
+    else:
+        _need(out, "out", x.shape, None, dev)
+    h = _residual_out(residual, residual_out, dev)
+    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=dev) if return_rstd else None
+    _norm(x, weight, residual, eps, _dt(out.dtype), out, None, h, rstd, rows, d, dev)
+    if given:
+        _was_written(given)
+    res = (out,) + ((h,) if residual is not None else ()) + ((rstd,) if return_rstd else ())
+    return res[0] if len(res) == 1 else res
+
+
+def rms_norm_fp8(x, weight=None, residual=None, *, eps=1e-5, residual_out=None):
+    """rms_norm_fwd with y in 8 bits, as ``matmul_fp8`` takes it.  Returns (q, scale) or, with a residual, (q, scale, h):
+    q (..., dim) float8_e4m3fn, scale (..., ceil(dim / 128)) fp32, y being q times its block's scale."""
+    load_library()
+    rows, d, dev = _norm_inputs(x, weight, residual)
+    q = torch.empty(x.shape, dtype=FP8, device=dev)
+    scale = torch.empty(x.shape[:-1] + (_blocks(d),), dtype=torch.float32, device=dev)
+    h = _residual_out(residual, residual_out, dev)
+    _norm(x, weight, residual, eps, MB_FP8, q, scale, h, None, rows, d, dev)
+    if residual_out is not None:
+        _was_written([residual_out])
+    return (q, scale) if residual is None else (q, scale, h)
+
+
+def rms_norm_bwd(dy, h, rstd, weight=None, dh=None, *, dx_dtype=None):
+    """Gradients of sum(dy * y) + sum(dh * h) for rms_norm_fwd.
+
+    dy: (..., dim) in y's type; h: the forward's h (x without a residual); rstd: the forward's; dh: h's shape and
+    type, the gradient that reaches h from behind, or None.  Returns a dict: dx in ``dx_dtype`` (dy's by default),
+    dweight (dim,) fp32 (None without a weight) and, with dh, dresidual in h's type (the tensor dx itself where that is
+    dx's type)."""
+    lib = load_library()
+    if not isinstance(h, torch.Tensor) or h.dim() < 1:
+        raise MBScanError("h must be a (..., dim) tensor")
+    dev, d = h.device, h.shape[-1]
+    _need(h, "h", h.shape)
+    _need(dy, "dy", h.shape, None, dev)
+    _need(rstd, "rstd", h.shape[:-1], torch.float32, dev)
+    if weight is not None:
+        _need(weight, "weight", (d,), torch.float32, dev)
+    if dh is not None:
+        _need(dh, "dh", h.shape, h.dtype, dev)
+    rows = rstd.numel()
+    dx = torch.empty(h.shape, dtype=dx_dtype or dy.dtype, device=dev)
+    g = {"dx": dx, "dweight": None if weight is None else torch.empty(d, dtype=torch.float32, device=dev)}
+    apart = dh is not None and h.dtype != dx.dtype
+    if dh is not None:
+        g["dresidual"] = torch.empty_like(h) if apart else dx
+    ws = _workspace(lib.mb_rms_norm_bwd_workspace(rows, d), "mb_rms_norm_bwd", dev) if weight is not None else None
+    with _on_device(dev):
+        st = lib.mb_rms_norm_bwd(rows, d, _dt(dy.dtype), _dt(h.dtype), _dt(dx.dtype), _ptr(dy), _ptr(h), _ptr(rstd), _ptr(weight),
+                                 _ptr(dh), _ptr(dx), _ptr(g["dresidual"]) if apart else None, _ptr(g["dweight"]), _ptr(ws),
+                                 _stream(dev))
+    _check(st, "mb_rms_norm_bwd")
+    return g
+
+
+def quantize_fp8(x, *, tile=False, transpose=False):
+    """Matrices (..., rows, cols), fp32 or bf16, in 8 bits: (q, scale), q float8_e4m3fn of x's shape and scale fp32
+    (..., rows, ceil(cols / 128)), or with ``tile`` (..., ceil(rows / 128), ceil(cols / 128)).  ``transpose``: the same of
+    x's transposed matrices, q (..., cols, rows)."""
+    lib = load_library()
+    if not isinstance(x, torch.Tensor) or x.dim() < 2:
+        raise MBScanError("x must be a (..., rows, cols) tensor")
+    _need(x, "x", x.shape)
+    dev, lead = x.device, tuple(x.shape[:-2])
+    rows, cols = x.shape[-2:]
+    R, C = (cols, rows) if transpose else (rows, cols)
+    q = torch.empty(lead + (R, C), dtype=FP8, device=dev)
+    scale = torch.empty(lead + (_blocks(R) if tile else R, _blocks(C)), dtype=torch.float32, device=dev)
+    batch = 1
+    for n in lead:
+        batch *= n
+    with _on_device(dev):
+        st = lib.mb_quantize_fp8(batch, rows, cols, _dt(x.dtype), 1 if tile else 0, 1 if transpose else 0, _ptr(x), _ptr(q),
+                                 _ptr(scale), _stream(dev))
+    _check(st, "mb_quantize_fp8")
+    return q, scale
+
+
+def _matrix(t, s, name, dev):
+    """An 8-bit matrix or a batch of them with its scales: batch (None without), rows, and whether scales are of tiles."""
+    if not isinstance(t, torch.Tensor) or t.dim() not in (2, 3):
+        raise MBScanError(f"{name} must be a (rows, k) or (batch, rows, k) tensor")
+    _need(t, name, t.shape, FP8, dev)
+    lead, (rows, k) = tuple(t.shape[:-2]), t.shape[-2:]
+    by_row, by_tile = lead + (rows, _blocks(k)), lead + (_blocks(rows), _blocks(k))
+    tile = isinstance(s, torch.Tensor) and tuple(s.shape) == by_tile and by_tile != by_row
+    _need(s, f"{name}_scale", by_tile if tile else by_row, torch.float32, dev)
+    return (lead[0] if lead else None), rows, tile
+
+
+def matmul_fp8(a, a_scale, b, b_scale, *, out_dtype=torch.bfloat16, out=None):
+    """c[m][n] = sum over k of a[m][k] b[n][k], values being 8 bits times their scales.
+
+    a: (m, k) or (batch, m, k), b: (n, k) or (batch, n, k), float8_e4m3fn, with the scales of ``quantize_fp8`` (per row
+    or per tile, told by their shape) or ``rms_norm_fp8``.  Returns (m, n), or (batch, m, n) if either has a batch, in
+    ``out_dtype``: fp32 or bf16."""
+    lib = load_library()
+    dev = a.device if isinstance(a, torch.Tensor) else None
+    a_batch, m, a_tile = _matrix(a, a_scale, "a", dev)
+    b_batch, n, b_tile = _matrix(b, b_scale, "b", dev)
+    k = a.shape[-1]
+    if b.shape[-1] != k:
+        raise MBScanError(f"b has {b.shape[-1]} columns, expected {k}")
+    if a_batch is not None and b_batch is not None and a_batch != b_batch:
+        raise MBScanError(f"b is a batch of {b_batch}, expected {a_batch}")
+    batch = a_batch if a_batch is not None else b_batch
+    shape = ((batch,) if batch is not None else ()) + (m, n)
+    given = out is not None
+    if out is None:
+        out = torch.empty(shape, dtype=out_dtype, device=dev)
+    else:
+        _need(out, "out", shape, None, dev)
+    desc = MatmulDesc(1 if batch is None else batch, m, n, k, a_batch is not None, b_batch is not None, a_tile, b_tile,
+                      _dt(out.dtype), 0)
+    with _on_device(dev):
+        st = lib.mb_matmul_fp8(ctypes.byref(desc), _ptr(a), _ptr(a_scale), _ptr(b), _ptr(b_scale), _ptr(out), _stream(dev))
+    _check(st, "mb_matmul_fp8")
+    if given:
+        _was_written([out])
+    return out
+
+
+def sample(logits, noise, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, return_prob=False):
+    """The next token of each sequence from its filtered probabilities and given random numbers.
+
+    logits: (batch, vocab) fp32 or bf16; noise: fp32 (batch, vocab), exponential of mean 1.  ``temperature`` (0: the
+    largest logit), ``top_k`` (<= 0: all), ``top_p`` (>= 1: all) and ``min_p`` (<= 0: all) are numbers, or tensors (batch,)
+    on the GPU, fp32 (top_k: int32), of one for each sequence.  Filters apply in this order; equal logits rank by
+    their index.  Returns the tokens, int32 (batch,), -1 for a row that is no distribution; ``return_prob`` adds the
+    probabilities that they were drawn with, fp32 (batch,)."""
+    lib = load_library()
+    if not isinstance(logits, torch.Tensor) or logits.dim() != 2:
+        raise MBScanError("logits must be a (batch, vocab) tensor")
+    nb, V = logits.shape
+    dev = logits.device
+    _need(logits, "logits", (nb, V))
+    _need(noise, "noise", (nb, V), torch.float32, dev)
+    each = {}
+    for name, v, dt in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                        ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+        if isinstance(v, torch.Tensor):
+            _need(v, name, (nb,), dt, dev)
+            each[name] = v
+    one = {n: d if n in each else v for n, v, d in (("temperature", temperature, 1.0), ("top_k", top_k, 0),
+                                                    ("top_p", top_p, 1.0), ("min_p", min_p, 0.0))}
+    token = torch.empty(nb, dtype=torch.int32, device=dev)
+    prob = torch.empty(nb, dtype=torch.float32, device=dev) if return_prob else None
+    with _on_device(dev):
+        st = lib.mb_sample(nb, V, _dt(logits.dtype), float(one["temperature"]), min(max(int(one["top_k"]), 0), 2 ** 31 - 1),
+                           float(one["top_p"]), float(one["min_p"]), *(_ptr(each.get(n)) for n in
+                                                                       ("temperature", "top_k", "top_p", "min_p")),
+                           _ptr(logits), _ptr(noise), _ptr(token), _ptr(prob), _stream(dev))
+    _check(st, "mb_sample")
+    return (token, prob) if return_prob else token

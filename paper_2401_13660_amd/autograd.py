@@ -1,5 +1,5 @@
-"""The selective scan, the causal convolution and the embedding as differentiable torch
-operations, for training.
+"""The selective scan, the causal convolution, the embedding, the norm and the projection in 8 bits as
+differentiable torch operations, for training.
 
 The scan's forward runs ``mb_scan_fwd_ckpt`` (y in u's dtype, h_last, and the state
 every 16 bytes); the backward runs ``mb_scan_bwd`` from those checkpoints.  All
@@ -8,7 +8,8 @@ the two calls.  dB and dC come back in fp32 and are handed to autograd in B's
 and C's dtype.  Supported as the library's backward is: dstate 16 and L a
 multiple of 16 (the library raises otherwise).  The convolution's backward is
 ``mb_conv1d_bwd``, which computes the forward again from x; the embedding's is
-``mb_embedding_bwd``.
+``mb_embedding_bwd``, the norm's ``mb_rms_norm_bwd``.  The projection's products are all
+``mb_matmul_fp8``, of what ``mb_quantize_fp8`` makes of the factors as each of them needs it.
 """
 from __future__ import annotations
 
@@ -90,3 +91,65 @@ def embedding(tokens, weight, *, scale=1.0, out_dtype=None):
     """Differentiable scale * weight[tokens].  Shapes and types as for ``embedding_fwd``; the gradient flows to
     ``weight``, in its type."""
     return _Embedding.apply(tokens, weight, scale, out_dtype)
+
+
+class _RmsNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, residual, eps, out_dtype):
+        res = _b.rms_norm_fwd(x, weight, residual, eps=eps, out_dtype=out_dtype, return_rstd=True)
+        y, rstd = res[0], res[-1]
+        h = x if residual is None else res[1]
+        ctx.xtype, ctx.ytype, ctx.added = x.dtype, y.dtype, residual is not None
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(h, rstd, weight)
+        return y if residual is None else (y, h)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, dh=None):
+        h, rstd, weight = ctx.saved_tensors
+        if dy is None:
+            if dh is None:
+                return None, None, None, None, None
+            return dh.to(ctx.xtype), None if weight is None else torch.zeros_like(weight), dh, None, None
+        if ctx.added and dh is None:
+            dh = torch.zeros_like(h)
+        g = _b.rms_norm_bwd(dy.contiguous(), h, rstd, weight, None if dh is None else dh.contiguous(), dx_dtype=ctx.xtype)
+        return g["dx"], g["dweight"], g.get("dresidual"), None, None
+
+
+def rms_norm(x, weight=None, residual=None, *, eps=1e-5, out_dtype=None):
+    """Differentiable ``rms_norm_fwd``: y, or (y, h) with a residual.  Shapes and types as there; gradients flow to every
+    tensor argument, once: a second derivative raises."""
+    return _RmsNorm.apply(x, weight, residual, eps, out_dtype)
+
+
+class _LinearFp8(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight):
+        ctx.save_for_backward(x, weight)
+        rows = x.reshape(-1, x.shape[-1])
+        y = _b.matmul_fp8(*_b.quantize_fp8(rows), *_b.quantize_fp8(weight, tile=True), out_dtype=x.dtype)
+        return y.view(x.shape[:-1] + (weight.shape[0],))
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        x, weight = ctx.saved_tensors
+        dy = dy.contiguous().view(-1, weight.shape[0])
+        dx = dw = None
+        if ctx.needs_input_grad[0]:
+            dx = _b.matmul_fp8(*_b.quantize_fp8(dy), *_b.quantize_fp8(weight, tile=True, transpose=True),
+                               out_dtype=x.dtype).view(x.shape)
+        if ctx.needs_input_grad[1]:
+            dw = _b.matmul_fp8(*_b.quantize_fp8(dy, transpose=True), *_b.quantize_fp8(x.reshape(-1, x.shape[-1]), transpose=True),
+                               out_dtype=weight.dtype)
+        return dx, dw
+
+
+def linear_fp8(x, weight):
+    """Differentiable projection x (..., k) by weight (n, k), each fp32 or bf16, with every product in 8 bits: (..., n) in
+    x's type.  x and the gradient are quantised per row and the weight per tile, as ``quantize_fp8`` does it; the weight's
+    gradient is the product of both per column, along the rows.  Gradients are those of the unrounded product, taken
+    once: a second derivative raises."""
+    return _LinearFp8.apply(x, weight)

@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "mbscan.h"
 
 namespace mbs {
@@ -34,6 +36,47 @@ inline bool mul_ok(int64_t a, int64_t b, int64_t *out) {
     *out = a * b;
     return true;
 }
+
+struct Range { const void *p; size_t n; };
+
+// Does any of the outputs overlap an input or another output?
+template <int NO, int NI> inline bool any_overlap(const Range (&outs)[NO], const Range (&ins)[NI]) {
+    for (int i = 0; i < NO; ++i) {
+        for (const Range &r : ins)
+            if (overlaps(outs[i].p, outs[i].n, r.p, r.n)) return true;
+        for (int k = i + 1; k < NO; ++k)
+            if (overlaps(outs[i].p, outs[i].n, outs[k].p, outs[k].n)) return true;
+    }
+    return false;
+}
+
+inline int status(hipError_t e) { return e == hipSuccess ? MB_OK : MB_ERR_HIP; }
+
+inline hipStream_t st_of(void *stream) { return static_cast<hipStream_t>(stream); }
+
+// The caller's workspace, or memory allocated on the stream for the call (`at` null: it could not be).
+struct Workspace {
+    char *at;
+    hipStream_t st;
+    bool own;
+    Workspace(void *given, size_t bytes, hipStream_t stream) : at(static_cast<char *>(given)), st(stream), own(!given) {
+        if (own && hipMallocAsync(reinterpret_cast<void **>(&at), std::max<size_t>(bytes, 16), st) != hipSuccess) at = nullptr;
+    }
+    hipError_t done(hipError_t e) const {
+        const hipError_t f = own ? hipFreeAsync(at, st) : hipSuccess;
+        return e != hipSuccess ? e : f;
+    }
+};
+
+// The workspace's areas, each on a 256-byte boundary.
+struct Areas {
+    size_t bytes = 0;
+    size_t add(size_t n) {
+        const size_t at = bytes;
+        bytes += (n + 255) / 256 * 256;
+        return at;
+    }
+};
 
 inline hipError_t launch(const void *fn, dim3 grid, dim3 block, void *params, void *stream) {
     void *args[] = {params};

@@ -1,0 +1,391 @@
+// fp8_matmul.hpp -- products of matrices in 8 bits (e4m3) with a scale for each block of 128 along the inner dimension.
+//
+//   C[m][n] = sum over blocks k of sa[m][k] sb[n][k] (sum over the block's 128 places of a[m][.] b[n][.])
+//
+// a (M, K), b (N, K) row-major, scales per row or per tile of 128 rows, C (M, N).
+//
+// A C of 16 bits: one matrix instruction (16 x 16 x 128) takes a whole block, and its result is scaled as it leaves.  It sums
+// 8 neighbouring products at a time with 14 bits from the largest's leading one down, and those sums in fp32 (found by products of
+// two powers of two): an error of at most 7 x 2^-13 of each 8's largest product, where the values themselves were rounded to
+// 4 bits and C will be to 8.  A C of 32 bits: values are widened to 16 bits, which is exact, and the 16-bit
+// instruction, at half the rate, sums in fp32.  Scaling and the sum over blocks are fp32 in both, with one rounding to C's type.
+//
+// The instruction is given b's rows as its first operand: a lane then holds 4 neighbouring columns of one row of C.  Which 16
+// of a wave's 64 columns make an instruction's is free, and they are taken 4 by 4 from each quarter, so that a lane's 4
+// results are 16 neighbouring columns and the 64 lanes store whole 128-byte lines.  Along the block any order is right that both
+// operands share.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "device_math.hpp"
+#include "fp8.hpp"
+#include "lanes.hpp"
+
+namespace mbs {
+namespace matmul {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kBlock = fp8::kBlock;
+
+struct Params {
+    int64_t m, n, k;
+    int64_t a_step, b_step;         // elements from one product of the batch to the next (0: the same matrix)
+    int64_t as_step, bs_step;       // and scales
+    int32_t blocks;                 // of the inner dimension
+    int32_t a_shift, b_shift;       // rows to a scale: 1 << shift
+    uint32_t m_tiles, n_tiles;
+    const uint8_t *a, *b;
+    const float *as, *bs;
+    void *c;
+};
+
+// 8 values in 16 bits.
+__device__ __forceinline__ bf16x8 widen(int lo, int hi) {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// The product over one block of 128, for a C of type OUT.
+template <int OUT> __device__ __forceinline__ f32x4 block_product(i32x8 b, i32x8 a) {
+    f32x4 d = {0.0f, 0.0f, 0.0f, 0.0f};
+    if constexpr (OUT == 1) return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, d, 0, 0, 0, 0, 0, 0);
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+        d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(b[2 * s], b[2 * s + 1]), widen(a[2 * s], a[2 * s + 1]), d, 0, 0, 0);
+    return d;
+}
+
+// The value is in registers from here on.
+__device__ __forceinline__ void formed(f32x4 &v) { asm volatile("" : "+v"(v)); }
+
+// 16 bytes of a row of `left` more bytes, zeros past its end.
+__device__ __forceinline__ u32x4 load16(const uint8_t *p, int64_t left) {
+    if (left >= 16) return *reinterpret_cast<const fp8::u32x4_byte *>(p);
+    u32x4 r = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (i < left) r[i / 4] |= (uint32_t)p[i] << (8 * (i % 4));
+    return r;
+}
+
+// Rows of 128 bytes in LDS as 8 pieces of 16.  16 lanes read a piece each of 16 rows at once, served from 256 bytes' worth of banks: a
+// row's pieces are permuted so that those 16 lie in different ones.  Of a the 16 rows are neighbours, of b 4 by 4.
+__device__ __forceinline__ int a_place(int row, int piece) { return row * kBlock + 16 * (piece ^ ((row >> 1) & 7)); }
+__device__ __forceinline__ int b_place(int row, int piece) {
+    return row * kBlock + 16 * (piece ^ (((row >> 1) & 1) | ((row >> 3) & 6)));
+}
+// The row of b that lane l (of 16) of column tile j reads.
+__device__ __forceinline__ int b_row(int j, int l) { return (l >> 2) * 16 + 4 * j + (l & 3); }
+
+__device__ __forceinline__ i32x8 join(u32x4 x, u32x4 y) {
+    return i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
+}
+
+__device__ __forceinline__ i32x8 two_pieces(const uint8_t *lds, int first, int second) {
+    return join(*reinterpret_cast<const u32x4 *>(lds + first), *reinterpret_cast<const u32x4 *>(lds + second));
+}
+
+// 16 neighbouring columns of a row of C, the first n of them.
+template <int OUT> __device__ __forceinline__ void store_columns(void *c, int64_t at, const f32x4 (&v)[4], int64_t n) {
+    if (n >= 16) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float s[8] = {v[2 * h][0], v[2 * h][1], v[2 * h][2], v[2 * h][3],
+                                v[2 * h + 1][0], v[2 * h + 1][1], v[2 * h + 1][2], v[2 * h + 1][3]};
+            store_span<OUT, 8>(c, at + 8 * h, s);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (i < n) st_out<OUT>(c, at + i, v[i / 4][i % 4]);
+    }
+}
+
+// The tile of a workgroup.  Consecutive workgroups go to the 8 dies in turn: each die gets a stretch of neighbouring tiles, whose
+// operands its cache then holds, and walks it in columns of kGroup tiles.
+constexpr uint32_t kDies = 8, kGroup = 8;
+struct Tile { uint32_t z, m, n; };
+__device__ __forceinline__ Tile tile_of(const Params &p) {
+    const uint32_t each = p.m_tiles * p.n_tiles, all = gridDim.x, die = blockIdx.x % kDies, at = blockIdx.x / kDies;
+    const uint32_t id = die * (all / kDies) + min(die, all % kDies) + at, z = id / each, t = id - z * each;
+    const uint32_t group = t / (kGroup * p.n_tiles), first = group * kGroup, high = min(kGroup, p.m_tiles - first);
+    const uint32_t in = t - first * p.n_tiles;
+    return Tile{z, first + in % high, in / high};
+}
+
+// ---- large products: tiles through LDS ------------------------------------------------
+
+// Rows whose pieces of 16 bytes are whole and aligned go from memory to LDS directly (buffer loads: what lies past a matrix's last row or
+// past k reads as zeros).  Two buffers: while a block's products are formed the next one's rows arrive, one barrier a
+// block.  A wave has 16 MI rows of a by 64 of b.  ONE: a scale per tile on that side (1: a, 2: b, 0: on neither), which leaves one
+// multiply-add per result and block instead of two instructions.
+template <int WM, int WN, int MI> struct Shape {
+    static constexpr int kThreads = 64 * WM * WN, kM = WM * 16 * MI, kN = WN * 64;
+    static constexpr int kStep = kThreads / 8;          // rows that one load of all threads brings
+};
+
+typedef __attribute__((address_space(3))) void lds_void;
+
+// 16 bytes for each lane from `offset` and `block` bytes on in a buffer of `bytes` to lane after lane of `lds`; zeros past the buffer.
+__device__ __forceinline__ void load_to_lds(const void *base, int bytes, void *lds, uint32_t offset, int block) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, bytes, 0x00027000),
+                                             (lds_void *)lds, 16, (int)offset, block, 0, 0);
+}
+// A float for each lane.
+__device__ __forceinline__ void load_to_lds(const float *from, float *lds) {
+    __builtin_amdgcn_global_load_lds(const_cast<float *>(from), (lds_void *)lds, 4, 0, 0);
+}
+
+template <int OUT, int ONE, int WM, int WN, int MI>
+__global__ __launch_bounds__(64 * WM * WN) void matmul_tiles(Params p) {
+    using S = Shape<WM, WN, MI>;
+    __shared__ __align__(128) uint8_t la0[S::kM * kBlock], lb0[S::kN * kBlock], la1[S::kM * kBlock], lb1[S::kN * kBlock];
+    __shared__ __align__(16) float ls0[S::kM + S::kN], ls1[S::kM + S::kN];
+    const int t = threadIdx.x, lane = t & 63, l16 = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const Tile tile = tile_of(p);
+    const int64_t m0 = (int64_t)tile.m * S::kM, n0 = (int64_t)tile.n * S::kN;
+    const int wm = wave % WM * 16 * MI, wn = wave / WM * 64;
+    const int rows_a = (int)min((int64_t)S::kM, p.m - m0), rows_b = (int)min((int64_t)S::kN, p.n - n0);
+    const int K = (int)p.k;
+    const uint8_t *a = p.a + tile.z * p.a_step + m0 * p.k, *b = p.b + tile.z * p.b_step + n0 * p.k;
+    const float *as = p.as + tile.z * p.as_step, *bs = p.bs + tile.z * p.bs_step;
+
+    // what a thread loads: a piece of row t / 8 and of every kStep-th from there on, and one row's scale (or two)
+    const int row = t / 8;
+    const int piece_a = 16 * ((t & 7) ^ ((row >> 1) & 7)), piece_b = 16 * ((t & 7) ^ (((row >> 1) & 1) | ((row >> 3) & 6)));
+    const int va = row * K + piece_a;
+    constexpr int kScales = (S::kM + S::kN + S::kThreads - 1) / S::kThreads;
+    const float *scale_at[kScales];
+#pragma unroll
+    for (int i = 0; i < kScales; ++i) {
+        const int at = i * S::kThreads + t;
+        scale_at[i] = at < S::kM ? as + (min(m0 + at, p.m - 1) >> p.a_shift) * p.blocks
+                                 : bs + (min(n0 + min(at - S::kM, S::kN - 1), p.n - 1) >> p.b_shift) * p.blocks;
+    }
+    auto fetch = [&](uint8_t *la, uint8_t *lb, float *ls, int kb) {
+        // 2^31 and more (a tile has less than 2^30 bytes) lies past every buffer
+        const int k = kb * kBlock;
+        const uint32_t oa = k + piece_a < K ? va : 0x80000000u;
+#pragma unroll
+        for (int i = 0; i < S::kM / S::kStep; ++i)
+            load_to_lds(a, rows_a * K, la + i * S::kStep * kBlock + wave * 1024, oa + i * S::kStep * K, k);
+#pragma unroll
+        for (int i = 0; i < S::kN / S::kStep; ++i) {
+            const int turn = i * S::kStep & 32 ? 64 : 0;            // bit 5 of b's row is in its pieces' permutation
+            const uint32_t ob = k + (piece_b ^ turn) < K ? row * K + (piece_b ^ turn) : 0x80000000u;
+            load_to_lds(b, rows_b * K, lb + i * S::kStep * kBlock + wave * 1024, ob + i * S::kStep * K, k);
+        }
+#pragma unroll
+        for (int i = 0; i < kScales; ++i)
+            if ((i + 1) * S::kThreads <= S::kM + S::kN || i * S::kThreads + wave * 64 < S::kM + S::kN)
+                load_to_lds(scale_at[i] + kb, ls + i * S::kThreads + wave * 64);
+    };
+
+    // a wave's rows begin at multiples of 16 and of 64: the pieces' permutations are the same for every i and j
+    const int pa = wm * kBlock + a_place(l16, g), pb = wn * kBlock + b_place(b_row(0, l16), g);
+    f32x4 acc[MI][4] = {};
+    auto products = [&](const uint8_t *la, const uint8_t *lb, const float *ls) {
+        i32x8 fb[4];
+        f32x4 sb[4];
+        const float *lsa = ls + wm, *lsb = ls + S::kM + wn;
+        float one = 1.0f;
+        if constexpr (ONE == 1) one = lsa[0];
+        if constexpr (ONE == 2) one = lsb[0];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            fb[j] = two_pieces(lb + 4 * j * kBlock, pb, pb ^ 64);
+            if constexpr (ONE != 2) sb[j] = *reinterpret_cast<const f32x4 *>(lsb + 16 * g + 4 * j) * one;
+        }
+        i32x8 fa = two_pieces(la, pa, pa ^ 64);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            float sa = 1.0f;
+            if constexpr (ONE != 1) sa = lsa[16 * i + l16];
+            if constexpr (ONE == 2) sa *= one;
+            i32x8 next = fa;
+            if (i + 1 < MI) next = two_pieces(la + 16 * (i + 1) * kBlock, pa, pa ^ 64);
+            f32x4 d[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) d[j] = block_product<OUT>(fb[j], fa);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    acc[i][j][q] = __builtin_fmaf(d[j][q], ONE == 1 ? sb[j][q] : ONE == 2 ? sa : sb[j][q] * sa, acc[i][j][q]);
+            fa = next;
+            // the sums stay here: put off until their next use, the unscaled results of a whole block would be kept instead.
+            // Rows of a are read one step ahead and no further: more would not fit the registers
+#pragma unroll
+            for (int j = 0; j < 4; ++j) formed(acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+
+    // tile kb arrived and nobody reads the buffer that kb + 1 goes to any more
+    if (p.blocks > 0) fetch(la0, lb0, ls0, 0);
+    for (int kb = 0; kb < p.blocks; kb += 2) {
+        __syncthreads();
+        if (kb + 1 < p.blocks) fetch(la1, lb1, ls1, kb + 1);
+        products(la0, lb0, ls0);
+        __syncthreads();
+        if (kb + 2 < p.blocks) fetch(la0, lb0, ls0, kb + 2);
+        if (kb + 1 < p.blocks) products(la1, lb1, ls1);
+    }
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+        const int64_t m = m0 + wm + 16 * i + l16, n = n0 + wn + 16 * g;
+        if (m < p.m && n < p.n) store_columns<OUT>(p.c, ((int64_t)tile.z * p.m + m) * p.n + n, acc[i], p.n - n);
+    }
+}
+
+// Rows of any length and alignment: they pass through registers on their way to LDS, cut to zeros where they end.
+constexpr int kAnyTile = 128, kAnyThreads = 256;        // 2 x 2 waves of 64 x 64
+template <int OUT>
+__global__ __launch_bounds__(kAnyThreads) void matmul_any(Params p) {
+    __shared__ __align__(16) uint8_t la[kAnyTile * kBlock], lb[kAnyTile * kBlock];
+    __shared__ __align__(16) float lsa[kAnyTile], lsb[kAnyTile];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, l16 = lane & 15, g = lane >> 4;
+    const Tile tile = tile_of(p);
+    const int64_t m0 = (int64_t)tile.m * kAnyTile, n0 = (int64_t)tile.n * kAnyTile;
+    const int wm = (wave & 1) * 64, wn = (wave >> 1) * 64;
+    const uint8_t *a = p.a + tile.z * p.a_step, *b = p.b + tile.z * p.b_step;
+    const float *as = p.as + tile.z * p.as_step, *bs = p.bs + tile.z * p.bs_step;
+
+    // a thread's pieces: rows t / 8 and every 32nd from there on
+    constexpr int kPieces = kAnyTile / 32;
+    u32x4 ra[kPieces], rb[kPieces];
+    float rs = 0.0f;
+    const bool of_a = t < kAnyTile;
+    const int64_t srow = of_a ? min(m0 + t, p.m - 1) >> p.a_shift : min(n0 + t - kAnyTile, p.n - 1) >> p.b_shift;
+    auto fetch = [&](int kb) {
+        const int64_t k = (int64_t)kb * kBlock + 16 * (t & 7);
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int64_t ma = min(m0 + t / 8 + 32 * i, p.m - 1), nb = min(n0 + t / 8 + 32 * i, p.n - 1);
+            ra[i] = load16(a + ma * p.k + k, p.k - k);
+            rb[i] = load16(b + nb * p.k + k, p.k - k);
+        }
+        rs = (of_a ? as : bs)[srow * p.blocks + kb];
+    };
+
+    f32x4 acc[4][4] = {};
+    if (p.blocks > 0) fetch(0);
+    for (int kb = 0; kb < p.blocks; ++kb) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            *reinterpret_cast<u32x4 *>(la + a_place(t / 8 + 32 * i, t & 7)) = ra[i];
+            *reinterpret_cast<u32x4 *>(lb + b_place(t / 8 + 32 * i, t & 7)) = rb[i];
+        }
+        (of_a ? lsa : lsb)[t & (kAnyTile - 1)] = rs;
+        __syncthreads();
+        if (kb + 1 < p.blocks) fetch(kb + 1);
+        i32x8 fb[4];
+        f32x4 sb[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int row = wn + b_row(j, l16);
+            fb[j] = two_pieces(lb, b_place(row, g), b_place(row, g + 4));
+            sb[j] = *reinterpret_cast<const f32x4 *>(lsb + wn + 16 * g + 4 * j);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = wm + 16 * i + l16;
+            const i32x8 fa = two_pieces(la, a_place(row, g), a_place(row, g + 4));
+            const float sa = lsa[row];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const f32x4 d = block_product<OUT>(fb[j], fa);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[i][j][r] = __builtin_fmaf(d[r], sb[j][r] * sa, acc[i][j][r]);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t m = m0 + wm + 16 * i + l16, n = n0 + wn + 16 * g;
+        if (m < p.m && n < p.n) store_columns<OUT>(p.c, ((int64_t)tile.z * p.m + m) * p.n + n, acc[i], p.n - n);
+    }
+}
+
+// ---- small products: a tile's blocks among a workgroup's waves --------------------------
+
+// Few tiles, or so few rows that reading the other operand is all the work: operands go to registers without a detour, each wave takes every
+// kSplit-th block, and the waves' sums are joined in LDS in their order.
+constexpr int kSplit = 8;
+template <int OUT, int MI, int NJ>
+__global__ __launch_bounds__(64 * kSplit) void matmul_split(Params p) {
+    __shared__ __align__(16) f32x4 sums[kSplit][MI * NJ][64];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, l16 = lane & 15, g = lane >> 4;
+    const Tile tile = tile_of(p);
+    const int64_t m0 = (int64_t)tile.m * 16 * MI, n0 = (int64_t)tile.n * 16 * NJ;
+    const uint8_t *a = p.a + tile.z * p.a_step, *b = p.b + tile.z * p.b_step;
+    const float *as = p.as + tile.z * p.as_step, *bs = p.bs + tile.z * p.bs_step;
+    // rows past the last: the last once more
+    const uint8_t *at_a[MI], *at_b[NJ];
+    const float *sa_at[MI], *sb_at[NJ][4];
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+        const int64_t m = min(m0 + 16 * i + l16, p.m - 1);
+        at_a[i] = a + m * p.k;
+        sa_at[i] = as + (m >> p.a_shift) * p.blocks;
+    }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+        at_b[j] = b + min(n0 + 16 * j + l16, p.n - 1) * p.k;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sb_at[j][q] = bs + (min(n0 + 16 * j + 4 * g + q, p.n - 1) >> p.b_shift) * p.blocks;
+    }
+    f32x4 acc[MI][NJ] = {};
+    for (int kb = wave; kb < p.blocks; kb += kSplit) {
+        const int64_t k = (int64_t)kb * kBlock + 32 * g, left = p.k - k;
+        i32x8 fa[MI], fb[NJ];
+        float sa[MI];
+        f32x4 sb[NJ];
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            fb[j] = join(load16(at_b[j] + k, left), load16(at_b[j] + k + 16, left - 16));
+#pragma unroll
+            for (int q = 0; q < 4; ++q) sb[j][q] = sb_at[j][q][kb];
+        }
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            fa[i] = join(load16(at_a[i] + k, left), load16(at_a[i] + k + 16, left - 16));
+            sa[i] = sa_at[i][kb];
+        }
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                const f32x4 d = block_product<OUT>(fb[j], fa[i]);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) acc[i][j][q] = __builtin_fmaf(d[q], sb[j][q] * sa[i], acc[i][j][q]);
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) sums[wave][i * NJ + j][lane] = acc[i][j];
+    __syncthreads();
+    for (int e = t; e < MI * NJ * 64; e += 64 * kSplit) {
+        const int ij = e / 64, l = e & 63, i = ij / NJ, j = ij % NJ;
+        f32x4 v = sums[0][ij][l];
+#pragma unroll
+        for (int w = 1; w < kSplit; ++w) v += sums[w][ij][l];
+        const int64_t m = m0 + 16 * i + (l & 15), n = n0 + 16 * j + 4 * (l >> 4);
+        if (m >= p.m) continue;
+        const int64_t at = ((int64_t)tile.z * p.m + m) * p.n + n;
+        const float r[4] = {v[0], v[1], v[2], v[3]};
+        if (n + 4 <= p.n) store_span<OUT, 4>(p.c, at, r);
+        else store_first<OUT, 4>(p.c, at, r, (int)max(p.n - n, (int64_t)0));
+    }
+}
+
+}  // namespace matmul
+}  // namespace mbs

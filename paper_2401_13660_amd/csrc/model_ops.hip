@@ -19,37 +19,6 @@ namespace {
 
 using namespace mbs::abi;
 
-struct Range { const void *p; size_t n; };
-
-// Does any of the outputs overlap an input or another output?
-template <int NO, int NI> bool any_overlap(const Range (&outs)[NO], const Range (&ins)[NI]) {
-    for (int i = 0; i < NO; ++i) {
-        for (const Range &r : ins)
-            if (overlaps(outs[i].p, outs[i].n, r.p, r.n)) return true;
-        for (int k = i + 1; k < NO; ++k)
-            if (overlaps(outs[i].p, outs[i].n, outs[k].p, outs[k].n)) return true;
-    }
-    return false;
-}
-
-int status(hipError_t e) { return e == hipSuccess ? MB_OK : MB_ERR_HIP; }
-
-hipStream_t st_of(void *stream) { return static_cast<hipStream_t>(stream); }
-
-// The caller's workspace, or memory allocated on the stream for the call (`at` null: it could not be).
-struct Workspace {
-    char *at;
-    hipStream_t st;
-    bool own;
-    Workspace(void *given, size_t bytes, hipStream_t stream) : at(static_cast<char *>(given)), st(stream), own(!given) {
-        if (own && hipMallocAsync(reinterpret_cast<void **>(&at), std::max<size_t>(bytes, 16), st) != hipSuccess) at = nullptr;
-    }
-    hipError_t done(hipError_t e) const {
-        const hipError_t f = own ? hipFreeAsync(at, st) : hipSuccess;
-        return e != hipSuccess ? e : f;
-    }
-};
-
 bool valid_token_type(int32_t t) { return t == MB_TOKEN_U8 || t == MB_TOKEN_I32 || t == MB_TOKEN_I64; }
 size_t token_size(int32_t t) { return t == MB_TOKEN_U8 ? 1 : t == MB_TOKEN_I32 ? 4 : 8; }
 
@@ -66,16 +35,6 @@ template <int TOK> const void *embed_fwd_fn(int32_t in, int32_t out, int64_t dim
     if (in == MB_F32) return out == MB_F32 ? embed_fwd_fn<TOK, 0, 0>(dim, span) : embed_fwd_fn<TOK, 0, 1>(dim, span);
     return out == MB_F32 ? embed_fwd_fn<TOK, 1, 0>(dim, span) : embed_fwd_fn<TOK, 1, 1>(dim, span);
 }
-
-// The workspace's areas, each on a 256-byte boundary.
-struct Areas {
-    size_t bytes = 0;
-    size_t add(size_t n) {
-        const size_t at = bytes;
-        bytes += (n + 255) / 256 * 256;
-        return at;
-    }
-};
 
 // The sort of an embedding's gradient and its workspace.
 struct EmbedPlan {
