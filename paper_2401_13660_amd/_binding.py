@@ -136,7 +136,9 @@ def _load_fast(lib):
                                                 lib.mb_embedding_bwd_workspace, lib.mb_conv1d_bwd,
                                                 lib.mb_conv1d_bwd_workspace, lib.mb_grad_norm,
                                                 lib.mb_grad_norm_workspace, lib.mb_clip_grad_norm,
-                                                lib.mb_verify_sample, lib.mb_verify_sample_workspace)]
+                                                lib.mb_verify_sample, lib.mb_verify_sample_workspace,
+                                                lib.mb_rms_norm_fwd, lib.mb_rms_norm_bwd, lib.mb_rms_norm_bwd_workspace,
+                                                lib.mb_quantize_fp8, lib.mb_matmul_fp8, lib.mb_sample)]
     _fastcall.setup(*at, _cur_device, _raw_stream, torch.nn.Parameter)
     return _fastcall
 
@@ -798,6 +800,10 @@ def rms_norm_fwd(x, weight=None, residual=None, *, eps=1e-5, out_dtype=None, ret
     ``residual_out`` may be ``residual``: h takes its place.  Returns y in ``out_dtype`` (x's by default), or (y, h)
     with a residual; ``return_rstd`` appends 1 / sqrt(mean(h^2) + eps), fp32 of x's leading shape, for ``rms_norm_bwd``."""
     load_library()
+    if _fast is not None:
+        res = _fast.rms_norm_fwd(x, weight, residual, eps, out_dtype, return_rstd, out, residual_out)
+        if res is not None:
+            return _done(res, "mb_rms_norm_fwd")
     rows, d, dev = _norm_inputs(x, weight, residual)
     given = [t for t in (out, residual_out) if t is not None]
     if out is None:
@@ -817,6 +823,10 @@ def rms_norm_fp8(x, weight=None, residual=None, *, eps=1e-5, residual_out=None):
     """rms_norm_fwd with y in 8 bits, as ``matmul_fp8`` takes it.  Returns (q, scale) or, with a residual, (q, scale, h):
     q (..., dim) float8_e4m3fn, scale (..., ceil(dim / 128)) fp32, y being q times its block's scale."""
     load_library()
+    if _fast is not None:
+        res = _fast.rms_norm_fp8(x, weight, residual, eps, residual_out)
+        if res is not None:
+            return _done(res, "mb_rms_norm_fwd")
     rows, d, dev = _norm_inputs(x, weight, residual)
     q = torch.empty(x.shape, dtype=FP8, device=dev)
     scale = torch.empty(x.shape[:-1] + (_blocks(d),), dtype=torch.float32, device=dev)
@@ -835,6 +845,13 @@ def rms_norm_bwd(dy, h, rstd, weight=None, dh=None, *, dx_dtype=None):
     dweight (dim,) fp32 (None without a weight) and, with dh, dresidual in h's type (the tensor dx itself where that is
     dx's type)."""
     lib = load_library()
+    if _fast is not None:
+        res = _fast.rms_norm_bwd(dy, h, rstd, weight, dh, dx_dtype)
+        if res is not None:
+            res = dict(zip(("dx", "dweight", "dresidual"), _done(res, "mb_rms_norm_bwd")))
+            if dh is None:
+                del res["dresidual"]
+            return res
     if not isinstance(h, torch.Tensor) or h.dim() < 1:
         raise MBScanError("h must be a (..., dim) tensor")
     dev, d = h.device, h.shape[-1]
@@ -865,6 +882,10 @@ def quantize_fp8(x, *, tile=False, transpose=False):
     (..., rows, ceil(cols / 128)), or with ``tile`` (..., ceil(rows / 128), ceil(cols / 128)).  ``transpose``: the same of
     x's transposed matrices, q (..., cols, rows)."""
     lib = load_library()
+    if _fast is not None:
+        res = _fast.quantize_fp8(x, tile, transpose)
+        if res is not None:
+            return _done(res, "mb_quantize_fp8")
     if not isinstance(x, torch.Tensor) or x.dim() < 2:
         raise MBScanError("x must be a (..., rows, cols) tensor")
     _need(x, "x", x.shape)
@@ -902,6 +923,10 @@ def matmul_fp8(a, a_scale, b, b_scale, *, out_dtype=torch.bfloat16, out=None):
     or per tile, told by their shape) or ``rms_norm_fp8``.  Returns (m, n), or (batch, m, n) if either has a batch, in
     ``out_dtype``: fp32 or bf16."""
     lib = load_library()
+    if _fast is not None:
+        res = _fast.matmul_fp8(a, a_scale, b, b_scale, out_dtype, out)
+        if res is not None:
+            return _done(res, "mb_matmul_fp8")
     dev = a.device if isinstance(a, torch.Tensor) else None
     a_batch, m, a_tile = _matrix(a, a_scale, "a", dev)
     b_batch, n, b_tile = _matrix(b, b_scale, "b", dev)
@@ -936,6 +961,10 @@ def sample(logits, noise, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, ret
     their index.  Returns the tokens, int32 (batch,), -1 for a row that is no distribution; ``return_prob`` adds the
     probabilities that they were drawn with, fp32 (batch,)."""
     lib = load_library()
+    if _fast is not None:
+        res = _fast.sample(logits, noise, temperature, top_k, top_p, min_p, return_prob)
+        if res is not None:
+            return _done(res, "mb_sample")
     if not isinstance(logits, torch.Tensor) or logits.dim() != 2:
         raise MBScanError("logits must be a (batch, vocab) tensor")
     nb, V = logits.shape

@@ -91,6 +91,17 @@ template <int X> const void *quant_fn(bool tile, bool transpose) {
                      : reinterpret_cast<const void *>(&Q::quantize<X, false, false>);
 }
 
+// ---- sampling -----------------------------------------------------------------------
+
+template <int DT> const void *sample_fn(int64_t vocab, unsigned *threads) {
+    namespace S = mbs::pick;
+    *threads = vocab <= 1024 ? 256 : 1024;
+    if (vocab <= 1024) return reinterpret_cast<const void *>(&S::sample_rows<DT, 256, 1>);
+    if (vocab <= 8192) return reinterpret_cast<const void *>(&S::sample_rows<DT, 1024, 2>);
+    if (vocab <= 32768) return reinterpret_cast<const void *>(&S::sample_rows<DT, 1024, 8>);
+    return reinterpret_cast<const void *>(&S::sample_rows<DT, 1024, 0>);
+}
+
 // Which kernel takes a product, and its tiles.
 struct MatmulPlan {
     const void *fn;
@@ -286,9 +297,9 @@ int mb_sample(int64_t batch, int64_t vocab, int32_t logit_dtype, float temperatu
                          {top_ks, b_b}, {top_ps, b_b}, {min_ps, b_b}};
     if (any_overlap(outs, ins)) return MB_ERR_ALIAS;
     S::Params p{batch, vocab, logits, noise, temperatures, top_ps, min_ps, top_ks, temperature, top_p, min_p, top_k, token, prob};
-    const void *fn = logit_dtype == MB_F32 ? reinterpret_cast<const void *>(&S::sample_any<0>)
-                                           : reinterpret_cast<const void *>(&S::sample_any<1>);
-    return status(launch(fn, dim3((unsigned)batch), dim3(S::kThreads), &p, stream));
+    unsigned threads;
+    const void *fn = logit_dtype == MB_F32 ? sample_fn<0>(vocab, &threads) : sample_fn<1>(vocab, &threads);
+    return status(launch(fn, dim3((unsigned)batch), dim3(threads), &p, stream));
 }
 
 }  // extern "C"

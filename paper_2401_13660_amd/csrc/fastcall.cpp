@@ -21,6 +21,7 @@
 
 #include <initializer_list>
 #include <optional>
+#include <utility>
 #include <vector>
 
 #include "mbscan.h"
@@ -44,6 +45,12 @@ decltype(&mb_grad_norm_workspace) grad_norm_workspace_fn;
 decltype(&mb_clip_grad_norm) clip_grad_norm_fn;
 decltype(&mb_verify_sample) verify_sample_fn;
 decltype(&mb_verify_sample_workspace) verify_sample_workspace_fn;
+decltype(&mb_rms_norm_fwd) rms_norm_fwd_fn;
+decltype(&mb_rms_norm_bwd) rms_norm_bwd_fn;
+decltype(&mb_rms_norm_bwd_workspace) rms_norm_bwd_workspace_fn;
+decltype(&mb_quantize_fp8) quantize_fp8_fn;
+decltype(&mb_matmul_fp8) matmul_fp8_fn;
+decltype(&mb_sample) sample_fn;
 PyObject *current_device, *raw_stream, *parameter_type;   // torch's accessors and nn.Parameter
 
 // A plain dense tensor on the GPU (no subclass, no transform's wrapper), or null.
@@ -577,9 +584,254 @@ PyObject *verify_sample(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
     });
 }
 
+constexpr auto kFp8 = at::kFloat8_e4m3fn;
+int64_t blocks(int64_t n) { return (n + 127) / 128; }
+using Shape = c10::SmallVector<int64_t, 5>;
+
+PyObject *tuple(std::initializer_list<PyObject *> items) {
+    PyObject *t = PyTuple_New((Py_ssize_t)items.size());
+    Py_ssize_t i = 0;
+    for (PyObject *o : items) PyTuple_SET_ITEM(t, i++, o);
+    return t;
+}
+
+// x, weight, residual, eps, out_dtype, return_rstd, out, residual_out
+PyObject *rms_norm_fwd(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    ARGS(8)
+    return guarded([&]() -> PyObject * {
+        Call c;
+        const at::Tensor *x = plain(a[0]);
+        if (!x || x->dim() < 1) Py_RETURN_NONE;
+        x = c.first(a[0], x->dim());
+        const at::Tensor *res = c.ok && a[2] != Py_None ? plain(a[2]) : nullptr;
+        if (!c.ok || !Call::act(x->scalar_type()) || (a[2] != Py_None && (!res || !Call::act(res->scalar_type())))) Py_RETURN_NONE;
+        const Shape shape(x->sizes().begin(), x->sizes().end());
+        const int64_t d = shape.back();
+        if (d == 0) Py_RETURN_NONE;
+        const auto rt = res ? res->scalar_type() : at::kFloat;
+        void *xp = c.need(a[0], shape, x->scalar_type()), *wp = c.maybe(a[1], {d}, at::kFloat), *rp = c.maybe(a[2], shape, rt);
+        const float eps = real(a[3], c.ok);
+        at::ScalarType ot = x->scalar_type();
+        if (a[6] == Py_None && a[4] != Py_None) c.dtype(a[4], ot);
+        void *op = c.given(a[6], shape, ot), *hp = c.maybe(a[7], shape, rt);
+        const int want = PyObject_IsTrue(a[5]);
+        if (want < 0 || (!res && hp)) { PyErr_Clear(); c.ok = false; }
+        PLAIN_OR_NONE(c);
+        at::Tensor out, h, rstd;
+        if (a[6] == Py_None) op = (out = c.fresh(shape, ot)).data_ptr();
+        if (res && a[7] == Py_None) hp = (h = c.fresh(shape, rt)).data_ptr();
+        if (want) rstd = c.fresh(at::IntArrayRef(shape.data(), shape.size() - 1), at::kFloat);
+        const int st = unlocked([&] {
+            return rms_norm_fwd_fn(x->numel() / d, d, code(x->scalar_type()), code(rt), code(ot), eps, xp, f(wp), rp, op, nullptr, hp,
+                                   static_cast<float *>(data(rstd)), c.stream);
+        });
+        if (st != MB_OK) return PyLong_FromLong(st);
+        if (a[6] != Py_None) was_written(a[6]);
+        if (a[7] != Py_None) was_written(a[7]);
+        PyObject *y = a[6] == Py_None ? wrap(std::move(out)) : same(a[6]);
+        if (!res) return want ? tuple({y, wrap(std::move(rstd))}) : y;
+        PyObject *k = a[7] == Py_None ? wrap(std::move(h)) : same(a[7]);
+        return want ? tuple({y, k, wrap(std::move(rstd))}) : tuple({y, k});
+    });
+}
+
+// x, weight, residual, eps, residual_out
+PyObject *rms_norm_fp8(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    ARGS(5)
+    return guarded([&]() -> PyObject * {
+        Call c;
+        const at::Tensor *x = plain(a[0]);
+        if (!x || x->dim() < 1) Py_RETURN_NONE;
+        x = c.first(a[0], x->dim());
+        const at::Tensor *res = c.ok && a[2] != Py_None ? plain(a[2]) : nullptr;
+        if (!c.ok || !Call::act(x->scalar_type()) || (a[2] != Py_None && (!res || !Call::act(res->scalar_type())))) Py_RETURN_NONE;
+        Shape shape(x->sizes().begin(), x->sizes().end());
+        const int64_t d = shape.back();
+        if (d == 0) Py_RETURN_NONE;
+        const auto rt = res ? res->scalar_type() : at::kFloat;
+        void *xp = c.need(a[0], shape, x->scalar_type()), *wp = c.maybe(a[1], {d}, at::kFloat), *rp = c.maybe(a[2], shape, rt);
+        const float eps = real(a[3], c.ok);
+        void *hp = c.maybe(a[4], shape, rt);
+        if (!res && hp) c.ok = false;
+        PLAIN_OR_NONE(c);
+        at::Tensor q = c.fresh(shape, kFp8), h;
+        if (res && a[4] == Py_None) hp = (h = c.fresh(shape, rt)).data_ptr();
+        shape.back() = blocks(d);
+        at::Tensor scale = c.fresh(shape, at::kFloat);
+        const int st = unlocked([&] {
+            return rms_norm_fwd_fn(x->numel() / d, d, code(x->scalar_type()), code(rt), MB_FP8, eps, xp, f(wp), rp, q.data_ptr(),
+                                   static_cast<float *>(scale.data_ptr()), hp, nullptr, c.stream);
+        });
+        if (st != MB_OK) return PyLong_FromLong(st);
+        if (a[4] != Py_None) was_written(a[4]);
+        PyObject *qo = wrap(std::move(q)), *so = wrap(std::move(scale));
+        return res ? tuple({qo, so, a[4] == Py_None ? wrap(std::move(h)) : same(a[4])}) : tuple({qo, so});
+    });
+}
+
+// dy, h, rstd, weight, dh, dx_dtype: dx, dweight, dresidual
+PyObject *rms_norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    ARGS(6)
+    return guarded([&]() -> PyObject * {
+        Call c;
+        const at::Tensor *h = plain(a[1]), *dy = plain(a[0]);
+        if (!h || !dy || h->dim() < 1) Py_RETURN_NONE;
+        h = c.first(a[1], h->dim());
+        if (!c.ok || !Call::act(h->scalar_type()) || !Call::act(dy->scalar_type())) Py_RETURN_NONE;
+        const Shape shape(h->sizes().begin(), h->sizes().end());
+        const int64_t d = shape.back();
+        if (d == 0) Py_RETURN_NONE;
+        const auto ht = h->scalar_type();
+        void *hp = c.need(a[1], shape, ht), *yp = c.need(a[0], shape, dy->scalar_type());
+        void *sp = c.need(a[2], at::IntArrayRef(shape.data(), shape.size() - 1), at::kFloat);
+        void *wp = c.maybe(a[3], {d}, at::kFloat), *dp = c.maybe(a[4], shape, ht);
+        at::ScalarType xt = dy->scalar_type();
+        if (a[5] != Py_None) c.dtype(a[5], xt);
+        PLAIN_OR_NONE(c);
+        const int64_t rows = h->numel() / d;
+        at::Tensor dx = c.fresh(shape, xt), dw, dres, ws;
+        if (wp) {
+            dw = c.fresh({d}, at::kFloat);
+            ws = c.workspace(rms_norm_bwd_workspace_fn(rows, d));
+        }
+        const bool apart = dp && ht != xt;
+        if (apart) dres = c.fresh(shape, ht);
+        const int st = unlocked([&] {
+            return rms_norm_bwd_fn(rows, d, code(dy->scalar_type()), code(ht), code(xt), yp, hp, f(sp), f(wp), dp, dx.data_ptr(),
+                                   data(dres), static_cast<float *>(data(dw)), data(ws), c.stream);
+        });
+        if (st != MB_OK) return PyLong_FromLong(st);
+        PyObject *x = wrap(std::move(dx)), *w = wp ? wrap(std::move(dw)) : same(Py_None);
+        return tuple({x, w, !dp ? same(Py_None) : apart ? wrap(std::move(dres)) : same(x)});
+    });
+}
+
+// x, tile, transpose
+PyObject *quantize_fp8(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    ARGS(3)
+    return guarded([&]() -> PyObject * {
+        Call c;
+        const at::Tensor *x = plain(a[0]);
+        if (!x || x->dim() < 2) Py_RETURN_NONE;
+        x = c.first(a[0], x->dim());
+        if (!c.ok || !Call::act(x->scalar_type())) Py_RETURN_NONE;
+        Shape shape(x->sizes().begin(), x->sizes().end());
+        void *xp = c.need(a[0], shape, x->scalar_type());
+        const int tile = PyObject_IsTrue(a[1]), transpose = PyObject_IsTrue(a[2]);
+        if (tile < 0 || transpose < 0) { PyErr_Clear(); c.ok = false; }
+        PLAIN_OR_NONE(c);
+        const size_t n = shape.size();
+        const int64_t rows = shape[n - 2], cols = shape[n - 1];
+        int64_t batch = 1;
+        for (size_t i = 0; i + 2 < n; ++i) batch *= shape[i];
+        if (transpose) std::swap(shape[n - 2], shape[n - 1]);
+        at::Tensor q = c.fresh(shape, kFp8);
+        if (tile) shape[n - 2] = blocks(shape[n - 2]);
+        shape[n - 1] = blocks(shape[n - 1]);
+        at::Tensor scale = c.fresh(shape, at::kFloat);
+        const int st = unlocked([&] {
+            return quantize_fp8_fn(batch, rows, cols, code(x->scalar_type()), tile, transpose, xp, q.data_ptr(),
+                                   static_cast<float *>(scale.data_ptr()), c.stream);
+        });
+        if (st != MB_OK) return PyLong_FromLong(st);
+        PyObject *qo = wrap(std::move(q));
+        return tuple({qo, wrap(std::move(scale))});
+    });
+}
+
+// a, a_scale, b, b_scale, out_dtype, out
+PyObject *matmul_fp8(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    ARGS(6)
+    return guarded([&]() -> PyObject * {
+        Call c;
+        const at::Tensor *t[2] = {plain(a[0]), plain(a[2])};
+        if (!t[0] || !t[1] || !c.first(a[0], t[0]->dim())) Py_RETURN_NONE;
+        void *at[2], *scales[2];
+        bool tile[2];
+        int64_t batch = -1;
+        for (int i = 0; i < 2; ++i) {
+            const int64_t n = t[i]->dim();
+            if (n != 2 && n != 3) Py_RETURN_NONE;
+            if (n == 3) {
+                if (batch >= 0 && batch != t[i]->size(0)) Py_RETURN_NONE;
+                batch = t[i]->size(0);
+            }
+            const at::Tensor *s = plain(a[2 * i + 1]);
+            if (!s || s->dim() != n) Py_RETURN_NONE;
+            Shape shape(t[i]->sizes().begin(), t[i]->sizes().end());
+            at[i] = c.need(a[2 * i], shape, kFp8);
+            const int64_t rows = shape[n - 2];
+            shape[n - 1] = blocks(shape[n - 1]);
+            tile[i] = s->size(n - 2) != rows;
+            if (tile[i]) shape[n - 2] = blocks(rows);
+            scales[i] = c.need(a[2 * i + 1], shape, at::kFloat);
+        }
+        const int64_t m = t[0]->size(-2), n = t[1]->size(-2), k = t[0]->size(-1);
+        if (t[1]->size(-1) != k) Py_RETURN_NONE;
+        Shape shape;
+        if (batch >= 0) shape.push_back(batch);
+        shape.push_back(m);
+        shape.push_back(n);
+        at::ScalarType ot = at::kBFloat16;
+        if (a[5] == Py_None) c.dtype(a[4], ot);
+        void *op = c.given(a[5], shape, ot);
+        PLAIN_OR_NONE(c);
+        at::Tensor out;
+        if (a[5] == Py_None) op = (out = c.fresh(shape, ot)).data_ptr();
+        const mb_matmul_desc desc{batch < 0 ? 1 : batch, m, n, k, t[0]->dim() == 3, t[1]->dim() == 3, tile[0], tile[1], code(ot), 0};
+        const int st = unlocked([&] { return matmul_fp8_fn(&desc, at[0], f(scales[0]), at[1], f(scales[1]), op, c.stream); });
+        if (st != MB_OK) return PyLong_FromLong(st);
+        if (a[5] != Py_None) was_written(a[5]);
+        return a[5] == Py_None ? wrap(std::move(out)) : same(a[5]);
+    });
+}
+
+// logits, noise, temperature, top_k, top_p, min_p, return_prob
+PyObject *sample(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
+    ARGS(7)
+    return guarded([&]() -> PyObject * {
+        Call c;
+        const at::Tensor *lg = c.first(a[0], 2);
+        if (!c.ok || !Call::act(lg->scalar_type())) Py_RETURN_NONE;
+        const int64_t nb = lg->size(0), V = lg->size(1);
+        void *lp = c.need(a[0], {nb, V}, lg->scalar_type()), *np = c.need(a[1], {nb, V}, at::kFloat);
+        // each setting a number for all, or a tensor of one for each
+        float one[4] = {1.0f, 0.0f, 1.0f, 0.0f};
+        void *each[4] = {};
+        int32_t top_k = 0;
+        for (int i = 0; i < 4; ++i) {
+            PyObject *o = a[2 + i];
+            if (THPVariable_Check(o)) {
+                each[i] = c.need(o, {nb}, i == 1 ? at::kInt : at::kFloat);
+            } else if (i == 1) {
+                int over = 0;
+                if (!PyLong_CheckExact(o)) Py_RETURN_NONE;
+                const long long k = PyLong_AsLongLongAndOverflow(o, &over);
+                if (over || k < 0 || k > INT32_MAX) Py_RETURN_NONE;
+                top_k = (int32_t)k;
+            } else {
+                one[i] = real(o, c.ok);
+            }
+        }
+        const int want = PyObject_IsTrue(a[6]);
+        if (want < 0) { PyErr_Clear(); c.ok = false; }
+        PLAIN_OR_NONE(c);
+        at::Tensor token = c.fresh({nb}, at::kInt), prob;
+        if (want) prob = c.fresh({nb}, at::kFloat);
+        const int st = unlocked([&] {
+            return sample_fn(nb, V, code(lg->scalar_type()), one[0], top_k, one[2], one[3], f(each[0]), static_cast<const int32_t *>(each[1]),
+                             f(each[2]), f(each[3]), lp, f(np), static_cast<int32_t *>(token.data_ptr()),
+                             static_cast<float *>(data(prob)), c.stream);
+        });
+        if (st != MB_OK) return PyLong_FromLong(st);
+        PyObject *t = wrap(std::move(token));
+        return want ? tuple({t, wrap(std::move(prob))}) : t;
+    });
+}
+
 // setup(function addresses in the order below, current_device, raw_stream, Parameter)
 PyObject *setup(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
-    constexpr int kFunctions = 17;
+    constexpr int kFunctions = 23;
     ARGS(kFunctions + 3)
     void *at[kFunctions];
     for (int i = 0; i < kFunctions; ++i) {
@@ -605,6 +857,12 @@ PyObject *setup(PyObject *, PyObject *const *a, Py_ssize_t nargs) {
     take(clip_grad_norm_fn);
     take(verify_sample_fn);
     take(verify_sample_workspace_fn);
+    take(rms_norm_fwd_fn);
+    take(rms_norm_bwd_fn);
+    take(rms_norm_bwd_workspace_fn);
+    take(quantize_fp8_fn);
+    take(matmul_fp8_fn);
+    take(sample_fn);
     current_device = same(a[k]);
     raw_stream = same(a[k + 1]);
     parameter_type = same(a[k + 2]);
@@ -616,6 +874,8 @@ PyMethodDef methods[] = {METHOD(setup),  METHOD(scan_step),   METHOD(scan_fwd),
                          METHOD(conv1d), METHOD(conv1d_step), METHOD(verify_rank),
                          METHOD(embedding_fwd), METHOD(embedding_bwd), METHOD(conv1d_bwd),
                          METHOD(grad_norm), METHOD(clip_grad_norm), METHOD(verify_sample),
+                         METHOD(rms_norm_fwd), METHOD(rms_norm_fp8), METHOD(rms_norm_bwd),
+                         METHOD(quantize_fp8), METHOD(matmul_fp8), METHOD(sample),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
