@@ -98,7 +98,6 @@ template <int DT> const void *sample_fn(int64_t vocab, unsigned *threads) {
     *threads = vocab <= 1024 ? 256 : 1024;
     if (vocab <= 1024) return reinterpret_cast<const void *>(&S::sample_rows<DT, 256, 1>);
     if (vocab <= 8192) return reinterpret_cast<const void *>(&S::sample_rows<DT, 1024, 2>);
-    if (vocab <= 32768) return reinterpret_cast<const void *>(&S::sample_rows<DT, 1024, 8>);
     return reinterpret_cast<const void *>(&S::sample_rows<DT, 1024, 0>);
 }
 

@@ -13,9 +13,9 @@
 // counted once more into bins of its own, of ranks.  Weights are summed as integers of 2^-44: sums do not depend
 // on the order of the atomics, and a border does not move from call to call.
 //
-// One workgroup per sequence, the row in registers from one load to the token drawn (up to 65,536 tokens; beyond, it is read
-// again from the cache); random numbers are only read where a token is kept.  Bound by latency and, for large
-// vocabularies, by one CU's instructions: about 30 per token for the weight and its bin.
+// One workgroup per sequence, the row in registers from one load to the token drawn (up to 32,768 tokens; beyond, it is read
+// again from the cache); the kept tokens go to a list, and random numbers are only read for those.  Bound by latency and, for large
+// vocabularies, by one CU's instructions: about 25 per token for the weight and its bin.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -99,29 +99,44 @@ template <class T> __device__ __forceinline__ T wave_running_sum(T v) {
     step(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});   // both into the upper two
     return v;
 }
-__device__ __forceinline__ uint64_t last_lane(uint64_t v) {
-    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), 63) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, 63);
-}
-
 // What is computed of v is computed again from here on: a row's weights, bins and ranks, kept from one reading of it to the
 // next, would not fit the registers.
 template <class V> __device__ __forceinline__ void opaque(V &v) { asm volatile("" : "+v"(v)); }
 __device__ __forceinline__ void opaque(f32x4 (&v)[1]) { asm volatile("" : "+v"(v[0])); }
 
-// T threads, S spans of 4 tokens each in registers (0: the row is read again each time).  Up to 1,024 tokens weights are exponentials in 64
-// bits: a token next to a border is a thousandth of a short row's sum, and an error in 32 bits would move it oftener.
-template <int DT, int T, int S> struct Row {
-    using Weight = std::conditional_t<T == 256, double, float>;
+// T threads, S spans of 4 tokens each in registers (0: the row is read again each time).  W: up to 1,024 tokens weights are exponentials in
+// 64 bits: a token next to a border is a thousandth of a short row's sum, and an error in 32 bits would move it oftener.
+template <int DT, int T, int S, class W> struct Row {
+    using Weight = W;
     const void *logits;
     int64_t at;
     uint32_t vocab;
     float max, inv_temp;
+    float per, per_rest, least;                     // log2 e / T and what it lacks, and the least difference told from others
     Span<DT, 4> s[S > 0 ? S : 1];
+
+    __device__ __forceinline__ void set_temperature(float inv) {
+        const double exact = 1.4426950408889634 * (double)inv;
+        inv_temp = inv;
+        per = __builtin_fminf((float)exact, 3.0e38f);
+        per_rest = exact < 3.0e38 ? (float)(exact - (double)per) : 0.0f;
+        least = -200.0f / per;
+    }
 
     __device__ __forceinline__ static uint32_t first_of(uint32_t k) { return (k * T + threadIdx.x) * 4; }
     __device__ __forceinline__ void load_span(Span<DT, 4> &to, uint32_t y) const {
-        if (y + 4 <= vocab) to.load(logits, at + y);
-        else to.load_first(logits, at + y, y < vocab ? (int)(vocab - y) : 0);
+        if (y + 4 <= vocab) {
+            to.load(logits, at + y);
+            return;
+        }
+        // masked past the row's end
+        const int n = y < vocab ? (int)(vocab - y) : 0;
+        to.load_first(logits, at + y, n);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (DT == 0) to.v[0][i] = i < n ? to.v[0][i] : -__builtin_inff();
+            else to.v[i / 2] |= i < n ? 0u : 0xff80u << 16 * (i % 2);
+        }
     }
     __device__ __forceinline__ void load() {
         if constexpr (S > 0) {
@@ -140,9 +155,37 @@ template <int DT, int T, int S> struct Row {
                 if (S > 2 && k % 2 == 1) __builtin_amdgcn_sched_barrier(0);
             }
         } else {
-            for (uint32_t k = 0; first_of(k) < vocab; ++k) {
-                load_span(s[0], first_of(k));
-                f(first_of(k), s[0]);
+            constexpr int kAhead = 2;
+#pragma unroll 1
+            for (uint32_t k = 0; first_of(k) < vocab; k += kAhead) {
+                Span<DT, 4> some[kAhead];
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) load_span(some[i], first_of(k + i));
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) f(first_of(k + i), some[i]);
+            }
+        }
+    }
+    // f(the first span's number, N spans), for all
+    template <int N, class F> __device__ __forceinline__ void groups(F f) {
+        if constexpr (S > 0) {
+#pragma unroll
+            for (int k = 0; k < S; k += N) {
+                Span<DT, 4> some[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    opaque(s[k + i].v);
+                    some[i] = s[k + i];
+                }
+                f(k, some);
+                if (S > 2) __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {
+            for (uint32_t k = 0; first_of(k) < vocab; k += N) {
+                Span<DT, 4> some[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) load_span(some[i], first_of(k + i));
+                f(k, some);
             }
         }
     }
@@ -152,7 +195,7 @@ template <int DT, int T, int S> struct Row {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float l = v.get(i);
-                if (y + i < vocab && l > -__builtin_inff()) f(y + i, l);
+                if (l > -__builtin_inff()) f(y + i, l);
             }
         });
     }
@@ -160,22 +203,57 @@ template <int DT, int T, int S> struct Row {
         if constexpr (std::is_same_v<Weight, double>) {
             return exp(((double)l - (double)max) * (double)inv_temp);
         } else {
-            // 2^(x log2 e), with what the product's rounding left over as a factor
-            const float x = (l - max) * inv_temp, t = x * kLog2e;
-            const float left = __builtin_fmaf(x, kLog2e, -t) + x * 1.925963033500547e-08f;      // log2 e - kLog2e
-            const float e = hw_exp2(t);
-            return x > -__builtin_inff() ? __builtin_fmaf(e, left * kLn2, e) : 0.0f;
+            // 2^(d log2 e / T), with what the product's rounding left over as a factor; below 2^-200 all is alike
+            const float d = __builtin_fmaxf(l - max, least), t = d * per;
+            const float left = __builtin_fmaf(d, per_rest, __builtin_fmaf(d, per, -t)), e = hw_exp2(t);
+            return __builtin_fmaf(e, left * kLn2, e);
         }
     }
 };
 
+// Bins of equal width from a row's largest logit to its least; halves, so that no difference overflows.
+template <int N> struct Bins {
+    float half_top, per;
+    __device__ __forceinline__ Bins(float top, float low)
+        : half_top(0.5f * top), per(__builtin_fminf((float)(N - 1) / (0.5f * top - 0.5f * low), 3.0e38f)) {}
+    __device__ __forceinline__ uint32_t of(float l) const { return (uint32_t)min((int)((half_top - 0.5f * l) * per), N - 1); }
+};
+
+// The largest logit, the least one that is not -infinity; a row that is no distribution: infinity.
+template <class R> __device__ __forceinline__ float2 wave_tops(R &row, bool ok) {
+    float top = -__builtin_inff(), low = __builtin_inff();
+    bool bad = !ok;
+    row.spans([&](uint32_t, const auto &v) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float l = v.get(i);
+            top = __builtin_fmaxf(top, l);
+            low = __builtin_fminf(low, l > -__builtin_inff() ? l : low);
+            bad |= !(l < __builtin_inff());
+        }
+    });
+    top = wave_max(top);
+    low = -wave_max(-low);
+    return make_float2(__builtin_amdgcn_ballot_w64(bad) ? __builtin_inff() : top, low);
+}
+
 template <int T> struct Shared {
-    static constexpr int kBins = 4 * T, kWaves = T / 64;
-    uint64_t weight[kBins];
-    uint32_t count[kBins];
-    uint64_t list[kList], list_weight[kList];
+    static constexpr int kBins = 4 * T, kWaves = T / 64, kKept = 4 * T;
+    union {
+        struct {
+            uint64_t weight[kBins];
+            uint32_t count[kBins];
+        };
+        struct {
+            uint32_t kept_at[kKept];
+            float kept_logit[kKept];
+        };
+    };
+    uint64_t list[kList], list_weight[kList], higher[kList];
+    uint32_t places[kList], kept;
     uint64_t wave_weight[kWaves], low, high, border, border_sum, found_weight;
-    uint32_t wave_count[kWaves], listed, found_bin, found_count, found_n;
+    uint32_t wave_count[kWaves], listed, found_bin, found_count;
+    uint64_t sums[kWaves];
     float tops[kWaves], lows[kWaves], scores[kWaves];
     int32_t who[kWaves];
     uint32_t bad;
@@ -189,26 +267,14 @@ __global__ __launch_bounds__(T) void sample_rows(Params p) {
     const int64_t b = blockIdx.x;
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const Filter f(p, b);
-    Row<DT, T, S> row;
+    using R = Row<DT, T, S, std::conditional_t<T == 256, double, float>>;
+    R row;
     row.logits = p.logits;
     row.at = b * p.vocab;
     row.vocab = (uint32_t)p.vocab;
-    row.inv_temp = f.inv_temp;
+    row.set_temperature(f.inv_temp);
     row.load();
 
-    // the largest logit, the least one that is not -infinity, and whether the row is a distribution
-    float top = -__builtin_inff(), low = __builtin_inff();
-    bool bad = !f.ok;
-    row.spans([&](uint32_t y, const Span<DT, 4> &v) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float l = v.get(i);
-            const bool in = y + i < row.vocab;
-            top = __builtin_fmaxf(top, in ? l : top);
-            low = __builtin_fminf(low, in && l > -__builtin_inff() ? l : low);
-            bad |= in && !(l < __builtin_inff());
-        }
-    });
     auto clear = [&] {
 #pragma unroll
         for (int i = 0; i < kBins / T; ++i) {
@@ -216,20 +282,19 @@ __global__ __launch_bounds__(T) void sample_rows(Params p) {
             sh.count[i * T + t] = 0;
         }
     };
-    top = wave_max(top);
-    low = -wave_max(-low);
-    bad = __builtin_amdgcn_ballot_w64(bad) != 0;
+    float2 ends = wave_tops(row, f.ok);
     if (lane == 0) {
-        sh.tops[wave] = bad ? __builtin_inff() : top;
-        sh.lows[wave] = low;
+        sh.tops[wave] = ends.x;
+        sh.lows[wave] = ends.y;
     }
-    clear();
+    if (t == 0) sh.kept = 0;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-        top = __builtin_fmaxf(top, sh.tops[w]);
-        low = __builtin_fminf(low, sh.lows[w]);
+        ends.x = __builtin_fmaxf(ends.x, sh.tops[w]);
+        ends.y = __builtin_fminf(ends.y, sh.lows[w]);
     }
+    const float top = ends.x;
     row.max = top;
     if (!(top < __builtin_inff()) || top == -__builtin_inff()) {            // the same in every thread
         if (t == 0) {
@@ -239,171 +304,161 @@ __global__ __launch_bounds__(T) void sample_rows(Params p) {
         return;
     }
 
-    uint64_t border = 0;                            // the least rank kept
+    uint64_t border = 0;                            // the least rank kept; 0: all are
     const bool by_count = f.top_k < row.vocab, by_weight = f.top_p < 1.0f;
     if (by_count || by_weight) {
-        // bins of equal width from the largest logit to the least; halves, so that no difference overflows
-        const float half_top = 0.5f * top, width = half_top - 0.5f * low;
-        const float per = __builtin_fminf((float)(kBins - 1) / width, 3.0e38f);
-        auto bin_of = [&](float l) { return (uint32_t)min((int)((half_top - 0.5f * l) * per), kBins - 1); };
-        auto count_all = [&] {
-            row.each([&](uint32_t, float l) {
-                const uint32_t at = bin_of(l);
-                atomicAdd(&sh.count[at], 1u);
-                if (by_weight) atomicAdd(reinterpret_cast<unsigned long long *>(&sh.weight[at]), (unsigned long long)units_of(row.weight(l)));
-            });
+        const Bins<kBins> bins(top, ends.y);
+        // What the filter at hand narrows the row down to: tokens of one bin of logits, then (fine) of bins of ranks.
+        bool fine = false;
+        uint32_t bin = 0, shift = 0;
+        uint64_t low_rank = 0, high_rank = 0;
+        auto inside = [&](uint32_t y, float l) {
+            if (!fine) return bins.of(l) == bin;
+            const uint64_t rank = rank_of(l, y);
+            return rank >= low_rank && rank <= high_rank && (high_rank - rank) >> shift == bin;
         };
-        // what lies before this thread's bins, and in all
-        uint32_t before_count = 0;
-        uint64_t before_weight = 0, all_weight = 0;
-        auto run = [&] {
-            uint32_t c = 0;
-            uint64_t w = 0;
-#pragma unroll
-            for (int i = 0; i < kBins / T; ++i) {
-                c += sh.count[t * (kBins / T) + i];
-                w += sh.weight[t * (kBins / T) + i];
-            }
-            const uint32_t rc = wave_running_sum(c);
-            const uint64_t rw = wave_running_sum(w);
-            if (lane == 63) {
-                sh.wave_count[wave] = rc;
-                sh.wave_weight[wave] = rw;
-            }
-            __syncthreads();
-            before_count = rc - c;
-            before_weight = rw - w;
-            all_weight = 0;
-#pragma unroll
-            for (int i = 0; i < kWaves; ++i) {
-                if (i < wave) {
-                    before_count += sh.wave_count[i];
-                    before_weight += sh.wave_weight[i];
+        uint64_t sum = 0;                           // of the weights that top-k leaves
+        bool counted = false;                       // the row's bins are there
+        // top-k first (weighs = 0: so many tokens are wanted), then top-p (1: so much of their weight)
+#pragma unroll 1
+        for (int weighs = by_count ? 0 : 1; weighs < (by_weight ? 2 : 1); ++weighs) {
+            uint64_t wanted = f.top_k, above = 0;
+            fine = false;
+#pragma unroll 1
+            for (bool whole = true;; whole = false) {
+                // tokens and weights of each bin: of the whole row, or of a bin's ranks
+                if (!whole || !counted) {
+                    clear();
+                    __syncthreads();
+                    row.each([&](uint32_t y, float l) {
+                        uint32_t to;
+                        if (whole) {
+                            to = bins.of(l);
+                        } else {
+                            const uint64_t rank = rank_of(l, y);
+                            if (rank < low_rank || rank > high_rank) return;
+                            to = (uint32_t)((high_rank - rank) >> shift);
+                        }
+                        if (by_count) atomicAdd(&sh.count[to], 1u);
+                        if (by_weight) atomicAdd(reinterpret_cast<unsigned long long *>(&sh.weight[to]), (unsigned long long)units_of(row.weight(l)));
+                    });
+                    counted = whole;
                 }
-                all_weight += sh.wave_weight[i];
-            }
-        };
-        // the bin in which `wanted` tokens, or that much of their weight, are reached
-        auto find = [&](bool weighs, uint64_t wanted) {
-            uint32_t c = before_count;
-            uint64_t w = before_weight;
+                __syncthreads();
+                // running sums over the bins: a thread's own, its wave's, the waves'
+                constexpr int kOwn = kBins / T;
+                uint32_t c = 0;
+                uint64_t w = 0;
 #pragma unroll
-            for (int i = 0; i < kBins / T; ++i) {
-                const uint32_t at = t * (kBins / T) + i, n = sh.count[at];
-                const uint64_t m = sh.weight[at];
-                if (weighs ? w < wanted && w + m >= wanted : c < wanted && c + n >= wanted) {
-                    sh.found_bin = at;
-                    sh.found_n = n;
-                    sh.found_count = c;
-                    sh.found_weight = w;
+                for (int i = 0; i < kOwn; ++i) {
+                    c += sh.count[t * kOwn + i];
+                    w += sh.weight[t * kOwn + i];
                 }
-                c += n;
-                w += m;
-            }
-            if (t == 0) {
-                sh.listed = 0;
-                sh.low = ~0ull;
-                sh.high = 0;
-                sh.border = 0;
-            }
-            __syncthreads();
-        };
-        // The least rank of those that reach `wanted`; what the ranks down to it weigh is left in border_sum.
-        bool counted_anew = false;
-        auto settle = [&](bool weighs, uint64_t wanted) {
-            if (t == 0) sh.found_n = 0;
-            __syncthreads();
-            find(weighs, wanted);
-            uint64_t low_rank = 0, high_rank = 0, above = 0;
-            uint32_t bin = sh.found_bin, n = sh.found_n, shift = 0;
-            if (n == 0) return (uint64_t)0;         // fewer tokens than top-k wants: all
-            bool fine = false;
-            wanted -= weighs ? sh.found_weight : sh.found_count;
-            above += sh.found_weight;
-            auto inside = [&](float l, uint64_t rank) {
-                return fine ? rank >= low_rank && rank <= high_rank && (high_rank - rank) >> shift == bin : bin_of(l) == bin;
-            };
-            while (n > kList) {
+                const uint32_t run_c = wave_running_sum(c);
+                const uint64_t run_w = wave_running_sum(w);
+                if (lane == 63) {
+                    sh.wave_count[wave] = run_c;
+                    sh.wave_weight[wave] = run_w;
+                }
+                if (t == 0) {
+                    sh.found_bin = kBins;
+                    sh.listed = 0;
+                    sh.low = ~0ull;
+                    sh.high = 0;
+                    sh.border = 0;
+                }
+                if (t < kList) {
+                    sh.places[t] = 0;
+                    sh.higher[t] = 0;
+                }
+                __syncthreads();
+                c = run_c - c;
+                w = run_w - w;
+                uint64_t all = 0;
+                for (int i = 0; i < kWaves; ++i) {
+                    if (i < wave) {
+                        c += sh.wave_count[i];
+                        w += sh.wave_weight[i];
+                    }
+                    all += sh.wave_weight[i];
+                }
+                if (whole && weighs) {
+                    if (!by_count || border == 0) sum = all;
+                    // the first that reaches it is the last one kept; sums are whole numbers, and 1 keeps the first alone
+                    const double share = ceil((double)f.top_p * (double)sum);
+                    wanted = share > 1.0 ? (uint64_t)share : 1;
+                }
+                // the bin in which what is wanted is reached
+#pragma unroll
+                for (int i = 0; i < kOwn; ++i) {
+                    const uint32_t n = sh.count[t * kOwn + i];
+                    const uint64_t m = sh.weight[t * kOwn + i];
+                    if (weighs ? w < wanted && w + m >= wanted : c < wanted && c + n >= wanted) {
+                        sh.found_bin = t * kOwn + i;
+                        sh.found_count = c;
+                        sh.found_weight = w;
+                    }
+                    c += n;
+                    w += m;
+                }
+                __syncthreads();
+                bin = sh.found_bin;
+                if (bin == kBins) break;            // fewer tokens than top-k wants: all
+                wanted -= weighs ? sh.found_weight : sh.found_count;
+                above += sh.found_weight;
+                // its tokens
                 uint64_t least = ~0ull, most = 0;
                 row.each([&](uint32_t y, float l) {
+                    if (!inside(y, l)) return;
                     const uint64_t rank = rank_of(l, y);
-                    if (inside(l, rank)) {
-                        least = rank < least ? rank : least;
-                        most = rank > most ? rank : most;
-                    }
+                    least = rank < least ? rank : least;
+                    most = rank > most ? rank : most;
+                    const uint32_t at = atomicAdd(&sh.listed, 1u);
+                    if (at >= kList) return;
+                    sh.list[at] = rank;
+                    sh.list_weight[at] = by_weight ? units_of(row.weight(l)) : 0;
                 });
                 if (most) {
                     atomicMin(reinterpret_cast<unsigned long long *>(&sh.low), (unsigned long long)least);
                     atomicMax(reinterpret_cast<unsigned long long *>(&sh.high), (unsigned long long)most);
                 }
-                clear();
                 __syncthreads();
-                low_rank = sh.low;
-                high_rank = sh.high;
-                shift = (uint32_t)max(0, 64 - __builtin_clzll((high_rank - low_rank) | 1) - (31 - __builtin_clz(kBins)));
-                fine = counted_anew = true;
-                row.each([&](uint32_t y, float l) {
-                    const uint64_t rank = rank_of(l, y);
-                    if (rank < low_rank || rank > high_rank) return;
-                    const uint32_t to = (uint32_t)((high_rank - rank) >> shift);
-                    atomicAdd(&sh.count[to], 1u);
-                    if (by_weight) atomicAdd(reinterpret_cast<unsigned long long *>(&sh.weight[to]), (unsigned long long)units_of(row.weight(l)));
-                });
-                __syncthreads();
-                run();
-                find(weighs, wanted);
-                bin = sh.found_bin;
-                n = sh.found_n;
-                wanted -= weighs ? sh.found_weight : sh.found_count;
-                above += sh.found_weight;
-            }
-            row.each([&](uint32_t y, float l) {
-                const uint64_t rank = rank_of(l, y);
-                if (!inside(l, rank)) return;
-                const uint32_t at = atomicAdd(&sh.listed, 1u);
-                sh.list[at] = rank;
-                sh.list_weight[at] = by_weight ? units_of(row.weight(l)) : 0;
-            });
-            __syncthreads();
-            if (wave == 0) {
-                const uint64_t mine = lane < n ? sh.list[lane] : 0, weighs_mine = lane < n ? sh.list_weight[lane] : 0;
+                const uint32_t n = sh.listed;
+                if (n > kList) {                    // too many to rank one by one
+                    low_rank = sh.low;
+                    high_rank = sh.high;
+                    shift = (uint32_t)max(0, 64 - __builtin_clzll((high_rank - low_rank) | 1) - (31 - __builtin_clz(kBins)));
+                    fine = true;
+                    continue;
+                }
+                // each token of the list against every kWaves-th of them, wave by wave
+                const uint64_t mine = lane < n ? sh.list[lane] : 0;
                 uint64_t higher = 0;
                 uint32_t places = 0;
-                for (uint32_t i = 0; i < n; ++i) {
-                    const uint64_t other = sh.list[i];
-                    if (other > mine) {
+                for (uint32_t i = wave; i < n; i += kWaves)
+                    if (sh.list[i] > mine) {
                         ++places;
                         higher += sh.list_weight[i];
                     }
+                if (places) {
+                    atomicAdd(&sh.places[lane], places);
+                    atomicAdd(reinterpret_cast<unsigned long long *>(&sh.higher[lane]), (unsigned long long)higher);
                 }
-                if (lane < n && (weighs ? higher < wanted && higher + weighs_mine >= wanted : places == wanted - 1)) {
-                    sh.border = mine;
-                    sh.border_sum = above + higher + weighs_mine;
+                __syncthreads();
+                if (wave == 0 && lane < n) {
+                    places = sh.places[lane];
+                    higher = sh.higher[lane];
+                    const uint64_t weighs_mine = sh.list_weight[lane];
+                    if (weighs ? higher < wanted && higher + weighs_mine >= wanted : places == wanted - 1) {
+                        sh.border = mine;
+                        sh.border_sum = above + higher + weighs_mine;
+                    }
                 }
-            }
-            __syncthreads();
-            return sh.border;
-        };
-        count_all();
-        __syncthreads();
-        run();
-        uint64_t sum = all_weight;
-        if (by_count) {
-            border = settle(false, f.top_k);
-            if (border) sum = sh.border_sum;
-        }
-        if (by_weight) {
-            if (counted_anew) {
-                clear();
                 __syncthreads();
-                count_all();
-                __syncthreads();
-                run();
+                border = sh.border > border ? sh.border : border;
+                sum = sh.border_sum;
+                break;
             }
-            // the first that reaches it is the last one kept; sums are whole numbers, and 1 keeps the first alone
-            const double wanted = ceil((double)f.top_p * (double)sum);
-            const uint64_t lowest = settle(true, wanted > 1.0 ? (uint64_t)wanted : 1);
-            border = lowest > border ? lowest : border;
         }
     }
 
@@ -411,45 +466,71 @@ __global__ __launch_bounds__(T) void sample_rows(Params p) {
     float best = 0.0f;
     int32_t at = kNobody;
     uint64_t sum = 0;
-    auto kept = [&](uint32_t y, float l, typename Row<DT, T, S>::Weight &e) {
-        if (y >= row.vocab || !(l > -__builtin_inff()) || rank_of(l, y) < border) return false;
-        e = row.weight(l);
-        return e > 0 && e >= f.min_p;
-    };
-    row.spans([&](uint32_t y, const Span<DT, 4> &v) {
-        typename Row<DT, T, S>::Weight e[4];
-        bool in[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) in[i] = kept(y + i, v.get(i), e[i]);
-        if (!(in[0] || in[1] || in[2] || in[3])) return;
-        float noise[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) noise[i] = in[i] && !f.greedy ? p.noise[row.at + y + i] : 1.0f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (!in[i]) continue;
-            sum += units_of(e[i]);
-            const float s = (float)e[i] / noise[i];
-            if (s > best) {
-                best = s;
-                at = (int32_t)(y + i);
-            }
+    // the border as a logit and the last index that is kept of it
+    const uint32_t border_bits = (uint32_t)(border >> 32), border_at = ~(uint32_t)border;
+    const float border_logit = border ? __uint_as_float(border_bits & 0x80000000u ? border_bits & 0x7fffffffu : ~border_bits) : -__builtin_inff();
+    auto kept = [&](uint32_t y, float l) { return l > border_logit || (l == border_logit && border && y <= border_at); };
+    auto run_race = [&](uint32_t y, float l, float noise) {
+        const typename R::Weight e = row.weight(l);
+        if (!(e > 0 && e >= f.min_p)) return;
+        sum += units_of(e);
+        const float s = (float)e * hw_rcp(noise);
+        if (s > best || (s == best && s > 0.0f && (int32_t)y < at)) {
+            best = s;
+            at = (int32_t)y;
         }
-    });
+    };
+    // with a border, the kept in a list where it has room for them: few threads' work instead of everyone's
+    bool listed = false;
+    if (border) {
+        __syncthreads();
+        row.each([&](uint32_t y, float l) {
+            if (!kept(y, l)) return;
+            const uint32_t to = atomicAdd(&sh.kept, 1u);
+            if (to >= Sh::kKept) return;
+            sh.kept_at[to] = y;
+            sh.kept_logit[to] = l;
+        });
+        __syncthreads();
+        listed = sh.kept <= Sh::kKept;
+        for (uint32_t i = t; listed && i < sh.kept; i += T) {
+            const uint32_t y = sh.kept_at[i];
+            run_race(y, sh.kept_logit[i], f.greedy ? 1.0f : p.noise[row.at + y]);
+        }
+    }
+    // kSide spans side by side, so that their random numbers are asked for together
+    constexpr int kSide = S > 0 ? S : 2;
+    auto race = [&](uint32_t first, const Span<DT, 4> (&v)[kSide]) {
+        Span<0, 4> noise[kSide];
+#pragma unroll
+        for (int k = 0; k < kSide; ++k) {
+            const uint32_t y = row.first_of(first + k);
+            if (y + 4 <= row.vocab) noise[k].load(p.noise, row.at + y);
+            else noise[k].load_first(p.noise, row.at + y, y < row.vocab ? (int)(row.vocab - y) : 0);
+        }
+#pragma unroll
+        for (int k = 0; k < kSide; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t y = row.first_of(first + k) + i;
+                if (kept(y, v[k].get(i))) run_race(y, v[k].get(i), f.greedy ? 1.0f : noise[k].get(i));
+            }
+    };
+    if (!listed) row.template groups<kSide>(race);
     const float won = wave_max(best);
     at = wave_min(best == won && at != kNobody ? at : kNobody);
     best = won;
-    sum = last_lane(wave_running_sum(sum));
+    for (int m = 1; m < 64; m *= 2) sum += __shfl_xor(sum, m);              // whole numbers: the list's order does not show
     __syncthreads();
     if (lane == 0) {
         sh.scores[wave] = won;
         sh.who[wave] = at;
-        sh.wave_weight[wave] = sum;
+        sh.sums[wave] = sum;
     }
     __syncthreads();
     if (t == 0) {
         for (int w = 1; w < kWaves; ++w) {
-            sum += sh.wave_weight[w];
+            sum += sh.sums[w];
             if (sh.who[w] != kNobody && (at == kNobody || sh.scores[w] > best || (sh.scores[w] == best && sh.who[w] < at))) {
                 best = sh.scores[w];
                 at = sh.who[w];
