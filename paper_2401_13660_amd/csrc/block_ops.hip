@@ -116,6 +116,13 @@ struct MatmulPlan {
         else if (d->b_tile) tiles<OUT, 2, WM, WN, MI>();
         else tiles<OUT, 0, WM, WN, MI>();
     }
+    void large(const mb_matmul_desc *d) {
+        namespace M = mbs::matmul;
+        fn = d->a_tile   ? reinterpret_cast<const void *>(&M::matmul_large<1>)
+             : d->b_tile ? reinterpret_cast<const void *>(&M::matmul_large<2>)
+                         : reinterpret_cast<const void *>(&M::matmul_large<0>);
+        tile_m = tile_n = 256; threads = 512;
+    }
     template <int OUT, int MI, int NJ> void split() {
         fn = reinterpret_cast<const void *>(&mbs::matmul::matmul_split<OUT, MI, NJ>);
         tile_m = 16 * MI; tile_n = 16 * NJ; threads = 64 * mbs::matmul::kSplit;
@@ -130,7 +137,7 @@ struct MatmulPlan {
         else if (!whole) {
             fn = reinterpret_cast<const void *>(&mbs::matmul::matmul_any<OUT>);
             tile_m = tile_n = mbs::matmul::kAnyTile; threads = mbs::matmul::kAnyThreads;
-        } else if (t256 >= 256) tiles<OUT, 2, 4, 8>(d);
+        } else if (OUT == 1 && t256 >= 256) large(d);
         else tiles<OUT, 2, 2, 4>(d);
     }
     MatmulPlan(const mb_matmul_desc *d, const mbs::matmul::Params &p, const void *a, const void *b) {

@@ -11,9 +11,9 @@
 // instruction, at half the rate, sums in fp32.  Scaling and the sum over blocks are fp32 in both, with one rounding to C's type.
 //
 // The instruction is given b's rows as its first operand: a lane then holds 4 neighbouring columns of one row of C.  Which 16
-// of a wave's 64 columns make an instruction's is free, and they are taken 4 by 4 from each quarter, so that a lane's 4
-// results are 16 neighbouring columns and the 64 lanes store whole 128-byte lines.  Along the block any order is right that both
-// operands share.
+// of a wave's 64 columns make an instruction's is free, and they are taken so that two instructions' results are 8
+// neighbouring columns of a lane and 32 of four lanes: 64 bytes of a row of C to a store.  Along the block any order is right that
+// both operands share.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -74,13 +74,16 @@ __device__ __forceinline__ u32x4 load16(const uint8_t *p, int64_t left) {
 }
 
 // Rows of 128 bytes in LDS as 8 pieces of 16.  16 lanes read a piece each of 16 rows at once, served from 256 bytes' worth of banks: a
-// row's pieces are permuted so that those 16 lie in different ones.  Of a the 16 rows are neighbours, of b 4 by 4.
+// row's pieces are permuted so that those 16 lie in different ones.  Of a the 16 rows are neighbours, of b every other 4.
 __device__ __forceinline__ int a_place(int row, int piece) { return row * kBlock + 16 * (piece ^ ((row >> 1) & 7)); }
+__device__ __forceinline__ int b_turn(int row) { return ((row >> 1) & 1) | ((row >> 2) & 6); }
 __device__ __forceinline__ int b_place(int row, int piece) {
-    return row * kBlock + 16 * (piece ^ (((row >> 1) & 1) | ((row >> 3) & 6)));
+    return row * kBlock + 16 * (piece ^ b_turn(row));
 }
-// The row of b that lane l (of 16) of column tile j reads.
-__device__ __forceinline__ int b_row(int j, int l) { return (l >> 2) * 16 + 4 * j + (l & 3); }
+// Where instruction j's columns lie among a wave's 64: the row of b that lane l (of 16) reads, and the first of the 4 columns of C that a lane
+// of group g has of it.
+__device__ __forceinline__ int b_row(int j, int l) { return (j >> 1) * 32 + (l >> 2) * 8 + (j & 1) * 4 + (l & 3); }
+__device__ __forceinline__ int c_column(int j, int g) { return (j >> 1) * 32 + g * 8 + (j & 1) * 4; }
 
 __device__ __forceinline__ i32x8 join(u32x4 x, u32x4 y) {
     return i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], (int)y[2], (int)y[3]};
@@ -90,19 +93,15 @@ __device__ __forceinline__ i32x8 two_pieces(const uint8_t *lds, int first, int s
     return join(*reinterpret_cast<const u32x4 *>(lds + first), *reinterpret_cast<const u32x4 *>(lds + second));
 }
 
-// 16 neighbouring columns of a row of C, the first n of them.
-template <int OUT> __device__ __forceinline__ void store_columns(void *c, int64_t at, const f32x4 (&v)[4], int64_t n) {
-    if (n >= 16) {
+// A lane's columns of a wave's 64, twice 8 neighbouring ones, of which n from the wave's first on are C's.
+template <int OUT> __device__ __forceinline__ void store_columns(void *c, int64_t at, int g, const f32x4 (&v)[4], int64_t n) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const float s[8] = {v[2 * h][0], v[2 * h][1], v[2 * h][2], v[2 * h][3],
-                                v[2 * h + 1][0], v[2 * h + 1][1], v[2 * h + 1][2], v[2 * h + 1][3]};
-            store_span<OUT, 8>(c, at + 8 * h, s);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (i < n) st_out<OUT>(c, at + i, v[i / 4][i % 4]);
+    for (int h = 0; h < 2; ++h) {
+        const int column = c_column(2 * h, g);
+        const float s[8] = {v[2 * h][0], v[2 * h][1], v[2 * h][2], v[2 * h][3],
+                            v[2 * h + 1][0], v[2 * h + 1][1], v[2 * h + 1][2], v[2 * h + 1][3]};
+        if (column + 8 <= n) store_span<OUT, 8>(c, at + column, s);
+        else store_first<OUT, 8>(c, at + column, s, (int)max(n - column, (int64_t)0));
     }
 }
 
@@ -141,51 +140,71 @@ __device__ __forceinline__ void load_to_lds(const float *from, float *lds) {
     __builtin_amdgcn_global_load_lds(const_cast<float *>(from), (lds_void *)lds, 4, 0, 0);
 }
 
+// A workgroup's tile, and what each thread brings of its blocks.
+template <class S> struct TileLoads {
+    static constexpr int kScales = (S::kM + S::kN + S::kThreads - 1) / S::kThreads;
+    const uint8_t *a, *b;
+    int bytes_a, bytes_b, K, wave, row, piece_a, piece_b;
+    const float *scale_at[kScales];
+    __device__ __forceinline__ TileLoads(const Params &p, const Tile &tile, int64_t m0, int64_t n0) {
+        const int t = threadIdx.x;
+        K = (int)p.k;
+        a = p.a + tile.z * p.a_step + m0 * p.k;
+        b = p.b + tile.z * p.b_step + n0 * p.k;
+        bytes_a = (int)min((int64_t)S::kM, p.m - m0) * K;
+        bytes_b = (int)min((int64_t)S::kN, p.n - n0) * K;
+        wave = __builtin_amdgcn_readfirstlane(t >> 6);
+        // a piece of row t / 8 and of every kStep-th from there on, and one row's scale (or two)
+        row = t / 8;
+        piece_a = 16 * ((t & 7) ^ ((row >> 1) & 7));
+        piece_b = 16 * ((t & 7) ^ b_turn(row));
+        const float *as = p.as + tile.z * p.as_step, *bs = p.bs + tile.z * p.bs_step;
+#pragma unroll
+        for (int i = 0; i < kScales; ++i) {
+            const int at = i * S::kThreads + t;
+            scale_at[i] = at < S::kM ? as + (min(m0 + at, p.m - 1) >> p.a_shift) * p.blocks
+                                     : bs + (min(n0 + min(at - S::kM, S::kN - 1), p.n - 1) >> p.b_shift) * p.blocks;
+        }
+    }
+    __device__ __forceinline__ void fetch(uint8_t *la, uint8_t *lb, float *ls, int kb) const {
+        // 2^31 and more (a tile has less than 2^30 bytes) lies past every buffer
+        const int k = kb * kBlock;
+        const uint32_t oa = k + piece_a < K ? row * K + piece_a : 0x80000000u, ob = k + piece_b < K ? row * K + piece_b : 0x80000000u;
+#pragma unroll
+        for (int i = 0; i < S::kM / S::kStep; ++i)
+            load_to_lds(a, bytes_a, la + i * S::kStep * kBlock + wave * 1024, oa + i * S::kStep * K, k);
+#pragma unroll
+        for (int i = 0; i < S::kN / S::kStep; ++i)
+            load_to_lds(b, bytes_b, lb + i * S::kStep * kBlock + wave * 1024, ob + i * S::kStep * K, k);
+#pragma unroll
+        for (int i = 0; i < kScales; ++i)
+            if ((i + 1) * S::kThreads <= S::kM + S::kN || i * S::kThreads + wave * 64 < S::kM + S::kN)
+                load_to_lds(scale_at[i] + kb, ls + i * S::kThreads + wave * 64);
+    }
+};
+
+// A wave's results: 16 MI rows by 64 columns from (m, n) on.
+template <int OUT, int MI> __device__ __forceinline__ void store_tile(const Params &p, uint32_t z, int64_t m, int64_t n, const f32x4 (&acc)[MI][4]) {
+    const int lane = threadIdx.x & 63, g = lane >> 4;
+    const int64_t first = m + (lane & 15), at = ((int64_t)z * p.m + first) * p.n + n;
+    // where the tile is whole no branch lies between the stores
+    const bool whole = m + 16 * MI <= p.m && n + 64 <= p.n;
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+        if (whole || first + 16 * i < p.m) store_columns<OUT>(p.c, at + 16 * i * p.n, g, acc[i], whole ? 64 : p.n - n);
+}
+
 template <int OUT, int ONE, int WM, int WN, int MI>
 __global__ __launch_bounds__(64 * WM * WN) void matmul_tiles(Params p) {
     using S = Shape<WM, WN, MI>;
     __shared__ __align__(128) uint8_t la0[S::kM * kBlock], lb0[S::kN * kBlock], la1[S::kM * kBlock], lb1[S::kN * kBlock];
     __shared__ __align__(16) float ls0[S::kM + S::kN], ls1[S::kM + S::kN];
-    const int t = threadIdx.x, lane = t & 63, l16 = lane & 15, g = lane >> 4;
-    const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
     const Tile tile = tile_of(p);
     const int64_t m0 = (int64_t)tile.m * S::kM, n0 = (int64_t)tile.n * S::kN;
-    const int wm = wave % WM * 16 * MI, wn = wave / WM * 64;
-    const int rows_a = (int)min((int64_t)S::kM, p.m - m0), rows_b = (int)min((int64_t)S::kN, p.n - n0);
-    const int K = (int)p.k;
-    const uint8_t *a = p.a + tile.z * p.a_step + m0 * p.k, *b = p.b + tile.z * p.b_step + n0 * p.k;
-    const float *as = p.as + tile.z * p.as_step, *bs = p.bs + tile.z * p.bs_step;
-
-    // what a thread loads: a piece of row t / 8 and of every kStep-th from there on, and one row's scale (or two)
-    const int row = t / 8;
-    const int piece_a = 16 * ((t & 7) ^ ((row >> 1) & 7)), piece_b = 16 * ((t & 7) ^ (((row >> 1) & 1) | ((row >> 3) & 6)));
-    const int va = row * K + piece_a;
-    constexpr int kScales = (S::kM + S::kN + S::kThreads - 1) / S::kThreads;
-    const float *scale_at[kScales];
-#pragma unroll
-    for (int i = 0; i < kScales; ++i) {
-        const int at = i * S::kThreads + t;
-        scale_at[i] = at < S::kM ? as + (min(m0 + at, p.m - 1) >> p.a_shift) * p.blocks
-                                 : bs + (min(n0 + min(at - S::kM, S::kN - 1), p.n - 1) >> p.b_shift) * p.blocks;
-    }
-    auto fetch = [&](uint8_t *la, uint8_t *lb, float *ls, int kb) {
-        // 2^31 and more (a tile has less than 2^30 bytes) lies past every buffer
-        const int k = kb * kBlock;
-        const uint32_t oa = k + piece_a < K ? va : 0x80000000u;
-#pragma unroll
-        for (int i = 0; i < S::kM / S::kStep; ++i)
-            load_to_lds(a, rows_a * K, la + i * S::kStep * kBlock + wave * 1024, oa + i * S::kStep * K, k);
-#pragma unroll
-        for (int i = 0; i < S::kN / S::kStep; ++i) {
-            const int turn = i * S::kStep & 32 ? 64 : 0;            // bit 5 of b's row is in its pieces' permutation
-            const uint32_t ob = k + (piece_b ^ turn) < K ? row * K + (piece_b ^ turn) : 0x80000000u;
-            load_to_lds(b, rows_b * K, lb + i * S::kStep * kBlock + wave * 1024, ob + i * S::kStep * K, k);
-        }
-#pragma unroll
-        for (int i = 0; i < kScales; ++i)
-            if ((i + 1) * S::kThreads <= S::kM + S::kN || i * S::kThreads + wave * 64 < S::kM + S::kN)
-                load_to_lds(scale_at[i] + kb, ls + i * S::kThreads + wave * 64);
-    };
+    const TileLoads<S> loads(p, tile, m0, n0);
+    const int wm = loads.wave % WM * 16 * MI, wn = loads.wave / WM * 64;
+    auto fetch = [&](uint8_t *la, uint8_t *lb, float *ls, int kb) { loads.fetch(la, lb, ls, kb); };
 
     // a wave's rows begin at multiples of 16 and of 64: the pieces' permutations are the same for every i and j
     const int pa = wm * kBlock + a_place(l16, g), pb = wn * kBlock + b_place(b_row(0, l16), g);
@@ -199,8 +218,8 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_tiles(Params p) {
         if constexpr (ONE == 2) one = lsb[0];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            fb[j] = two_pieces(lb + 4 * j * kBlock, pb, pb ^ 64);
-            if constexpr (ONE != 2) sb[j] = *reinterpret_cast<const f32x4 *>(lsb + 16 * g + 4 * j) * one;
+            fb[j] = two_pieces(lb + b_row(j, 0) * kBlock, pb, pb ^ 64);
+            if constexpr (ONE != 2) sb[j] = *reinterpret_cast<const f32x4 *>(lsb + c_column(j, g)) * one;
         }
         i32x8 fa = two_pieces(la, pa, pa ^ 64);
 #pragma unroll
@@ -237,11 +256,114 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_tiles(Params p) {
         if (kb + 2 < p.blocks) fetch(la0, lb0, ls0, kb + 2);
         if (kb + 1 < p.blocks) products(la1, lb1, ls1);
     }
+    store_tile<OUT>(p, tile.z, m0 + wm, n0 + wn, acc);
+}
+
+// All waves of the workgroup are here, and what each has read of LDS is in its registers.
+__device__ __forceinline__ void meet() { asm volatile("s_waitcnt lgkmcnt(0)\ns_barrier" ::: "memory"); }
+// What this wave asked of memory is in LDS.
+__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// Tiles of 256 x 256 by 8 waves, two to a SIMD.  In matmul_tiles all waves read their operands after the same barrier and then all
+// multiply; here the waves of one half are a turn behind the other's, so that on each SIMD one multiplies while the other reads.
+// A block is four turns: read b's rows and half of a's, multiply, read the other half of a's, multiply.
+//
+//   turn         4 kb          4 kb + 1      4 kb + 2      4 kb + 3      4 kb + 4
+//   first half   read, ask     multiply      read          multiply *    read, ask
+//   second       multiply      read, ask     multiply      read *        multiply
+//
+// "ask" lets the next block's rows begin to arrive in the other buffer, whose last reader was the second half's read a turn before the
+// first half asks; at * each wave waits for its own, so that they are there in the next turn, when the first half reads them.
+// For a C of 16 bits (widened operands do not fit beside 128 sums).
+template <int ONE>
+__global__ __launch_bounds__(512) void matmul_large(Params p) {
+    constexpr int MI = 8, kHalf = MI / 2;
+    using S = Shape<2, 4, MI>;
+    __shared__ __align__(128) uint8_t la0[S::kM * kBlock], lb0[S::kN * kBlock], la1[S::kM * kBlock], lb1[S::kN * kBlock];
+    __shared__ __align__(16) float ls0[S::kM + S::kN], ls1[S::kM + S::kN];
+    const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
+    const Tile tile = tile_of(p);
+    const int64_t m0 = (int64_t)tile.m * S::kM, n0 = (int64_t)tile.n * S::kN;
+    const TileLoads<S> loads(p, tile, m0, n0);
+    const int wm = loads.wave % 2 * 16 * MI, wn = loads.wave / 2 * 64;
+    const bool second = loads.wave >= 4;                // waves w and w + 4 share a SIMD
+    // a wave's rows begin at multiples of 16 and of 64: the pieces' permutations are the same for every i and j
+    const int pa = wm * kBlock + a_place(l16, g), pb = wn * kBlock + b_place(b_row(0, l16), g);
+    f32x4 acc[MI][4] = {};
+    i32x8 fb[4], fa[kHalf];
+    f32x4 sb[4];
+    float sa[kHalf], one = 1.0f;
+    auto read_a = [&](const uint8_t *la, const float *ls, int first) {
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
-        const int64_t m = m0 + wm + 16 * i + l16, n = n0 + wn + 16 * g;
-        if (m < p.m && n < p.n) store_columns<OUT>(p.c, ((int64_t)tile.z * p.m + m) * p.n + n, acc[i], p.n - n);
+        for (int i = 0; i < kHalf; ++i) {
+            fa[i] = two_pieces(la + 16 * (first + i) * kBlock, pa, pa ^ 64);
+            if constexpr (ONE != 1) sa[i] = ls[wm + 16 * (first + i) + l16] * one;
+        }
+    };
+    auto read_b = [&](const uint8_t *lb, const float *ls) {
+        if constexpr (ONE == 1) one = ls[wm];
+        if constexpr (ONE == 2) one = ls[S::kM + wn];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            fb[j] = two_pieces(lb + b_row(j, 0) * kBlock, pb, pb ^ 64);
+            if constexpr (ONE != 2) sb[j] = *reinterpret_cast<const f32x4 *>(ls + S::kM + wn + c_column(j, g));
+            if constexpr (ONE == 1) sb[j] *= one;
+        }
+    };
+    // Product after product, each one's scaling two products later, when it is done: between them the matrix unit never waits.  The last two are
+    // scaled in the next turn.
+    f32x4 d[3];
+    auto add = [&](int first, int n) {
+        f32x4 &to = acc[first + n / 4][n % 4];
+        const f32x4 from = d[n % 3];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            to[q] = __builtin_fmaf(from[q], ONE == 1 ? sb[n % 4][q] : ONE == 2 ? sa[n / 4] : sb[n % 4][q] * sa[n / 4], to[q]);
+        formed(to);
+    };
+    auto multiply = [&](int first) {
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int n = 0; n < 4 * kHalf; ++n) {
+            d[n % 3] = block_product<1>(fb[n % 4], fa[n / 4]);
+            __builtin_amdgcn_sched_barrier(0);              // in this order
+            if (n >= 2) add(first, n - 2);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_s_setprio(0);
+    };
+    auto finish = [&](int first) {
+        add(first, 4 * kHalf - 2);
+        add(first, 4 * kHalf - 1);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto block = [&](uint8_t *la, uint8_t *lb, float *ls, uint8_t *next_a, uint8_t *next_b, float *next_s, int kb) {
+        if (kb > 0) finish(kHalf);
+        read_b(lb, ls);
+        read_a(la, ls, 0);
+        if (kb + 1 < p.blocks) loads.fetch(next_a, next_b, next_s, kb + 1);
+        meet();
+        multiply(0);
+        meet();
+        finish(0);
+        read_a(la, ls, kHalf);
+        if (second) arrived();
+        meet();
+        multiply(kHalf);
+        if (!second) arrived();
+        meet();
+    };
+    if (p.blocks > 0) loads.fetch(la0, lb0, ls0, 0);
+    arrived();
+    meet();
+    if (second) meet();
+    for (int kb = 0; kb < p.blocks; kb += 2) {
+        block(la0, lb0, ls0, la1, lb1, ls1, kb);
+        if (kb + 1 < p.blocks) block(la1, lb1, ls1, la0, lb0, ls0, kb + 1);
     }
+    if (p.blocks > 0) finish(kHalf);
+    if (!second) meet();
+    store_tile<1>(p, tile.z, m0 + wm, n0 + wn, acc);
 }
 
 // Rows of any length and alignment: they pass through registers on their way to LDS, cut to zeros where they end.
@@ -292,7 +414,7 @@ __global__ __launch_bounds__(kAnyThreads) void matmul_any(Params p) {
         for (int j = 0; j < 4; ++j) {
             const int row = wn + b_row(j, l16);
             fb[j] = two_pieces(lb, b_place(row, g), b_place(row, g + 4));
-            sb[j] = *reinterpret_cast<const f32x4 *>(lsb + wn + 16 * g + 4 * j);
+            sb[j] = *reinterpret_cast<const f32x4 *>(lsb + wn + c_column(j, g));
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -307,11 +429,7 @@ __global__ __launch_bounds__(kAnyThreads) void matmul_any(Params p) {
             }
         }
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t m = m0 + wm + 16 * i + l16, n = n0 + wn + 16 * g;
-        if (m < p.m && n < p.n) store_columns<OUT>(p.c, ((int64_t)tile.z * p.m + m) * p.n + n, acc[i], p.n - n);
-    }
+    store_tile<OUT>(p, tile.z, m0 + wm, n0 + wn, acc);
 }
 
 // ---- small products: a tile's blocks among a workgroup's waves --------------------------
