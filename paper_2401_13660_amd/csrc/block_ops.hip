@@ -128,12 +128,16 @@ struct MatmulPlan {
         tile_m = 16 * MI; tile_n = 16 * NJ; threads = 64 * mbs::matmul::kSplit;
     }
     template <int OUT> void choose(const mb_matmul_desc *d, const mbs::matmul::Params &p, const void *a, const void *b) {
-        const int64_t t128 = d->batch * ((p.m + 127) / 128) * ((p.n + 127) / 128);
-        const int64_t t256 = d->batch * ((p.m + 255) / 256) * ((p.n + 255) / 256);
         // whole aligned pieces of 16 bytes, and a tile's rows within the 31 bits of a buffer's offsets
         const bool whole = p.k % 16 == 0 && aligned(a, 16) && aligned(b, 16) && p.k < (int64_t(1) << 22);
-        if (p.m <= 16) split<OUT, 1, 1>();
-        else if (p.n <= 16 || t128 < 128) split<OUT, 2, 1>();
+        const int64_t t16 = d->batch * ((p.m + 15) / 16) * ((p.n + 15) / 16), t256 = d->batch * ((p.m + 255) / 256) * ((p.n + 255) / 256);
+        if (t16 < 512) split<OUT, 1, 1>();
+        else if (p.m <= 16) t16 < 1024 ? split<OUT, 1, 2>() : split<OUT, 1, 4>();
+        else if (p.n <= 16) t16 < 1024 ? split<OUT, 2, 1>() : split<OUT, 4, 1>();
+        else if (t16 < 1024) split<OUT, 2, 2>();
+        else if (p.m <= 32) split<OUT, 2, 4>();
+        else if (p.n <= 32 || t16 < 2048) split<OUT, 4, 2>();
+        else if (p.m <= 64 || p.n <= 64 || t16 < 5120) split<OUT, 4, 4>();
         else if (!whole) {
             fn = reinterpret_cast<const void *>(&mbs::matmul::matmul_any<OUT>);
             tile_m = tile_n = mbs::matmul::kAnyTile; threads = mbs::matmul::kAnyThreads;

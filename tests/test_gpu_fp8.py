@@ -163,7 +163,9 @@ def check_matmul(a, sa, b, sb, out="f32"):
 
 SIZES = [(1, 1, 1), (1, 16, 16), (3, 5, 7), (16, 16, 128), (17, 33, 129), (1, 300, 256), (300, 1, 256), (32, 512, 1792), (64, 64, 64),
          (100, 144, 3584), (127, 129, 127), (128, 128, 128), (129, 257, 272), (200, 1000, 520), (1021, 144, 384), (513, 300, 1003),
-         (2, 4000, 1024), (48, 1000, 2304), (700, 700, 144), (1500, 1700, 272), (2900, 1300, 400), (4100, 4100, 272), (8200, 2100, 640)]
+         (2, 4000, 1024), (48, 1000, 2304), (700, 700, 144), (1500, 1700, 272), (2900, 1300, 400), (4100, 4100, 272), (8200, 2100, 640),
+         (5, 9000, 200), (5, 20000, 130), (9000, 5, 200), (20000, 5, 130), (40, 7168, 256), (30, 17000, 128), (17000, 30, 128), (500, 1000, 1030),
+         (700, 900, 260), (60, 40000, 140), (40000, 60, 140), (1300, 1100, 1001)]
 
 
 @pytest.mark.parametrize("m,n,k", SIZES)
