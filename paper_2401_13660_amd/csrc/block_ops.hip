@@ -21,42 +21,52 @@ int64_t blocks_of(int64_t n) { return n / mbs::fp8::kBlock + (n % mbs::fp8::kBlo
 
 // ---- norm -----------------------------------------------------------------------
 
-// Waves per row and spans per lane for a row of this width; a walk past the widest.
-template <int X, int RES, int OUT> const void *norm_fn(int64_t dim, int *waves) {
+// Waves per row and spans per lane for a row of this width, whole spans where it is made of them; a walk past the widest.
+template <int X, int RES, int OUT> const void *norm_fn(int64_t rows, int64_t dim, int *waves) {
     namespace N = mbs::norm;
     const int64_t spans = (dim + 7) / 8;
-    *waves = 1;
-    if (spans <= 64) return reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, 1, 1>);
-    if (spans <= 128) return reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, 1, 2>);
-    if (spans <= 256) return reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, 1, 4>);
+    const bool cut = dim % 8 != 0;
     *waves = 4;
-    if (spans <= 768) return reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, 4, 3>);
+    // few rows: 4 waves each, which ask for everything at once
+    if (!cut && rows <= 1024 && spans > 64 && spans <= 256) return reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, 4, 1, false>);
+    if (spans > 256 && spans <= 768)
+        return cut ? reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, 4, 3, true>)
+                   : reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, 4, 3, false>);
+    *waves = 1;
+    if (cut && spans <= 256) return reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, 1, 4, true>);
+    if (spans <= 64) return reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, 1, 1, false>);
+    if (spans <= 128) return reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, 1, 2, false>);
+    if (spans <= 256) return reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, 1, 4, false>);
     *waves = N::kLoopWaves;
-    if (spans <= 2048) return reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, N::kLoopWaves, 2>);
+    if (spans <= 2048) return reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, N::kLoopWaves, 2, true>);
     return reinterpret_cast<const void *>(&N::rms_norm_walk<X, RES, OUT>);
 }
-template <int X, int RES> const void *norm_fn(int32_t out, int64_t dim, int *waves) {
-    return out == MB_F32    ? norm_fn<X, RES, 0>(dim, waves)
-           : out == MB_BF16 ? norm_fn<X, RES, 1>(dim, waves)
-                            : norm_fn<X, RES, mbs::norm::kFp8>(dim, waves);
+template <int X, int RES> const void *norm_fn(int32_t out, int64_t rows, int64_t dim, int *waves) {
+    return out == MB_F32    ? norm_fn<X, RES, 0>(rows, dim, waves)
+           : out == MB_BF16 ? norm_fn<X, RES, 1>(rows, dim, waves)
+                            : norm_fn<X, RES, mbs::norm::kFp8>(rows, dim, waves);
 }
-template <int X> const void *norm_fn(int32_t res, int32_t out, int64_t dim, int *waves) {
-    return res == MB_F32    ? norm_fn<X, 0>(out, dim, waves)
-           : res == MB_BF16 ? norm_fn<X, 1>(out, dim, waves)
-                            : norm_fn<X, mbs::norm::kNone>(out, dim, waves);
+template <int X> const void *norm_fn(int32_t res, int32_t out, int64_t rows, int64_t dim, int *waves) {
+    return res == MB_F32    ? norm_fn<X, 0>(out, rows, dim, waves)
+           : res == MB_BF16 ? norm_fn<X, 1>(out, rows, dim, waves)
+                            : norm_fn<X, mbs::norm::kNone>(out, rows, dim, waves);
 }
 
 template <int DY, int H, int DX> const void *norm_bwd_fn(int64_t dim, int *waves) {
     namespace N = mbs::norm;
     const int64_t spans = (dim + 7) / 8;
+    const bool cut = dim % 8 != 0;
     *waves = 1;
-    if (spans <= 64) return reinterpret_cast<const void *>(&N::rms_norm_bwd_rows<DY, H, DX, 1, 1>);
-    if (spans <= 128) return reinterpret_cast<const void *>(&N::rms_norm_bwd_rows<DY, H, DX, 1, 2>);
-    if (spans <= 256) return reinterpret_cast<const void *>(&N::rms_norm_bwd_rows<DY, H, DX, 1, 4>);
+    if (cut && spans <= 256) return reinterpret_cast<const void *>(&N::rms_norm_bwd_rows<DY, H, DX, 1, 4, true>);
+    if (spans <= 64) return reinterpret_cast<const void *>(&N::rms_norm_bwd_rows<DY, H, DX, 1, 1, false>);
+    if (spans <= 128) return reinterpret_cast<const void *>(&N::rms_norm_bwd_rows<DY, H, DX, 1, 2, false>);
+    if (spans <= 256) return reinterpret_cast<const void *>(&N::rms_norm_bwd_rows<DY, H, DX, 1, 4, false>);
     *waves = 4;
-    if (spans <= 768) return reinterpret_cast<const void *>(&N::rms_norm_bwd_rows<DY, H, DX, 4, 3>);
+    if (spans <= 768)
+        return cut ? reinterpret_cast<const void *>(&N::rms_norm_bwd_rows<DY, H, DX, 4, 3, true>)
+                   : reinterpret_cast<const void *>(&N::rms_norm_bwd_rows<DY, H, DX, 4, 3, false>);
     *waves = N::kLoopWaves;
-    if (spans <= 2048) return reinterpret_cast<const void *>(&N::rms_norm_bwd_rows<DY, H, DX, N::kLoopWaves, 2>);
+    if (spans <= 2048) return reinterpret_cast<const void *>(&N::rms_norm_bwd_rows<DY, H, DX, N::kLoopWaves, 2, true>);
     return reinterpret_cast<const void *>(&N::rms_norm_bwd_walk<DY, H, DX>);
 }
 template <int DY> const void *norm_bwd_fn(int32_t h, int32_t dx, int64_t dim, int *waves) {
@@ -71,7 +81,8 @@ bool norm_sizes(int64_t rows, int64_t dim, int64_t *elems) {
 
 // Workgroups of the gradient: what runs at once, 8 waves per CU.
 int64_t norm_bwd_groups(int64_t rows, int64_t dim) {
-    const int64_t per = dim <= 2048 ? 4 : 1, most = dim <= 2048 ? 512 : dim <= 6144 ? 512 : 256;
+    // at least two rows to a wave (or workgroup): (2042, 1536) fp32 16.9 us with one, 15.4 with two
+    const int64_t per = dim <= 2048 ? 8 : 2, most = dim <= 6144 ? 512 : 256;
     return std::min(most, (rows + per - 1) / per);
 }
 
@@ -95,7 +106,13 @@ template <int X> const void *quant_fn(bool tile, bool transpose) {
 
 template <int DT> const void *sample_fn(int64_t vocab, unsigned *threads) {
     namespace S = mbs::pick;
-    *threads = vocab <= 1024 ? 256 : 1024;
+    // one wave needs no barriers
+    *threads = vocab <= 256 ? 64 : vocab <= 1024 ? 256 : 1024;
+    if (vocab <= 256) return reinterpret_cast<const void *>(&S::sample_rows<DT, 64, 1>);
+#ifdef WAVE4
+    *threads = vocab <= 1024 ? 64 : 1024;
+    if (vocab <= 1024) return reinterpret_cast<const void *>(&S::sample_rows<DT, 64, 4>);
+#endif
     if (vocab <= 1024) return reinterpret_cast<const void *>(&S::sample_rows<DT, 256, 1>);
     if (vocab <= 8192) return reinterpret_cast<const void *>(&S::sample_rows<DT, 1024, 2>);
     return reinterpret_cast<const void *>(&S::sample_rows<DT, 1024, 0>);
@@ -175,7 +192,7 @@ int mb_rms_norm_fwd(int64_t rows, int64_t dim, int32_t x_dtype, int32_t residual
     mbs::norm::FwdParams p{rows, dim, x, weight, residual, y, scales, residual_out, rstd, eps};
     const int32_t res = adds ? residual_dtype : -1;
     int waves;
-    const void *fn = x_dtype == MB_F32 ? norm_fn<0>(res, out_dtype, dim, &waves) : norm_fn<1>(res, out_dtype, dim, &waves);
+    const void *fn = x_dtype == MB_F32 ? norm_fn<0>(res, out_dtype, rows, dim, &waves) : norm_fn<1>(res, out_dtype, rows, dim, &waves);
     const int64_t per = waves == 1 ? 4 : 1;
     const int64_t blocks = std::min<int64_t>((rows + per - 1) / per, 1 << 20);
     return status(launch(fn, dim3((unsigned)blocks), dim3(waves == 1 ? 256 : 64 * waves), &p, stream));

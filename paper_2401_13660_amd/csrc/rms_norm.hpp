@@ -51,14 +51,14 @@ struct BwdParams {
     float *part;                    // (workgroups, dim), or dweight itself where there is one workgroup
 };
 
-// Spans of 8 columns that may be cut by the row's end.
-template <int DT> __device__ __forceinline__ void load8(Span<DT, 8> &s, const void *p, int64_t at, int n) {
+// Spans of 8 columns, of which n are the row's.  CUT: the row may end within one; else n is 8 or 0.
+template <bool CUT, int DT> __device__ __forceinline__ void load8(Span<DT, 8> &s, const void *p, int64_t at, int n) {
     if (n >= 8) s.load(p, at);
-    else s.load_first(p, at, n);
+    else s.load_first(p, at, CUT ? n : 0);
 }
-template <int DT> __device__ __forceinline__ void store8(void *p, int64_t at, const float (&v)[8], int n) {
+template <bool CUT, int DT> __device__ __forceinline__ void store8(void *p, int64_t at, const float (&v)[8], int n) {
     if (n >= 8) store_span<DT, 8>(p, at, v);
-    else store_first<DT, 8>(p, at, v, n);
+    else if (CUT) store_first<DT, 8>(p, at, v, n);
 }
 
 // The sum over a row's W waves; `red` holds two rounds of W values, so that one barrier a row is enough.
@@ -76,12 +76,12 @@ template <int W> __device__ __forceinline__ float row_sum(float v, float *red, i
 }
 
 // The columns of a span as the norm sees them.
-template <int X, int RES> struct Sum8 {
+template <int X, int RES, bool CUT> struct Sum8 {
     Span<X, 8> x;
     Span<RES == kNone ? X : RES, 8> res;
     __device__ __forceinline__ void load(const FwdParams &p, int64_t at, int n) {
-        load8(x, p.x, at, n);
-        if constexpr (RES != kNone) load8(res, p.residual, at, n);
+        load8<CUT>(x, p.x, at, n);
+        if constexpr (RES != kNone) load8<CUT>(res, p.residual, at, n);
     }
     // h, kept in residual_out
     __device__ __forceinline__ void add(const FwdParams &p, int64_t at, int n, float (&h)[8]) {
@@ -91,7 +91,7 @@ template <int X, int RES> struct Sum8 {
             if constexpr (RES != kNone) h[i] += res.get(i);
         }
         if constexpr (RES != kNone) {
-            store8<RES>(p.residual_out, at, h, n);
+            store8<CUT, RES>(p.residual_out, at, h, n);
             if constexpr (RES == 1) {
 #pragma unroll
                 for (int i = 0; i < 8; i += 2) {
@@ -104,27 +104,29 @@ template <int X, int RES> struct Sum8 {
     }
 };
 
-template <int OUT>
-__device__ __forceinline__ void emit(const FwdParams &p, int64_t row, int64_t col, int n, const float (&h)[8], float r) {
-    float w[8], y[8];
+template <bool CUT> __device__ __forceinline__ void load_weight(const float *weight, int64_t col, int n, float (&w)[8]) {
     Span<0, 8> s;
-    if (p.weight && n > 0) load8(s, p.weight, col, n);
+    if (weight) load8<CUT>(s, weight, col, n);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        w[i] = p.weight ? (i < n ? s.get(i) : 0.0f) : 1.0f;
-        y[i] = h[i] * r * w[i];
-    }
+    for (int i = 0; i < 8; ++i) w[i] = weight ? s.get(i) : 1.0f;
+}
+
+template <int OUT, bool CUT>
+__device__ __forceinline__ void emit(const FwdParams &p, int64_t row, int64_t col, int n, const float (&h)[8], const float (&w)[8], float r) {
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = h[i] * r * w[i];
     if constexpr (OUT == kFp8) {
         float top = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = __builtin_fmaxf(top, __builtin_fabsf(i < n ? y[i] : 0.0f));
+        for (int i = 0; i < 8; ++i) top = __builtin_fmaxf(top, __builtin_fabsf(CUT && i >= n ? 0.0f : y[i]));
         const float scale = fp8::scale_of(fp8::max_of_16(top));
         if (n > 0) {
-            fp8::store8(static_cast<uint8_t *>(p.y) + row * p.dim + col, y, 1.0f / scale, n);
+            fp8::store8(static_cast<uint8_t *>(p.y) + row * p.dim + col, y, 1.0f / scale, CUT ? n : 8);
             if (col % fp8::kBlock == 0) p.scales[row * ((p.dim + fp8::kBlock - 1) / fp8::kBlock) + col / fp8::kBlock] = scale;
         }
     } else {
-        if (n > 0) store8<OUT>(p.y, row * p.dim + col, y, n);
+        if (n > 0) store8<CUT, OUT>(p.y, row * p.dim + col, y, n);
     }
 }
 
@@ -133,11 +135,11 @@ __device__ __forceinline__ float inverse_length(float squares, const FwdParams &
 }
 
 // Columns of a span within the row: 8, fewer at its end, none past it.
-__device__ __forceinline__ int within(int64_t dim, int64_t col) {
-    return (int)min((int64_t)8, max((int64_t)0, dim - col));
+template <bool CUT> __device__ __forceinline__ int within(int64_t dim, int64_t col) {
+    return CUT ? (int)min((int64_t)8, max((int64_t)0, dim - col)) : col < dim ? 8 : 0;
 }
 
-template <int X, int RES, int OUT, int W, int J>
+template <int X, int RES, int OUT, int W, int J, bool CUT>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_rows(FwdParams p) {
     constexpr int kRows = W == 1 ? 4 : 1;
     __shared__ float red[2 * W];
@@ -145,27 +147,36 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_rows(FwdParams
     const int64_t step = (int64_t)gridDim.x * kRows;
     int round = 0;
     for (int64_t row = (int64_t)blockIdx.x * kRows + (W == 1 ? threadIdx.x >> 6 : 0); row < p.rows; row += step, ++round) {
-        Sum8<X, RES> in[J];
-        float h[J][8];
+        Sum8<X, RES, CUT> in[J];
+        float h[J][8], w[J][8];
         const int64_t at = row * p.dim;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int64_t col = 8 * (j * 64 * W + t);
-            in[j].load(p, at + col, within(p.dim, col));
+            in[j].load(p, at + col, within<CUT>(p.dim, col));
+            // ahead where the registers are there for it; rows of more spans hide its latency behind each other
+            if (J == 1) load_weight<CUT>(p.weight, col, within<CUT>(p.dim, col), w[j]);
         }
-        float sum = 0.0f;
+        // A wave alone adds up its spans' sums as four waves of a span each would: a row's bits do not hang on how many rows there are.
+        float sum = 0.0f, whole = 0.0f;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int64_t col = 8 * (j * 64 * W + t);
-            in[j].add(p, at + col, within(p.dim, col), h[j]);
+            in[j].add(p, at + col, within<CUT>(p.dim, col), h[j]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(h[j][i], h[j][i], sum);
+            if constexpr (W == 1) {
+                whole = j == 0 ? wave_sum(sum) : whole + wave_sum(sum);
+                sum = 0.0f;
+            }
         }
-        const float r = inverse_length(row_sum<W>(sum, red, round), p);
+        if constexpr (W > 1) whole = row_sum<W>(sum, red, round);
+        const float r = inverse_length(whole, p);
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int64_t col = 8 * (j * 64 * W + t);
-            emit<OUT>(p, row, col, within(p.dim, col), h[j], r);
+            if (J > 1) load_weight<CUT>(p.weight, col, within<CUT>(p.dim, col), w[j]);
+            emit<OUT, CUT>(p, row, col, within<CUT>(p.dim, col), h[j], w[j], r);
         }
         if (p.rstd && t == 0) p.rstd[row] = r;
     }
@@ -182,8 +193,8 @@ __global__ __launch_bounds__(64 * kLoopWaves) void rms_norm_walk(FwdParams p) {
         float sum = 0.0f;
         for (int64_t first = 0; first < p.dim; first += 8 * 64 * kLoopWaves) {
             const int64_t col = first + 8 * t;
-            const int n = within(p.dim, col);
-            Sum8<X, RES> in;
+            const int n = within<true>(p.dim, col);
+            Sum8<X, RES, true> in;
             float h[8];
             in.load(p, at + col, n);
             in.add(p, at + col, n, h);
@@ -193,26 +204,27 @@ __global__ __launch_bounds__(64 * kLoopWaves) void rms_norm_walk(FwdParams p) {
         const float r = inverse_length(row_sum<kLoopWaves>(sum, red, round), p);
         for (int64_t first = 0; first < p.dim; first += 8 * 64 * kLoopWaves) {
             const int64_t col = first + 8 * t;
-            const int n = within(p.dim, col);
+            const int n = within<true>(p.dim, col);
             Span<RES == kNone ? X : RES, 8> s;
-            float h[8];
-            load8(s, RES == kNone ? p.x : p.residual_out, at + col, n);
+            float h[8], w[8];
+            load8<true>(s, RES == kNone ? p.x : p.residual_out, at + col, n);
 #pragma unroll
             for (int i = 0; i < 8; ++i) h[i] = s.get(i);
-            emit<OUT>(p, row, col, n, h, r);
+            load_weight<true>(p.weight, col, n, w);
+            emit<OUT, true>(p, row, col, n, h, w, r);
         }
         if (p.rstd && t == 0) p.rstd[row] = r;
     }
 }
 
 // One span of a row's gradient.
-template <int DY, int H> struct Grad8 {
+template <int DY, int H, bool CUT> struct Grad8 {
     Span<DY, 8> dy;
     Span<H, 8> h, dh;
     __device__ __forceinline__ void load(const BwdParams &p, int64_t at, int n) {
-        load8(dy, p.dy, at, n);
-        load8(h, p.h, at, n);
-        if (p.dh) load8(dh, p.dh, at, n);
+        load8<CUT>(dy, p.dy, at, n);
+        load8<CUT>(h, p.h, at, n);
+        if (p.dh) load8<CUT>(dh, p.dh, at, n);
     }
     template <int DX>
     __device__ __forceinline__ void store(const BwdParams &p, int64_t at, int n, const float (&w)[8], float r, float along) const {
@@ -223,20 +235,13 @@ template <int DY, int H> struct Grad8 {
             if (p.dh) d[i] += dh.get(i);
         }
         if (n > 0) {
-            store8<DX>(p.dx, at, d, n);
-            if (p.dresidual) store8<H>(p.dresidual, at, d, n);
+            store8<CUT, DX>(p.dx, at, d, n);
+            if (p.dresidual) store8<CUT, H>(p.dresidual, at, d, n);
         }
     }
 };
 
-__device__ __forceinline__ void load_weight(const BwdParams &p, int64_t col, int n, float (&w)[8]) {
-    Span<0, 8> s;
-    if (p.weight) load8(s, p.weight, col, n);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = p.weight ? s.get(i) : 1.0f;
-}
-
-template <int DY, int H, int DX, int W, int J>
+template <int DY, int H, int DX, int W, int J, bool CUT>
 __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_bwd_rows(BwdParams p) {
     constexpr int kRows = W == 1 ? 4 : 1;
     __shared__ float red[2 * W];
@@ -246,16 +251,16 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_bwd_rows(BwdPa
     float dw[J][8] = {};
     int round = 0;
     for (int64_t row = (int64_t)blockIdx.x * kRows + (W == 1 ? wave : 0); row < p.rows; row += step, ++round) {
-        Grad8<DY, H> in[J];
+        Grad8<DY, H, CUT> in[J];
         float w[J][8];
         const int64_t at = row * p.dim;
         const float r = p.rstd[row];
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int64_t col = 8 * (j * 64 * W + t);
-            const int n = within(p.dim, col);
+            const int n = within<CUT>(p.dim, col);
             in[j].load(p, at + col, n);
-            load_weight(p, col, n, w[j]);
+            load_weight<CUT>(p.weight, col, n, w[j]);
         }
         float sum = 0.0f;
 #pragma unroll
@@ -270,7 +275,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_bwd_rows(BwdPa
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int64_t col = 8 * (j * 64 * W + t);
-            in[j].template store<DX>(p, at + col, within(p.dim, col), w[j], r, along);
+            in[j].template store<DX>(p, at + col, within<CUT>(p.dim, col), w[j], r, along);
         }
     }
     if (!p.dweight) return;
@@ -294,8 +299,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_bwd_rows(BwdPa
 #pragma unroll
     for (int j = 0; j < J; ++j) {
         const int64_t col = 8 * (j * 64 * W + t);
-        const int n = within(p.dim, col);
-        if (n > 0) store8<0>(out, col, dw[j], n);
+        const int n = within<CUT>(p.dim, col);
+        if (n > 0) store8<CUT, 0>(out, col, dw[j], n);
     }
 }
 
@@ -312,33 +317,33 @@ __global__ __launch_bounds__(64 * kLoopWaves) void rms_norm_bwd_walk(BwdParams p
         float sum = 0.0f;
         for (int64_t first = 0; first < p.dim; first += 8 * 64 * kLoopWaves) {
             const int64_t col = first + 8 * t;
-            const int n = within(p.dim, col);
+            const int n = within<true>(p.dim, col);
             if (n <= 0) continue;
             Span<DY, 8> dy;
             Span<H, 8> h;
             float w[8], dw[8];
-            load8(dy, p.dy, at + col, n);
-            load8(h, p.h, at + col, n);
-            load_weight(p, col, n, w);
+            load8<true>(dy, p.dy, at + col, n);
+            load8<true>(h, p.h, at + col, n);
+            load_weight<true>(p.weight, col, n, w);
             Span<0, 8> before;
-            if (p.dweight && round > 0) load8(before, out, col, n);
+            if (p.dweight && round > 0) load8<true>(before, out, col, n);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float u = h.get(i) * r, g = dy.get(i);
                 sum = __builtin_fmaf(g * w[i], u, sum);
                 dw[i] = round > 0 && p.dweight ? __builtin_fmaf(g, u, before.get(i)) : g * u;
             }
-            if (p.dweight) store8<0>(out, col, dw, n);
+            if (p.dweight) store8<true, 0>(out, col, dw, n);
         }
         const float along = row_sum<kLoopWaves>(sum, red, round) / (float)p.dim;
         for (int64_t first = 0; first < p.dim; first += 8 * 64 * kLoopWaves) {
             const int64_t col = first + 8 * t;
-            const int n = within(p.dim, col);
+            const int n = within<true>(p.dim, col);
             if (n <= 0) continue;
-            Grad8<DY, H> in;
+            Grad8<DY, H, true> in;
             float w[8];
             in.load(p, at + col, n);
-            load_weight(p, col, n, w);
+            load_weight<true>(p.weight, col, n, w);
             in.template store<DX>(p, at + col, n, w, r, along);
         }
     }

@@ -267,7 +267,7 @@ __global__ __launch_bounds__(T) void sample_rows(Params p) {
     const int64_t b = blockIdx.x;
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const Filter f(p, b);
-    using R = Row<DT, T, S, std::conditional_t<T == 256, double, float>>;
+    using R = Row<DT, T, S, std::conditional_t<T <= 256, double, float>>;
     R row;
     row.logits = p.logits;
     row.at = b * p.vocab;
