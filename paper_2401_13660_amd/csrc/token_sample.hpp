@@ -149,7 +149,7 @@ template <int DT, int T, int S, class W> struct Row {
         if constexpr (S > 0) {
 #pragma unroll
             for (int k = 0; k < S; ++k) {
-                opaque(s[k].v);
+                if (S > 1) opaque(s[k].v);
                 f(first_of(k), s[k]);
                 // span after span: the work of many side by side would not fit the registers
                 if (S > 2 && k % 2 == 1) __builtin_amdgcn_sched_barrier(0);
@@ -174,7 +174,7 @@ template <int DT, int T, int S, class W> struct Row {
                 Span<DT, 4> some[N];
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    opaque(s[k + i].v);
+                    if (S > 1) opaque(s[k + i].v);
                     some[i] = s[k + i];
                 }
                 f(k, some);
@@ -254,6 +254,7 @@ template <int T> struct Shared {
     uint64_t wave_weight[kWaves], low, high, border, border_sum, found_weight;
     uint32_t wave_count[kWaves], listed, found_bin, found_count;
     uint64_t sums[kWaves];
+    double weights[kWaves];
     float tops[kWaves], lows[kWaves], scores[kWaves];
     int32_t who[kWaves];
     uint32_t bad;
@@ -470,6 +471,7 @@ __global__ __launch_bounds__(T) void sample_rows(Params p) {
     const uint32_t border_bits = (uint32_t)(border >> 32), border_at = ~(uint32_t)border;
     const float border_logit = border ? __uint_as_float(border_bits & 0x80000000u ? border_bits & 0x7fffffffu : ~border_bits) : -__builtin_inff();
     auto kept = [&](uint32_t y, float l) { return l > border_logit || (l == border_logit && border && y <= border_at); };
+    typename R::Weight weighs = 0;                  // of this thread's best
     auto run_race = [&](uint32_t y, float l, float noise) {
         const typename R::Weight e = row.weight(l);
         if (!(e > 0 && e >= f.min_p)) return;
@@ -478,6 +480,7 @@ __global__ __launch_bounds__(T) void sample_rows(Params p) {
         if (s > best || (s == best && s > 0.0f && (int32_t)y < at)) {
             best = s;
             at = (int32_t)y;
+            weighs = e;
         }
     };
     // with a border, the kept in a list where it has room for them: few threads' work instead of everyone's
@@ -518,26 +521,26 @@ __global__ __launch_bounds__(T) void sample_rows(Params p) {
     };
     if (!listed) row.template groups<kSide>(race);
     const float won = wave_max(best);
-    at = wave_min(best == won && at != kNobody ? at : kNobody);
-    best = won;
-    for (int m = 1; m < 64; m *= 2) sum += __shfl_xor(sum, m);              // whole numbers: the list's order does not show
+    const int32_t first = wave_min(best == won ? at : kNobody);
+    sum = wave_running_sum(sum);                    // whole numbers: the list's order does not show
     __syncthreads();
-    if (lane == 0) {
+    if (lane == 63) {
         sh.scores[wave] = won;
-        sh.who[wave] = at;
+        sh.who[wave] = first;
         sh.sums[wave] = sum;
     }
+    if (at == first && at != kNobody) sh.weights[wave] = (double)weighs;
     __syncthreads();
     if (t == 0) {
-        for (int w = 1; w < kWaves; ++w) {
+        sum = 0;
+        int winner = -1;
+        for (int w = 0; w < kWaves; ++w) {
             sum += sh.sums[w];
-            if (sh.who[w] != kNobody && (at == kNobody || sh.scores[w] > best || (sh.scores[w] == best && sh.who[w] < at))) {
-                best = sh.scores[w];
-                at = sh.who[w];
-            }
+            if (sh.who[w] == kNobody) continue;
+            if (winner < 0 || sh.scores[w] > sh.scores[winner] || (sh.scores[w] == sh.scores[winner] && sh.who[w] < sh.who[winner])) winner = w;
         }
-        p.token[b] = at == kNobody ? -1 : at;
-        if (p.prob) p.prob[b] = at == kNobody ? 0.0f : (float)((double)row.weight(Act<DT>::ld(p.logits, row.at + at)) * 17592186044416.0 / (double)sum);
+        p.token[b] = winner < 0 ? -1 : sh.who[winner];
+        if (p.prob) p.prob[b] = winner < 0 ? 0.0f : (float)(sh.weights[winner] * 17592186044416.0 / (double)sum);
     }
 }
 
