@@ -9,11 +9,11 @@
 // The order is that of 64-bit ranks (the logit's bits in an order of integers, then the index from the last), and all that a
 // filter does is to find the lowest rank that it keeps.  Nothing is sorted: tokens are counted into bins of falling logits with what
 // they weigh, the bin in which the wanted count or weight is reached is found by a running sum over the bins, and its few
-// tokens are ranked one by one.  A bin of more than kList of them (logits far apart from the rest, equals by the hundred) is
+// tokens are ranked one by one.  A bin of more than 256 of them (logits far apart from the rest, equals by the hundred) is
 // counted once more into bins of its own, of ranks.  Weights are summed as integers of 2^-44: sums do not depend
 // on the order of the atomics, and a border does not move from call to call.
 //
-// One workgroup per sequence, the row in registers from one load to the token drawn (up to 32,768 tokens; beyond, it is read
+// One workgroup per sequence, the row in registers from one load to the token drawn (up to 8,192 tokens; beyond, it is read
 // again from the cache); the kept tokens go to a list, and random numbers are only read for those.  Bound by latency and, for large
 // vocabularies, by one CU's instructions: about 25 per token for the weight and its bin.
 #pragma once
@@ -29,7 +29,6 @@ namespace mbs {
 namespace pick {
 
 constexpr int32_t kNobody = 0x7fffffff;
-constexpr int kList = 64;                           // tokens of a bin that are ranked one by one
 
 struct Params {
     int64_t batch, vocab;
@@ -239,6 +238,7 @@ template <class R> __device__ __forceinline__ float2 wave_tops(R &row, bool ok) 
 
 template <int T> struct Shared {
     static constexpr int kBins = 4 * T, kWaves = T / 64, kKept = 4 * T;
+    static constexpr int kList = T == 64 ? 64 : 256;    // tokens of a bin that are ranked one by one
     union {
         struct {
             uint64_t weight[kBins];
@@ -263,7 +263,7 @@ template <int T> struct Shared {
 template <int DT, int T, int S>
 __global__ __launch_bounds__(T) void sample_rows(Params p) {
     using Sh = Shared<T>;
-    constexpr int kBins = Sh::kBins, kWaves = Sh::kWaves;
+    constexpr int kBins = Sh::kBins, kWaves = Sh::kWaves, kList = Sh::kList;
     __shared__ Sh sh;
     const int64_t b = blockIdx.x;
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -368,9 +368,9 @@ __global__ __launch_bounds__(T) void sample_rows(Params p) {
                     sh.high = 0;
                     sh.border = 0;
                 }
-                if (t < kList) {
-                    sh.places[t] = 0;
-                    sh.higher[t] = 0;
+                for (int i = t; i < kList; i += T) {
+                    sh.places[i] = 0;
+                    sh.higher[i] = 0;
                 }
                 __syncthreads();
                 c = run_c - c;
@@ -433,26 +433,27 @@ __global__ __launch_bounds__(T) void sample_rows(Params p) {
                     continue;
                 }
                 // each token of the list against every kWaves-th of them, wave by wave
-                const uint64_t mine = lane < n ? sh.list[lane] : 0;
-                uint64_t higher = 0;
-                uint32_t places = 0;
-                for (uint32_t i = wave; i < n; i += kWaves)
-                    if (sh.list[i] > mine) {
-                        ++places;
-                        higher += sh.list_weight[i];
+                for (uint32_t k = lane; k < n; k += 64) {
+                    const uint64_t mine = sh.list[k];
+                    uint64_t higher = 0;
+                    uint32_t places = 0;
+                    for (uint32_t i = wave; i < n; i += kWaves)
+                        if (sh.list[i] > mine) {
+                            ++places;
+                            higher += sh.list_weight[i];
+                        }
+                    if (places) {
+                        atomicAdd(&sh.places[k], places);
+                        atomicAdd(reinterpret_cast<unsigned long long *>(&sh.higher[k]), (unsigned long long)higher);
                     }
-                if (places) {
-                    atomicAdd(&sh.places[lane], places);
-                    atomicAdd(reinterpret_cast<unsigned long long *>(&sh.higher[lane]), (unsigned long long)higher);
                 }
                 __syncthreads();
-                if (wave == 0 && lane < n) {
-                    places = sh.places[lane];
-                    higher = sh.higher[lane];
-                    const uint64_t weighs_mine = sh.list_weight[lane];
-                    if (weighs ? higher < wanted && higher + weighs_mine >= wanted : places == wanted - 1) {
-                        sh.border = mine;
-                        sh.border_sum = above + higher + weighs_mine;
+                for (uint32_t k = t; k < n; k += T) {
+                    const uint32_t places = sh.places[k];
+                    const uint64_t higher = sh.higher[k], mine = sh.list_weight[k];
+                    if (weighs ? higher < wanted && higher + mine >= wanted : places == wanted - 1) {
+                        sh.border = sh.list[k];
+                        sh.border_sum = above + higher + mine;
                     }
                 }
                 __syncthreads();
