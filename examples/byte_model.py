@@ -1,7 +1,7 @@
 """A small byte-level model of Mamba blocks, trained and then sampled by speculation, with the library's operators
-running together: the embedding, the convolution and the scan with their gradients, the clipping of all gradients; then
-drafts from byte-pair counts, the convolution and the scan over a draft from their carried states, the verification
-against the model's probabilities, and the states at the last accepted byte.
+running together: the embedding, the norm, the convolution and the scan with their gradients, the clipping of all gradients;
+then drafts from byte-pair counts, the convolution and the scan over a draft from their carried states, the verification
+against the model's probabilities, and the states at the last accepted byte; then byte by byte from a nucleus.
 
     python examples/byte_model.py [steps]
 """
@@ -41,7 +41,7 @@ class Block(torch.nn.Module):
 
     def split(self, h):
         """(batch, L, width) -> the convolution's input and the gate, (batch, D, L)."""
-        h = h * torch.rsqrt(h.square().mean(-1, keepdim=True) + 1e-5) * self.norm
+        h = mb.rms_norm(h, self.norm)
         x, z = (h @ self.in_proj.t()).transpose(1, 2).chunk(2, 1)
         return x.contiguous(), z.contiguous()
 
@@ -165,6 +165,20 @@ def generate(model, drafter, prompt, rounds, drafts=8, temperature=1.0, seed=0):
     return out, states, torch.stack(accepted_all)
 
 
+@torch.no_grad()
+def complete(model, prompt, count, temperature=1.0, top_p=0.98, seed=0):
+    """`count` bytes after each of a batch of prompts (batch, L), one by one from the nucleus of the model's probabilities."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    b, states, cur, out = prompt.shape[0], model.empty(prompt.shape[0]), prompt, []
+    for _ in range(count):
+        logits, seen = model.extend(cur, states)
+        states = [Block.at(s, torch.full((b,), cur.shape[1] - 1, dtype=torch.int32, device=DEV)) for s in seen]
+        noise = torch.empty(b, VOCAB, device=DEV).exponential_(generator=g)
+        cur = mb.sample(logits[:, -1].contiguous(), noise, temperature=temperature, top_p=top_p)[:, None]
+        out.append(cur)
+    return torch.cat(out, 1)
+
+
 def main():
     steps = int(sys.argv[1]) if len(sys.argv) > 1 else 300
     torch.manual_seed(0)
@@ -177,6 +191,7 @@ def main():
     out, _, accepted = generate(model, pair_logits(text), prompt, rounds=24)
     print(f"{accepted.float().mean():.2f} of 8 drafted bytes accepted per round")
     print(bytes(out[0][200:]).decode("utf-8", "replace"))
+    print(bytes(complete(model, prompt[:1], 64)[0].tolist()).decode("utf-8", "replace"))
 
 
 if __name__ == "__main__":

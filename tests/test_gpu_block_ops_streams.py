@@ -242,3 +242,19 @@ def test_training_step():
     ((y @ w.t() * cy).sum() + (h * ch).sum()).backward()
     for a, t in zip(got, leaves):
         assert (a - t.grad).norm() <= 2 * 2.0 ** -4 * 1.1 * t.grad.norm()
+
+
+def test_example_completes():
+    """The example's byte-by-byte continuation: bytes, the same for the same seed, and the model's largest logit at temperature 0."""
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import byte_model as E
+    announce("byte model: bytes one by one")
+    torch.manual_seed(0)
+    model = E.ByteModel(32, 2)
+    prompt = torch.randint(0, 256, (3, 20), device="cuda:0").to(torch.uint8)
+    a = E.complete(model, prompt, 6)
+    assert a.shape == (3, 6) and torch.equal(a, E.complete(model, prompt, 6)) and a.min() >= 0 and a.max() < 256
+    with torch.no_grad():
+        assert torch.equal(E.complete(model, prompt, 1, temperature=0.0)[:, 0].long(), model.extend(prompt, model.empty(3))[0][:, -1].argmax(1))
