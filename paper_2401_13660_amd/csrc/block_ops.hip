@@ -109,10 +109,6 @@ template <int DT> const void *sample_fn(int64_t vocab, unsigned *threads) {
     // one wave needs no barriers
     *threads = vocab <= 256 ? 64 : vocab <= 1024 ? 256 : 1024;
     if (vocab <= 256) return reinterpret_cast<const void *>(&S::sample_rows<DT, 64, 1>);
-#ifdef WAVE4
-    *threads = vocab <= 1024 ? 64 : 1024;
-    if (vocab <= 1024) return reinterpret_cast<const void *>(&S::sample_rows<DT, 64, 4>);
-#endif
     if (vocab <= 1024) return reinterpret_cast<const void *>(&S::sample_rows<DT, 256, 1>);
     if (vocab <= 8192) return reinterpret_cast<const void *>(&S::sample_rows<DT, 1024, 2>);
     return reinterpret_cast<const void *>(&S::sample_rows<DT, 1024, 0>);
@@ -144,22 +140,27 @@ struct MatmulPlan {
         fn = reinterpret_cast<const void *>(&mbs::matmul::matmul_split<OUT, MI, NJ>);
         tile_m = 16 * MI; tile_n = 16 * NJ; threads = 64 * mbs::matmul::kSplit;
     }
+    template <int OUT> void tiled(const mb_matmul_desc *d, bool whole, int64_t t256) {
+        if (!whole) {
+            fn = reinterpret_cast<const void *>(&mbs::matmul::matmul_any<OUT>);
+            tile_m = tile_n = mbs::matmul::kAnyTile; threads = mbs::matmul::kAnyThreads;
+        } else if (OUT == 1 && t256 >= 256) large(d);
+        else tiles<OUT, 2, 2, 4>(d);
+    }
     template <int OUT> void choose(const mb_matmul_desc *d, const mbs::matmul::Params &p, const void *a, const void *b) {
         // whole aligned pieces of 16 bytes, and a tile's rows within the 31 bits of a buffer's offsets
         const bool whole = p.k % 16 == 0 && aligned(a, 16) && aligned(b, 16) && p.k < (int64_t(1) << 22);
         const int64_t t16 = d->batch * ((p.m + 15) / 16) * ((p.n + 15) / 16), t256 = d->batch * ((p.m + 255) / 256) * ((p.n + 255) / 256);
-        if (t16 < 512) split<OUT, 1, 1>();
+        // past 2^23 of the smallest pieces a launch of theirs could have 2^32 threads
+        if (t16 >= (int64_t(1) << 23)) tiled<OUT>(d, whole, t256);
+        else if (t16 < 512) split<OUT, 1, 1>();
         else if (p.m <= 16) t16 < 1024 ? split<OUT, 1, 2>() : split<OUT, 1, 4>();
         else if (p.n <= 16) t16 < 1024 ? split<OUT, 2, 1>() : split<OUT, 4, 1>();
         else if (t16 < 1024) split<OUT, 2, 2>();
         else if (p.m <= 32) split<OUT, 2, 4>();
         else if (p.n <= 32 || t16 < 2048) split<OUT, 4, 2>();
         else if (p.m <= 64 || p.n <= 64 || t16 < 5120) split<OUT, 4, 4>();
-        else if (!whole) {
-            fn = reinterpret_cast<const void *>(&mbs::matmul::matmul_any<OUT>);
-            tile_m = tile_n = mbs::matmul::kAnyTile; threads = mbs::matmul::kAnyThreads;
-        } else if (OUT == 1 && t256 >= 256) large(d);
-        else tiles<OUT, 2, 2, 4>(d);
+        else tiled<OUT>(d, whole, t256);
     }
     MatmulPlan(const mb_matmul_desc *d, const mbs::matmul::Params &p, const void *a, const void *b) {
         if (d->out_dtype == MB_F32) choose<0>(d, p, a, b);

@@ -304,3 +304,15 @@ def test_linear(shape, n, dtype):
     g, = torch.autograd.grad(mb.linear_fp8(x, w).square().sum(), x, create_graph=True)
     with pytest.raises(RuntimeError, match="differentiate twice|once_differentiable"):
         g.square().sum().backward()
+
+
+def test_matmul_of_millions():
+    """A batch whose pieces of 64 rows would take a launch of 2^32 threads.  Whole numbers, exact."""
+    import paper_2401_13660_amd as mb
+    batch, m, k = (1 << 22) + 1, 65, 8
+    announce(f"matmul_fp8 batch {batch} of ({m}, 1, {k})")
+    a = torch.randint(-3, 4, (m, k), device="cuda:0").float()
+    b = torch.randint(-3, 4, (batch, 1, k), device="cuda:0").float()
+    one = torch.ones(batch, 1, 1, device="cuda:0")
+    c = mb.matmul_fp8(a.to(FP8), one[0].expand(m, 1).contiguous(), b.to(FP8), one, out_dtype=torch.bfloat16)
+    assert c.shape == (batch, m, 1) and torch.equal(c[:, :, 0].float(), b[:, 0] @ a.t())
