@@ -13,6 +13,8 @@ multiple of 16 (the library raises otherwise).  The convolution's backward is
 """
 from __future__ import annotations
 
+import math
+
 import torch
 from torch.autograd.function import once_differentiable
 
@@ -124,25 +126,29 @@ def rms_norm(x, weight=None, residual=None, *, eps=1e-5, out_dtype=None):
     return _RmsNorm.apply(x, weight, residual, eps, out_dtype)
 
 
+def _rows(t):
+    """t's leading dimensions as one, whatever of them is 0."""
+    return t.reshape(math.prod(t.shape[:-1]), t.shape[-1])
+
+
 class _LinearFp8(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight):
         ctx.save_for_backward(x, weight)
-        rows = x.reshape(-1, x.shape[-1])
-        y = _b.matmul_fp8(*_b.quantize_fp8(rows), *_b.quantize_fp8(weight, tile=True), out_dtype=x.dtype)
+        y = _b.matmul_fp8(*_b.quantize_fp8(_rows(x)), *_b.quantize_fp8(weight, tile=True), out_dtype=x.dtype)
         return y.view(x.shape[:-1] + (weight.shape[0],))
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
         x, weight = ctx.saved_tensors
-        dy = dy.contiguous().view(-1, weight.shape[0])
+        dy = _rows(dy.contiguous())
         dx = dw = None
         if ctx.needs_input_grad[0]:
             dx = _b.matmul_fp8(*_b.quantize_fp8(dy), *_b.quantize_fp8(weight, tile=True, transpose=True),
                                out_dtype=x.dtype).view(x.shape)
         if ctx.needs_input_grad[1]:
-            dw = _b.matmul_fp8(*_b.quantize_fp8(dy, transpose=True), *_b.quantize_fp8(x.reshape(-1, x.shape[-1]), transpose=True),
+            dw = _b.matmul_fp8(*_b.quantize_fp8(dy, transpose=True), *_b.quantize_fp8(_rows(x), transpose=True),
                                out_dtype=weight.dtype)
         return dx, dw
 

@@ -316,3 +316,20 @@ def test_matmul_of_millions():
     one = torch.ones(batch, 1, 1, device="cuda:0")
     c = mb.matmul_fp8(a.to(FP8), one[0].expand(m, 1).contiguous(), b.to(FP8), one, out_dtype=torch.bfloat16)
     assert c.shape == (batch, m, 1) and torch.equal(c[:, :, 0].float(), b[:, 0] @ a.t())
+
+
+def rows_of(shape):
+    return int(np.prod(shape, dtype=np.int64))
+
+
+@pytest.mark.parametrize("rows,k,n", [((0,), 7, 5), ((2, 0), 7, 5), ((3,), 0, 5), ((2, 3), 7, 0), ((0,), 0, 0), ((), 7, 5)])
+def test_linear_of_nothing(rows, k, n):
+    """Empty factors.  Values of 448 have a scale of 1: exact."""
+    import paper_2401_13660_amd as mb
+    announce(f"linear_fp8 {rows} x {k} to {n}")
+    x, w = (torch.full(shape, 448.0, device="cuda:0", requires_grad=True) for shape in (rows + (k,), (n, k)))
+    y = mb.linear_fp8(x, w)
+    assert y.shape == rows + (n,) and (y == 448.0 ** 2 * k).all()
+    y.backward(torch.full_like(y, 448.0))
+    assert x.grad.shape == x.shape and (x.grad == 448.0 ** 2 * n).all()
+    assert w.grad.shape == w.shape and (w.grad == 448.0 ** 2 * rows_of(rows)).all()
