@@ -3,8 +3,8 @@
 // Transposed, rows and columns are the output's: (channels, time) becomes (time, channels) with scales along the channels,
 // as a product over the channels wants it.
 //
-// Bound by memory: one reading, one writing of half or a quarter of it.  (4, 3584, 8192) in bf16, turned, takes 72 us, 4.9 TB/s
-// (88 with LDS lines of 33 words and every thread finding its columns' scales for itself); (7168, 1792) in fp32 by tiles 11.3 us, 5.7 TB/s.  Streaming loads or stores were no faster.  A workgroup takes a 128 x 128 piece of the input into
+// Bound by memory: one reading, one writing of half or a quarter of it.  (4, 3584, 8192) in bf16, turned, takes 69 us, 5.2 TB/s
+// (79 with LDS lines of 33 words and every thread finding its columns' scales for itself); (7168, 1792) in fp32 by tiles 11.3 us, 5.7 TB/s.  Streaming loads or stores were no faster.  A workgroup takes a 128 x 128 piece of the input into
 // registers, 8 columns per lane and span.  As it lies, 16 lanes hold a row's block and its largest value is theirs; transposed,
 // the lanes of one column group join theirs in LDS, and the bytes pass through LDS, 4 rows of a column to a word, so
 // that both sides of memory see whole lines.
