@@ -244,6 +244,38 @@ def test_training_step():
         assert (a - t.grad).norm() <= 2 * 2.0 ** -4 * 1.1 * t.grad.norm()
 
 
+def test_training_step_in_a_graph():
+    """Forward and gradients of the norm and the projection, captured, replayed on new inputs, against eager passes."""
+    import paper_2401_13660_amd as mb
+    announce("norm and projection in 8 bits: gradients in a graph")
+    x, r, cy, ch = (randn((2, 300, 256), k, "bf16") for k in (1, 2, 3, 4))
+    w, p = randn((256,), 5, "f32"), randn((384, 256), 6, "f32") / 16
+    c = randn((2, 300, 384), 7, "bf16")
+    leaves = [x.requires_grad_(), r.requires_grad_(), w.requires_grad_(), p.requires_grad_()]
+
+    def step():
+        y, h = mb.rms_norm(x, w, r)
+        return torch.autograd.grad([mb.linear_fp8(y, p), y, h], leaves, [c, cy, ch])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for k in range(4):
+        with torch.no_grad():
+            x.copy_(randn(x.shape, 10 + k, "bf16"))
+        want = [t.clone() for t in step()]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(held, want):
+            assert torch.equal(a, b), f"replay {k}"
+
+
 def test_example_completes():
     """The example's byte-by-byte continuation: bytes, the same for the same seed, and the model's largest logit at temperature 0."""
     import os

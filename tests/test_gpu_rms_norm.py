@@ -269,6 +269,28 @@ def test_autograd_parts():
         g.square().sum().backward()
 
 
+def test_autograd_leaves_of_one_type():
+    """Both summands are leaves of one type, or one and the same: gradients in memory of their own, added up over two passes."""
+    import paper_2401_13660_amd as mb
+    announce("rms_norm: gradients of two leaves")
+    x, r = (randn((5, 24), k, "f32").requires_grad_() for k in (1, 2))
+    w, c = randn((24,), 3, "f32"), randn((5, 24), 4, "f32")
+
+    def loss(a, b):
+        y, h = mb.rms_norm(a, w, b)
+        return (y * c).sum() + h.sum()
+    loss(x, r).backward()
+    once = x.grad.clone()
+    assert torch.equal(once, r.grad) and x.grad.data_ptr() != r.grad.data_ptr()
+    loss(x, r).backward()
+    assert torch.equal(x.grad, 2 * once) and torch.equal(r.grad, 2 * once)
+    s = randn((5, 24), 5, "f32").requires_grad_()
+    loss(s, s).backward()
+    a, b = s.detach().clone().requires_grad_(), s.detach().clone().requires_grad_()
+    loss(a, b).backward()
+    assert torch.equal(s.grad, a.grad + b.grad)
+
+
 def test_past_32_bits():
     """Rows past element 2^31, against the rows on their own."""
     import paper_2401_13660_amd as mb
