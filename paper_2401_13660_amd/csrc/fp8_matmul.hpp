@@ -373,7 +373,8 @@ __global__ __launch_bounds__(512) void matmul_large(Params p) {
 }
 
 // Rows of any length and alignment: they pass through registers on their way to LDS, cut to zeros where they end.
-// (3000, 7168, 1790) takes 123 us, 625 TFLOP/s, bound by the shifting of what is not aligned and one buffer.
+// (3000, 7168, 1790) takes 123 to 132 us, 580 to 625 TFLOP/s: two barriers a block around one buffer, and loads that begin at any byte.  With
+// rows' addresses kept in registers, whole blocks loaded without a look at their end, and matmul_tiles' order of instructions it took 135.
 constexpr int kAnyTile = 128, kAnyThreads = 256;        // 2 x 2 waves of 64 x 64
 template <int OUT>
 __global__ __launch_bounds__(kAnyThreads) void matmul_any(Params p) {
