@@ -22,34 +22,34 @@ int64_t blocks_of(int64_t n) { return n / mbs::fp8::kBlock + (n % mbs::fp8::kBlo
 // ---- norm -----------------------------------------------------------------------
 
 // Waves per row and spans per lane for a row of this width, whole spans where it is made of them; a walk past the widest.
-template <int X, int RES, int OUT> const void *norm_fn(int64_t rows, int64_t dim, int *waves) {
+template <int X, int RES, int OUT> const void *norm_fn(int64_t dim, int *waves) {
     namespace N = mbs::norm;
     const int64_t spans = (dim + 7) / 8;
     const bool cut = dim % 8 != 0;
     *waves = 4;
-    // few rows: 4 waves each, which ask for everything at once
-    if (!cut && rows <= 1024 && spans > 64 && spans <= 256) return reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, 4, 1, false>);
+    // to 8 bits, 4 waves instead of one: 32 rows of 1,792 2.6 and 4.1 us in a graph, 2,048 rows 7.6 and 9.3, 32,768 119.5 and 120.8;
+    // 32,768 rows of 640 40 and 36
+    if (!cut && spans >= 128 && spans <= 256) return reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, 4, 1, false>);
     if (spans > 256 && spans <= 768)
         return cut ? reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, 4, 3, true>)
                    : reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, 4, 3, false>);
     *waves = 1;
     if (cut && spans <= 256) return reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, 1, 4, true>);
     if (spans <= 64) return reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, 1, 1, false>);
-    if (spans <= 128) return reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, 1, 2, false>);
-    if (spans <= 256) return reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, 1, 4, false>);
+    if (spans < 128) return reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, 1, 2, false>);
     *waves = N::kLoopWaves;
     if (spans <= 2048) return reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, N::kLoopWaves, 2, true>);
     return reinterpret_cast<const void *>(&N::rms_norm_walk<X, RES, OUT>);
 }
-template <int X, int RES> const void *norm_fn(int32_t out, int64_t rows, int64_t dim, int *waves) {
-    return out == MB_F32    ? norm_fn<X, RES, 0>(rows, dim, waves)
-           : out == MB_BF16 ? norm_fn<X, RES, 1>(rows, dim, waves)
-                            : norm_fn<X, RES, mbs::norm::kFp8>(rows, dim, waves);
+template <int X, int RES> const void *norm_fn(int32_t out, int64_t dim, int *waves) {
+    return out == MB_F32    ? norm_fn<X, RES, 0>(dim, waves)
+           : out == MB_BF16 ? norm_fn<X, RES, 1>(dim, waves)
+                            : norm_fn<X, RES, mbs::norm::kFp8>(dim, waves);
 }
-template <int X> const void *norm_fn(int32_t res, int32_t out, int64_t rows, int64_t dim, int *waves) {
-    return res == MB_F32    ? norm_fn<X, 0>(out, rows, dim, waves)
-           : res == MB_BF16 ? norm_fn<X, 1>(out, rows, dim, waves)
-                            : norm_fn<X, mbs::norm::kNone>(out, rows, dim, waves);
+template <int X> const void *norm_fn(int32_t res, int32_t out, int64_t dim, int *waves) {
+    return res == MB_F32    ? norm_fn<X, 0>(out, dim, waves)
+           : res == MB_BF16 ? norm_fn<X, 1>(out, dim, waves)
+                            : norm_fn<X, mbs::norm::kNone>(out, dim, waves);
 }
 
 template <int DY, int H, int DX> const void *norm_bwd_fn(int64_t dim, int *waves) {
@@ -140,19 +140,23 @@ struct MatmulPlan {
         fn = reinterpret_cast<const void *>(&mbs::matmul::matmul_split<OUT, MI, NJ>);
         tile_m = 16 * MI; tile_n = 16 * NJ; threads = 64 * mbs::matmul::kSplit;
     }
-    template <int OUT> void tiled(const mb_matmul_desc *d, bool whole, int64_t t256) {
+    template <int OUT> void tiled(const mb_matmul_desc *d, const mbs::matmul::Params &p, bool whole) {
+        const int64_t t128 = d->batch * ((p.m + 127) / 128) * ((p.n + 127) / 128), t256 = d->batch * ((p.m + 255) / 256) * ((p.n + 255) / 256);
         if (!whole) {
             fn = reinterpret_cast<const void *>(&mbs::matmul::matmul_any<OUT>);
             tile_m = tile_n = mbs::matmul::kAnyTile; threads = mbs::matmul::kAnyThreads;
-        } else if (OUT == 1 && t256 >= 256) large(d);
+        // tiles of 256 where those of 128 do not all run at once (two per CU) and the larger ones' places are mostly used: (2176, 4096, 1792)
+        // 29.5 us against 36.5, (384, 30000, 1792) 31 and 36; but (2048, 4096, 1792) 30 and 27, 100 of (300, 300, 1792) 53 and 40, 600 of
+        // (100, 100, 1792) 76 and 45
+        } else if (OUT == 1 && t128 > 512 && 5 * t256 <= 2 * t128) large(d);
         else tiles<OUT, 2, 2, 4>(d);
     }
     template <int OUT> void choose(const mb_matmul_desc *d, const mbs::matmul::Params &p, const void *a, const void *b) {
         // whole aligned pieces of 16 bytes, and a tile's rows within the 31 bits of a buffer's offsets
         const bool whole = p.k % 16 == 0 && aligned(a, 16) && aligned(b, 16) && p.k < (int64_t(1) << 22);
-        const int64_t t16 = d->batch * ((p.m + 15) / 16) * ((p.n + 15) / 16), t256 = d->batch * ((p.m + 255) / 256) * ((p.n + 255) / 256);
+        const int64_t t16 = d->batch * ((p.m + 15) / 16) * ((p.n + 15) / 16);
         // past 2^23 of the smallest pieces a launch of theirs could have 2^32 threads
-        if (t16 >= (int64_t(1) << 23)) tiled<OUT>(d, whole, t256);
+        if (t16 >= (int64_t(1) << 23)) tiled<OUT>(d, p, whole);
         else if (t16 < 512) split<OUT, 1, 1>();
         else if (p.m <= 16) t16 < 1024 ? split<OUT, 1, 2>() : split<OUT, 1, 4>();
         else if (p.n <= 16) t16 < 1024 ? split<OUT, 2, 1>() : split<OUT, 4, 1>();
@@ -160,7 +164,7 @@ struct MatmulPlan {
         else if (p.m <= 32) split<OUT, 2, 4>();
         else if (p.n <= 32 || t16 < 2048) split<OUT, 4, 2>();
         else if (p.m <= 64 || p.n <= 64 || t16 < 5120) split<OUT, 4, 4>();
-        else tiled<OUT>(d, whole, t256);
+        else tiled<OUT>(d, p, whole);
     }
     MatmulPlan(const mb_matmul_desc *d, const mbs::matmul::Params &p, const void *a, const void *b) {
         if (d->out_dtype == MB_F32) choose<0>(d, p, a, b);
@@ -193,7 +197,7 @@ int mb_rms_norm_fwd(int64_t rows, int64_t dim, int32_t x_dtype, int32_t residual
     mbs::norm::FwdParams p{rows, dim, x, weight, residual, y, scales, residual_out, rstd, eps};
     const int32_t res = adds ? residual_dtype : -1;
     int waves;
-    const void *fn = x_dtype == MB_F32 ? norm_fn<0>(res, out_dtype, rows, dim, &waves) : norm_fn<1>(res, out_dtype, rows, dim, &waves);
+    const void *fn = x_dtype == MB_F32 ? norm_fn<0>(res, out_dtype, dim, &waves) : norm_fn<1>(res, out_dtype, dim, &waves);
     const int64_t per = waves == 1 ? 4 : 1;
     const int64_t blocks = std::min<int64_t>((rows + per - 1) / per, 1 << 20);
     return status(launch(fn, dim3((unsigned)blocks), dim3(waves == 1 ? 256 : 64 * waves), &p, stream));

@@ -184,6 +184,15 @@ def test_matmul_batches(m, n, k, ab, bb):
     check_matmul(*operand(m, k, 3, True, ab), *operand(n, k, 4, False, bb), "f32")
 
 
+@pytest.mark.parametrize("m,n,k,batch", [(4500, 4400, 16, None), (4200, 4608, 128, None), (4608, 4100, 144, None), (4100, 4300, 256, None),
+                                         (1100, 1050, 400, 8), (384, 30000, 144, None), (100, 90, 272, 600), (300, 290, 256, 100)])
+@pytest.mark.parametrize("a_tile,b_tile", [(False, True), (True, False), (False, False)])
+def test_matmul_many_tiles(m, n, k, batch, a_tile, b_tile):
+    """Many tiles of few blocks, whole and mostly empty ones, in batches."""
+    announce(f"matmul_fp8 batch {batch} of {m} x {n} x {k} tiles {a_tile} {b_tile}")
+    check_matmul(*operand(m, k, 1, a_tile, batch), *operand(n, k, 2, b_tile, batch), "bf16")
+
+
 @pytest.mark.parametrize("shift", [1, 2, 4, 8, 15])
 def test_matmul_alignment(shift):
     announce(f"matmul_fp8 at addresses {shift} bytes on")
