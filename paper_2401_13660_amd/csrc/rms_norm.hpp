@@ -159,20 +159,17 @@ __global__ __launch_bounds__(W == 1 ? 256 : 64 * W) void rms_norm_rows(FwdParams
             // ahead where the registers are there for it; rows of more spans hide its latency behind each other
             if (J == 1) load_weight<CUT>(p.weight, col, within<CUT>(p.dim, col), w[j]);
         }
-        // A wave alone adds up its spans' sums as four waves of a span each would: a row's bits do not hang on how many rows there are.
-        float sum = 0.0f, whole = 0.0f;
+        float sum = 0.0f;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const int64_t col = 8 * (j * 64 * W + t);
             in[j].add(p, at + col, within<CUT>(p.dim, col), h[j]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum = __builtin_fmaf(h[j][i], h[j][i], sum);
-            if constexpr (W == 1) {
-                whole = j == 0 ? wave_sum(sum) : whole + wave_sum(sum);
-                sum = 0.0f;
-            }
         }
+        float whole;
         if constexpr (W > 1) whole = row_sum<W>(sum, red, round);
+        else whole = wave_sum(sum);
         const float r = inverse_length(whole, p);
 #pragma unroll
         for (int j = 0; j < J; ++j) {
