@@ -111,7 +111,8 @@ template <int DT> const void *sample_fn(int64_t vocab, unsigned *threads) {
     if (vocab <= 256) return reinterpret_cast<const void *>(&S::sample_rows<DT, 64, 1>);
     if (vocab <= 1024) return reinterpret_cast<const void *>(&S::sample_rows<DT, 256, 1>);
     if (vocab <= 8192) return reinterpret_cast<const void *>(&S::sample_rows<DT, 1024, 2>);
-    return reinterpret_cast<const void *>(&S::sample_rows<DT, 1024, 0>);
+    if (vocab < S::kLongRow) return reinterpret_cast<const void *>(&S::sample_rows<DT, 1024, 0>);
+    return reinterpret_cast<const void *>(&S::sample_rows<DT, 1024, 0, true>);
 }
 
 // Which kernel takes a product, and its tiles.

@@ -11,7 +11,8 @@
 // they weigh, the bin in which the wanted count or weight is reached is found by a running sum over the bins, and its few
 // tokens are ranked one by one.  A bin of more than 256 of them (logits far apart from the rest, equals by the hundred) is
 // counted once more into bins of its own, of ranks.  Weights are summed as integers of 2^-44: sums do not depend
-// on the order of the atomics, and a border does not move from call to call.
+// on the order of the atomics, and a border does not move from call to call.  2^20 tokens' weights could pass 64 bits of those: rows
+// that long are summed once before, in 64-bit floats, and their unit is between 2^-63 and 2^-62 of that sum.
 //
 // One workgroup per sequence, the row in registers from one load to the token drawn (up to 8,192 tokens; beyond, it is read
 // again from the cache); the kept tokens go to a list, and random numbers are only read for those.  The race takes the hardware's
@@ -69,13 +70,17 @@ __device__ __forceinline__ uint32_t order_of(float l) {
 }
 __device__ __forceinline__ uint64_t rank_of(float l, uint32_t y) { return (uint64_t)order_of(l) << 32 | (uint32_t)~y; }
 
-// e in [0, 1] in units of 2^-44; what is below half of one counts as nothing.
-__device__ __forceinline__ uint64_t units_of(float e) {
+// Tokens from which on a row's unit goes by its sum, and 2^-bits, the unit of all shorter rows.
+constexpr int64_t kLongRow = int64_t(1) << 20;
+constexpr int kBits = 44;
+
+// e in [0, 1] in units of 2^-bits; what is below half of one counts as nothing.
+__device__ __forceinline__ uint64_t units_of(float e, int bits) {
     const uint32_t u = __float_as_uint(e), down = 127 - (u >> 23);
-    return ((uint64_t)((u & 0x7fffffu) | 0x800000u) << 21) >> min(down, 63u);
+    return ((uint64_t)((u & 0x7fffffu) | 0x800000u) << (bits - 23)) >> min(down, 63u);
 }
-__device__ __forceinline__ uint64_t units_of(double e) {
-    const double v = e * 17592186044416.0;          // 2^44
+__device__ __forceinline__ uint64_t units_of(double e, int bits) {
+    const double v = e * (double)(1ull << bits);
     const uint32_t high = (uint32_t)(v * (1.0 / 4294967296.0));
     return (uint64_t)high << 32 | (uint32_t)__builtin_fma((double)high, -4294967296.0, v);
 }
@@ -263,7 +268,8 @@ template <int T> struct Shared {
     uint32_t bad;
 };
 
-template <int DT, int T, int S>
+// LONG: rows of kLongRow tokens and more.
+template <int DT, int T, int S, bool LONG = false>
 __global__ __launch_bounds__(T) void sample_rows(Params p) {
     using Sh = Shared<T>;
     constexpr int kBins = Sh::kBins, kWaves = Sh::kWaves, kList = Sh::kList;
@@ -308,6 +314,20 @@ __global__ __launch_bounds__(T) void sample_rows(Params p) {
         return;
     }
 
+    int bits = kBits;
+    if constexpr (LONG) {
+        // so many that the sum, 2^x at least and less than 2^(x + 1), is below 2^63; x is 0 to 30
+        double all = 0.0;
+        row.each([&](uint32_t, float l) { all += (double)row.weight(l); });
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2) all += __shfl_xor(all, m);
+        if (lane == 0) sh.weights[wave] = all;
+        __syncthreads();
+        all = 0.0;
+        for (int w = 0; w < kWaves; ++w) all += sh.weights[w];
+        bits = 62 - ilogb(all);
+    }
+
     uint64_t border = 0;                            // the least rank kept; 0: all are
     const bool by_count = f.top_k < row.vocab, by_weight = f.top_p < 1.0f;
     if (by_count || by_weight) {
@@ -344,7 +364,7 @@ __global__ __launch_bounds__(T) void sample_rows(Params p) {
                             to = (uint32_t)((high_rank - rank) >> shift);
                         }
                         if (by_count) atomicAdd(&sh.count[to], 1u);
-                        if (by_weight) atomicAdd(reinterpret_cast<unsigned long long *>(&sh.weight[to]), (unsigned long long)units_of(row.weight(l)));
+                        if (by_weight) atomicAdd(reinterpret_cast<unsigned long long *>(&sh.weight[to]), (unsigned long long)units_of(row.weight(l), bits));
                     });
                     counted = whole;
                 }
@@ -420,7 +440,7 @@ __global__ __launch_bounds__(T) void sample_rows(Params p) {
                     const uint32_t at = atomicAdd(&sh.listed, 1u);
                     if (at >= kList) return;
                     sh.list[at] = rank;
-                    sh.list_weight[at] = by_weight ? units_of(row.weight(l)) : 0;
+                    sh.list_weight[at] = by_weight ? units_of(row.weight(l), bits) : 0;
                 });
                 if (most) {
                     atomicMin(reinterpret_cast<unsigned long long *>(&sh.low), (unsigned long long)least);
@@ -479,7 +499,7 @@ __global__ __launch_bounds__(T) void sample_rows(Params p) {
     auto run_race = [&](uint32_t y, float l, float noise) {
         const typename R::Weight e = row.weight(l);
         if (!(e > 0 && e >= f.min_p)) return;
-        sum += units_of(e);
+        sum += units_of(e, bits);
         const float s = (float)e * hw_rcp(noise);
         if (s > best || (s == best && s > 0.0f && (int32_t)y < at)) {
             best = s;
@@ -544,7 +564,7 @@ __global__ __launch_bounds__(T) void sample_rows(Params p) {
             if (winner < 0 || sh.scores[w] > sh.scores[winner] || (sh.scores[w] == sh.scores[winner] && sh.who[w] < sh.who[winner])) winner = w;
         }
         p.token[b] = winner < 0 ? -1 : sh.who[winner];
-        if (p.prob) p.prob[b] = winner < 0 ? 0.0f : (float)(sh.weights[winner] * 17592186044416.0 / (double)sum);
+        if (p.prob) p.prob[b] = winner < 0 ? 0.0f : (float)(sh.weights[winner] * (double)(1ull << bits) / (double)sum);
     }
 }
 
