@@ -127,25 +127,25 @@ def rms_norm(x, weight=None, residual=None, *, eps=1e-5, out_dtype=None):
 
 
 def _rows(t):
-    """t's leading dimensions as one, whatever of them is 0."""
-    return t.reshape(math.prod(t.shape[:-1]), t.shape[-1])
+    """t's leading dimensions as one, whatever of them is 0, as a dense matrix: a copy where t is strided."""
+    return t.contiguous().view(math.prod(t.shape[:-1]), t.shape[-1])
 
 
 class _LinearFp8(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight):
         ctx.save_for_backward(x, weight)
-        y = _b.matmul_fp8(*_b.quantize_fp8(_rows(x)), *_b.quantize_fp8(weight, tile=True), out_dtype=x.dtype)
+        y = _b.matmul_fp8(*_b.quantize_fp8(_rows(x)), *_b.quantize_fp8(weight.contiguous(), tile=True), out_dtype=x.dtype)
         return y.view(x.shape[:-1] + (weight.shape[0],))
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
         x, weight = ctx.saved_tensors
-        dy = _rows(dy.contiguous())
+        dy = _rows(dy)
         dx = dw = None
         if ctx.needs_input_grad[0]:
-            dx = _b.matmul_fp8(*_b.quantize_fp8(dy), *_b.quantize_fp8(weight, tile=True, transpose=True),
+            dx = _b.matmul_fp8(*_b.quantize_fp8(dy), *_b.quantize_fp8(weight.contiguous(), tile=True, transpose=True),
                                out_dtype=x.dtype).view(x.shape)
         if ctx.needs_input_grad[1]:
             dw = _b.matmul_fp8(*_b.quantize_fp8(dy, transpose=True), *_b.quantize_fp8(_rows(x), transpose=True),
@@ -155,7 +155,11 @@ class _LinearFp8(torch.autograd.Function):
 
 def linear_fp8(x, weight):
     """Differentiable projection x (..., k) by weight (n, k), each fp32 or bf16, with every product in 8 bits: (..., n) in
-    x's type.  x and the gradient are quantised per row and the weight per tile, as ``quantize_fp8`` does it; the weight's
-    gradient is the product of both per column, along the rows.  Gradients are those of the unrounded product, taken
-    once: a second derivative raises."""
+    x's type.  Both may be strided; they are copied for each of their products then.  x and the gradient are quantised per
+    row and the weight per tile, as ``quantize_fp8`` does it; the weight's gradient is the product of both per column,
+    along the rows.  Gradients are those of the unrounded product, taken once: a second derivative raises."""
+    if not isinstance(x, torch.Tensor) or x.dim() < 1:
+        raise _b.MBScanError("x must be a (..., k) tensor")
+    if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
+        raise _b.MBScanError("weight must be a (n, k) tensor")
     return _LinearFp8.apply(x, weight)
