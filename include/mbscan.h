@@ -576,6 +576,7 @@ int mb_matmul_fp8(const mb_matmul_desc *desc, const void *a, const float *a_scal
  *   token = the y with the largest e(y) / noise(y) of the kept, the lowest such y
  *   prob  = e(token) / the kept tokens' sum: the probability that it was drawn with
  *
+ * The race is in fp32: an e below 2^-126 may count as 0 there and cannot win then, quotients past fp32's range are all infinite.
  * With exponential noise of mean 1 tokens are distributed as the filtered probabilities.  Temperature 0 takes the
  * largest logit, whatever the noise.  A row of logits that is no distribution (as for mb_verify_sample) gives token -1 and
  * prob 0; so does a row whose noise lets no token win.  -infinity masks a token.

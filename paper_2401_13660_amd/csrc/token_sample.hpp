@@ -15,10 +15,10 @@
 // that long are summed once before, in 64-bit floats, and their unit is between 2^-63 and 2^-62 of that sum.
 //
 // One workgroup per sequence, the row in registers from one load to the token drawn (up to 8,192 tokens; beyond, it is read
-// again from the cache); the kept tokens go to a list, and random numbers are only read for those.  The race takes the hardware's
-// reciprocal of the noise, which is within a step of it and takes a noise below 2^-126 for 0.  Bound by latency and, for large vocabularies, by one CU's
-// instructions: about 25 per token for the weight and its bin.  Replayed from a graph, without a filter, with top-k, top-p and both:
-// (32, 256) in fp32 3.7, 6.8, 6.2 and 8.5 us; (16, 32,000) in bf16 17, 23, 30 and 32; (16, 131,072) 52, 63, 124 and 91.  With a
+// again from the cache); the kept tokens go to a list, and random numbers are only read for those.  The race divides, as verify_sample's does:
+// times the hardware's reciprocal, (16, 131,072) without a filter took 52 us, but a noise below 2^-126 counted as 0.  Bound by latency and, for large vocabularies, by one CU's
+// instructions: about 25 per token for the weight and its bin, 10 for the quotient.  Replayed from a graph, without a filter, with top-k, top-p and both:
+// (32, 256) in fp32 3.8, 6.5, 6.4 and 8.4 us; (16, 32,000) in bf16 18, 23, 30 and 32; (16, 131,072) 57, 63, 129 and 91.  With a
 // row's pieces among several workgroups, three launches, (16, 32,000) with top-p took 36.
 #pragma once
 
@@ -500,7 +500,7 @@ __global__ __launch_bounds__(T) void sample_rows(Params p) {
         const typename R::Weight e = row.weight(l);
         if (!(e > 0 && e >= f.min_p)) return;
         sum += units_of(e, bits);
-        const float s = (float)e * hw_rcp(noise);
+        const float s = (float)e / noise;
         if (s > best || (s == best && s > 0.0f && (int32_t)y < at)) {
             best = s;
             at = (int32_t)y;
