@@ -119,15 +119,23 @@ template <int DT, int T, int S, class W> struct Row {
     int64_t at;
     uint32_t vocab;
     float max, inv_temp;
-    float per, per_rest, least;                     // log2 e / T and what it lacks, and the least difference told from others
+    // From T = 1 on differences of half logits are taken, as those of whole ones could overflow and yet weigh something.
+    float scale, top;                               // 1 or 1/2, and the largest logit times it
+    float per, per_rest, least;                     // log2 e / (T scale) and what it lacks, and the least difference told from others
     Span<DT, 4> s[S > 0 ? S : 1];
 
     __device__ __forceinline__ void set_temperature(float inv) {
-        const double exact = 1.4426950408889634 * (double)inv;
         inv_temp = inv;
+        scale = inv <= 1.0f ? 0.5f : 1.0f;
+        const double exact = 1.4426950408889634 * (double)inv / (double)scale;
         per = __builtin_fminf((float)exact, 3.0e38f);
         per_rest = exact < 3.0e38 ? (float)(exact - (double)per) : 0.0f;
         least = -200.0f / per;
+    }
+
+    __device__ __forceinline__ void set_max(float m) {
+        max = m;
+        top = m * scale;
     }
 
     __device__ __forceinline__ static uint32_t first_of(uint32_t k) { return (k * T + threadIdx.x) * 4; }
@@ -211,7 +219,7 @@ template <int DT, int T, int S, class W> struct Row {
             return exp(((double)l - (double)max) * (double)inv_temp);
         } else {
             // 2^(d log2 e / T), with what the product's rounding left over as a factor; below 2^-200 all is alike
-            const float d = __builtin_fmaxf(l - max, least), t = d * per;
+            const float d = __builtin_fmaxf(__builtin_fmaf(l, scale, -top), least), t = d * per;
             const float left = __builtin_fmaf(d, per_rest, __builtin_fmaf(d, per, -t)), e = hw_exp2(t);
             return __builtin_fmaf(e, left * kLn2, e);
         }
@@ -305,7 +313,7 @@ __global__ __launch_bounds__(T) void sample_rows(Params p) {
         ends.y = __builtin_fminf(ends.y, sh.lows[w]);
     }
     const float top = ends.x;
-    row.max = top;
+    row.set_max(top);
     if (!(top < __builtin_inff()) || top == -__builtin_inff()) {            // the same in every thread
         if (t == 0) {
             p.token[b] = -1;
