@@ -581,7 +581,7 @@ int mb_matmul_fp8(const mb_matmul_desc *desc, const void *a, const float *a_scal
  * largest logit, whatever the noise.  A row of logits that is no distribution (as for mb_verify_sample) gives token -1 and
  * prob 0; so does a row whose noise lets no token win.  -infinity masks a token.
  *
- *   temperature, top_k, top_p, min_p   for every sequence: temperature 0, or > 0 with it and its inverse finite; top_p
+ *   temperature, top_k, top_p, min_p   for every sequence: temperature 0, or > 2^-127 and finite; top_p
  *                  not NaN; min_p <= 1 (MB_ERR_UNSUPPORTED otherwise)
  *   temperatures, top_ks, top_ps, min_ps   float (top_ks: int32) (batch) DEVICE memory: one for each sequence instead;
  *                  a sequence for which they are out of those ranges gives token -1 and prob 0.  NULL: the ones above

@@ -316,7 +316,7 @@ int mb_sample(int64_t batch, int64_t vocab, int32_t logit_dtype, float temperatu
     if (batch < 0 || vocab < 1 || vocab >= (int64_t(1) << 30) || batch >= int64_t(1) << 22 || !mul_ok(batch, vocab, &elems)) return MB_ERR_SHAPE;
     if (!valid_dtype(logit_dtype)) return MB_ERR_DTYPE;
     if (!temperatures && temperature != 0.0f &&
-        (!(temperature > 0.0f) || std::isinf(temperature) || std::isinf(1.0f / temperature))) return MB_ERR_UNSUPPORTED;
+        (!(temperature > 0.0f) || std::isinf(temperature) || std::isinf(2.0f / temperature))) return MB_ERR_UNSUPPORTED;
     if ((!top_ps && std::isnan(top_p)) || (!min_ps && !(min_p <= 1.0f))) return MB_ERR_UNSUPPORTED;
     if (batch == 0) return MB_OK;
     if (!logits || !noise || !token) return MB_ERR_NULL;

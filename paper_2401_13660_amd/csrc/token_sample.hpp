@@ -59,7 +59,7 @@ struct Filter {
         greedy = t == 0.0f;
         inv_temp = greedy ? 1.0f : 1.0f / t;
         top_k = greedy ? 1 : (uint32_t)(k <= 0 || k > p.vocab ? p.vocab : k);
-        ok = t >= 0.0f && t < __builtin_inff() && inv_temp < __builtin_inff() && top_p == top_p && min_p <= 1.0f;
+        ok = t >= 0.0f && t < __builtin_inff() && 2.0f * inv_temp < __builtin_inff() && top_p == top_p && min_p <= 1.0f;
     }
 };
 
@@ -128,8 +128,8 @@ template <int DT, int T, int S, class W> struct Row {
         inv_temp = inv;
         scale = inv <= 1.0f ? 0.5f : 1.0f;
         const double exact = 1.4426950408889634 * (double)inv / (double)scale;
-        per = __builtin_fminf((float)exact, 3.0e38f);
-        per_rest = exact < 3.0e38 ? (float)(exact - (double)per) : 0.0f;
+        per = (float)exact;                         // finite, as 2 / T is
+        per_rest = (float)(exact - (double)per);
         least = -200.0f / per;
     }
 

@@ -40,3 +40,22 @@ def test_largest(V, logits, temperature):
     for kw in (dict(), dict(top_p=0.9999999), dict(top_k=5)):
         for got, ref in zip(shares(V, logits, temperature, **kw), want):
             assert abs(got - ref) <= TOL * ref, kw
+
+
+@pytest.mark.parametrize("V", VOCABS)
+def test_smallest(V):
+    """Down to 2^-127, subnormal temperatures and logits; below it they are refused, as numbers and row by row."""
+    import paper_2401_13660_amd as mb
+    for temperature, other in ((2.0 ** -126, -2.0 ** -126), (2.0 ** -127 * 1.01, -2.0 ** -128), (6e-39, -9e-39), (1e-30, -2e-30)):
+        announce(f"sample of {V} at temperature {temperature}")
+        t, b = (float(torch.tensor(v, dtype=torch.float32)) for v in (temperature, other))
+        want = [1 / (1 + math.exp(b / t)), 1 / (1 + math.exp(-b / t))]
+        for got, ref in zip(shares(V, (0.0, other), temperature), want):
+            assert abs(got - ref) <= TOL * ref
+    logits, noise = torch.zeros(2, V, device="cuda:0"), torch.ones(2, V, device="cuda:0")
+    for temperature in (2.0 ** -127, 4e-39, 3e-39):
+        with pytest.raises(mb.MBScanError):
+            mb.sample(logits, noise, temperature=temperature)
+        t = torch.tensor([temperature, 1.0], device="cuda:0")
+        token, prob = mb.sample(logits, noise, temperature=t, return_prob=True)
+        assert token.tolist() == [-1, 0] and prob[0] == 0
