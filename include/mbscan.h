@@ -497,7 +497,7 @@ int64_t mb_verify_sample_workspace(int64_t batch, int64_t ndraft, int64_t vocab)
  *   y            out_dtype (rows, dim)       fp32, bf16 or MB_FP8
  *   scales       float (rows, ceil(dim/128)) with MB_FP8 (required): those of y's blocks, as mb_quantize_fp8's
  *   residual_out (rows, dim)                 h, in residual's type; may be residual
- *   rstd         float (rows)                for the gradient; NULL means not written
+ *   rstd         float (rows)                for the gradient, NaN where dim is 0; NULL means not written
  * Outputs overlap nothing else.  eps finite, >= 0 (MB_ERR_UNSUPPORTED otherwise); dim below 2^25.  Arithmetic is fp32,
  * squares included: a row of elements above 1e19 has rstd 0.
  */

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import math
 import os
 import warnings
 
@@ -769,7 +770,7 @@ def _norm_inputs(x, weight, residual):
         _need(weight, "weight", (d,), torch.float32, dev)
     if residual is not None:
         _need(residual, "residual", x.shape, None, dev)
-    return x.numel() // d if d else 0, d, dev
+    return math.prod(x.shape[:-1]), d, dev
 
 
 def _norm(x, weight, residual, eps, code, y, scales, residual_out, rstd, rows, d, dev):

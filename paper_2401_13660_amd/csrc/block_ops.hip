@@ -185,8 +185,8 @@ int mb_rms_norm_fwd(int64_t rows, int64_t dim, int32_t x_dtype, int32_t residual
     const bool fp8 = out_dtype == MB_FP8, adds = residual || residual_out;
     if (!valid_dtype(x_dtype) || (!valid_dtype(out_dtype) && !fp8) || (adds && !valid_dtype(residual_dtype))) return MB_ERR_DTYPE;
     if (!(eps >= 0.0f) || std::isinf(eps)) return MB_ERR_UNSUPPORTED;
-    if (elems == 0) return MB_OK;
-    if (!x || !y || (adds && (!residual || !residual_out)) || (fp8 && !scales)) return MB_ERR_NULL;
+    if (elems == 0 && (rows == 0 || !rstd)) return MB_OK;       // rows without columns have a rstd all the same
+    if (elems > 0 && (!x || !y || (adds && (!residual || !residual_out)) || (fp8 && !scales))) return MB_ERR_NULL;
     const size_t xsz = dtype_size(x_dtype), rsz = dtype_size(residual_dtype), ysz = fp8 ? 1 : dtype_size(out_dtype);
     if (!aligned(x, xsz) || !aligned(y, ysz) || !aligned(residual, rsz) || !aligned(residual_out, rsz)) return MB_ERR_ALIGN;
     if (!aligned(weight, 4) || !aligned(scales, 4) || !aligned(rstd, 4)) return MB_ERR_ALIGN;
