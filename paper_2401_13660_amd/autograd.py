@@ -101,7 +101,7 @@ class _RmsNorm(torch.autograd.Function):
         res = _b.rms_norm_fwd(x, weight, residual, eps=eps, out_dtype=out_dtype, return_rstd=True)
         y, rstd = res[0], res[-1]
         h = x if residual is None else res[1]
-        ctx.xtype, ctx.ytype, ctx.added = x.dtype, y.dtype, residual is not None
+        ctx.xtype, ctx.added = x.dtype, residual is not None
         ctx.set_materialize_grads(False)
         ctx.save_for_backward(h, rstd, weight)
         return y if residual is None else (y, h)

@@ -120,15 +120,12 @@ struct MatmulPlan {
     const void *fn;
     int64_t tile_m, tile_n;
     unsigned threads;
-    template <int OUT, int ONE, int WM, int WN, int MI> void tiles() {
-        using S = mbs::matmul::Shape<WM, WN, MI>;
-        fn = reinterpret_cast<const void *>(&mbs::matmul::matmul_tiles<OUT, ONE, WM, WN, MI>);
-        tile_m = S::kM; tile_n = S::kN; threads = S::kThreads;
-    }
-    template <int OUT, int WM, int WN, int MI> void tiles(const mb_matmul_desc *d) {
-        if (d->a_tile) tiles<OUT, 1, WM, WN, MI>();
-        else if (d->b_tile) tiles<OUT, 2, WM, WN, MI>();
-        else tiles<OUT, 0, WM, WN, MI>();
+    template <int OUT> void tiles(const mb_matmul_desc *d) {
+        namespace M = mbs::matmul;
+        fn = d->a_tile   ? reinterpret_cast<const void *>(&M::matmul_tiles<OUT, 1>)
+             : d->b_tile ? reinterpret_cast<const void *>(&M::matmul_tiles<OUT, 2>)
+                         : reinterpret_cast<const void *>(&M::matmul_tiles<OUT, 0>);
+        tile_m = M::Tile128::kM; tile_n = M::Tile128::kN; threads = M::Tile128::kThreads;
     }
     void large(const mb_matmul_desc *d) {
         namespace M = mbs::matmul;
@@ -150,7 +147,7 @@ struct MatmulPlan {
         // 29.5 us against 36.5, (384, 30000, 1792) 31 and 36; but (2048, 4096, 1792) 30 and 27, 100 of (300, 300, 1792) 53 and 40, 600 of
         // (100, 100, 1792) 76 and 45
         } else if (OUT == 1 && t128 > 512 && 5 * t256 <= 2 * t128) large(d);
-        else tiles<OUT, 2, 2, 4>(d);
+        else tiles<OUT>(d);
     }
     template <int OUT> void choose(const mb_matmul_desc *d, const mbs::matmul::Params &p, const void *a, const void *b) {
         // whole aligned pieces of 16 bytes, and a tile's rows within the 31 bits of a buffer's offsets

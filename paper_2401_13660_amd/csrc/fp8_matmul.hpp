@@ -195,9 +195,11 @@ template <int OUT, int MI> __device__ __forceinline__ void store_tile(const Para
         if (whole || first + 16 * i < p.m) store_columns<OUT>(p.c, at + 16 * i * p.n, g, acc[i], whole ? 64 : p.n - n);
 }
 
-template <int OUT, int ONE, int WM, int WN, int MI>
-__global__ __launch_bounds__(64 * WM * WN) void matmul_tiles(Params p) {
-    using S = Shape<WM, WN, MI>;
+using Tile128 = Shape<2, 2, 4>;
+template <int OUT, int ONE>
+__global__ __launch_bounds__(Tile128::kThreads) void matmul_tiles(Params p) {
+    using S = Tile128;
+    constexpr int WM = 2, MI = 4;
     __shared__ __align__(128) uint8_t la0[S::kM * kBlock], lb0[S::kN * kBlock], la1[S::kM * kBlock], lb1[S::kN * kBlock];
     __shared__ __align__(16) float ls0[S::kM + S::kN], ls1[S::kM + S::kN];
     const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
