@@ -499,7 +499,7 @@ int64_t mb_verify_sample_workspace(int64_t batch, int64_t ndraft, int64_t vocab)
  *   residual_out (rows, dim)                 h, in residual's type; may be residual
  *   rstd         float (rows)                for the gradient, NaN where dim is 0; NULL means not written
  * Outputs overlap nothing else.  eps finite, >= 0 (MB_ERR_UNSUPPORTED otherwise); dim below 2^25.  Arithmetic is fp32,
- * squares included: a row of elements above 1e19 has rstd 0.
+ * squares included: a row of elements above 1e19 has rstd 0, and one of elements below 1e-23 that of a row of zeros.
  */
 int mb_rms_norm_fwd(int64_t rows, int64_t dim, int32_t x_dtype, int32_t residual_dtype, int32_t out_dtype, float eps,
                     const void *x, const float *weight, const void *residual, void *y, float *scales, void *residual_out,
@@ -560,7 +560,9 @@ typedef struct {
  *   c         out_dtype (batch, m, n), overlaps nothing else
  * Scaling, by the product of a block's two scales, and the sum over blocks of 128 are fp32, rounded once to out_dtype.
  * Within a block: fp32 for an fp32 c; for a bf16 c the matrix unit first sums 8 neighbouring products at a time, each to
- * 2^-13 of the largest of the 8, and those sums in fp32.  The same bits on every call.  k = 0 gives zeros.  m, n and k
+ * 2^-13 of the largest of the 8, and those sums in fp32.  The same bits on every call.  Nothing depends on the values of the
+ * other rows, columns and products, but their numbers choose the kernel, and with it the order in which blocks are summed: past
+ * k = 128 a product's bits may be others in a batch of another size.  k = 0 gives zeros.  m, n and k
  * below 2^30, batch * ceil(m/128) * ceil(n/128) below 2^23.
  */
 int mb_matmul_fp8(const mb_matmul_desc *desc, const void *a, const float *a_scales, const void *b, const float *b_scales,

@@ -157,7 +157,8 @@ def linear_fp8(x, weight):
     """Differentiable projection x (..., k) by weight (n, k), each fp32 or bf16, with every product in 8 bits: (..., n) in
     x's type.  Both may be strided; they are copied for each of their products then.  x and the gradient are quantised per
     row and the weight per tile, as ``quantize_fp8`` does it; the weight's gradient is the product of both per column,
-    along the rows.  Gradients are those of the unrounded product, taken once: a second derivative raises."""
+    along the rows, and in fp32 for an fp32 weight, which takes twice as long.  Gradients are those of the unrounded
+    product, taken once: a second derivative raises."""
     if not isinstance(x, torch.Tensor) or x.dim() < 1:
         raise _b.MBScanError("x must be a (..., k) tensor")
     if not isinstance(weight, torch.Tensor) or weight.dim() != 2:

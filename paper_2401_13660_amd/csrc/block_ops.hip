@@ -28,7 +28,7 @@ template <int X, int RES, int OUT> const void *norm_fn(int64_t dim, int *waves) 
     const bool cut = dim % 8 != 0;
     *waves = 4;
     // to 8 bits, 4 waves instead of one: 32 rows of 1,792 2.6 and 4.1 us in a graph, 2,048 rows 7.6 and 9.3, 32,768 119.5 and 120.8;
-    // 32,768 rows of 640 40 and 36
+    // of 1,024 (half of the waves have nothing) 32 rows 2.2 and 2.8, 2,048 rows 5.0 and 5.4, 32,768 67 and 70; but 32,768 rows of 640 40 and 36
     if (!cut && spans >= 128 && spans <= 256) return reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, 4, 1, false>);
     if (spans > 256 && spans <= 768)
         return cut ? reinterpret_cast<const void *>(&N::rms_norm_rows<X, RES, OUT, 4, 3, true>)

@@ -280,9 +280,9 @@ __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::
 // For a C of 16 bits (widened operands do not fit beside 128 sums).
 //
 // (32768, 7168, 1792) with tiles' scales on b takes 468 us, 1800 TFLOP/s (638 in tiles of 128; a large product in bf16 by the
-// library runs at 1218, one in this type at 2670).  The matrix units are busy 41% of the time.  Bound by what else a SIMD's two waves
-// issue: 1 VALU instruction per result, block and side's scale.  In a copy without the scaling it took 16% less, without the
-// operands' reads 3%, without memory's 8%.  Streaming stores of C cost 11%.
+// library runs at 1218, one in this type at 2670).  The matrix units are busy 41% of the time.  What a SIMD's two waves issue beside them
+// is part of the rest: the scaling, 1 VALU instruction per result, block and side's scale (16% less time in a copy without), the operands' reads (3%)
+// and memory's (8%).  What holds the turns up beyond that was not measured.  Streaming stores of C cost 11%.
 template <int ONE>
 __global__ __launch_bounds__(512) void matmul_large(Params p) {
     constexpr int MI = 8, kHalf = MI / 2;

@@ -10,7 +10,7 @@
 // Bound by memory: every tensor passes once.  (32,768, 1792) in bf16 with a residual in fp32 takes 129 us, 5.4 TB/s, and its gradient
 // 184 us, 5.1 TB/s, where a 1 GiB copy runs at 5.1; (2042, 1536) in fp32 the gradient 13 us, two launches that wait for chains of
 // loads; 32 rows to 8 bits 6.7 us a call, of which the kernel is 3.2.  Streaming loads or stores cost the forward 6 to 17%.  A row stays in registers between its sum and its
-// output: 8 columns per lane and span, up to kSpans spans per lane, a wave per row for narrow ones (no
+// output: 8 columns per lane and span, J spans (1 to 4) per lane, a wave per row for narrow ones (no
 // barrier; four rows per workgroup), several waves per row beyond, and a walk that reads its row twice past that.
 // The gradient's waves keep dw's sums of their columns in registers from row to row; a workgroup's sums are
 // joined in LDS, and a second launch joins the workgroups' in a fixed order.

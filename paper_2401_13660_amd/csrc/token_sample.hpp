@@ -74,7 +74,7 @@ __device__ __forceinline__ uint64_t rank_of(float l, uint32_t y) { return (uint6
 constexpr int64_t kLongRow = int64_t(1) << 20;
 constexpr int kBits = 44;
 
-// e in [0, 1] in units of 2^-bits; what is below half of one counts as nothing.
+// e in [0, 1] in units of 2^-bits, cut: what is below one counts as nothing.
 __device__ __forceinline__ uint64_t units_of(float e, int bits) {
     const uint32_t u = __float_as_uint(e), down = 127 - (u >> 23);
     return ((uint64_t)((u & 0x7fffffu) | 0x800000u) << (bits - 23)) >> min(down, 63u);
